@@ -326,6 +326,66 @@ int spark_measure_read(spark_ctx *ctx, const void *buf, size_t bytes, int32_t re
  * SPARK_EINVAL for an unknown name. */
 int spark_tune(spark_ctx *ctx, const char *name, int32_t value);
 
+/* ---- Operators on 8-bit rows -------------------------------------------------------------------
+ *
+ * A decoding step streams every projection matrix once (Sec. IV-B.3), a prompt multiplies them with
+ * many rows: both get shorter with weights and activations in 8 bits.  These calls need no context;
+ * spark_scaled_projections below puts them under the layers of one.
+ *
+ * 8-bit rows: m rows of k values are `codes`, uint8 [m][kp] of e4m3 numbers (4 exponent, 3 fraction
+ * bits, largest 448, no infinities), kp = k rounded up to a multiple of 128, zeros behind k; and
+ * `powers`, uint8 [m][pitch], pitch = kp / 128 rounded up to a multiple of 4: a byte b for every 128
+ * codes of a row, which stand for code * 2^(b - 127); 127 behind kp / 128.  The power is the smallest
+ * of 2^-126 and up for which no magnitude of the block passes 448 (a block of zeros: 2^0); values are
+ * rounded to the nearest code, half to even.  A NaN or infinity becomes e4m3's NaN and has no part in
+ * the block's power.  codes 16-byte, powers 4-byte aligned.
+ *
+ * In all of them: pointers are [device] unless marked, of the current device, on which hip_stream
+ * (NULL: its default stream) has to be as well; nothing is allocated, copied or waited for, so the calls
+ * may be captured into a graph; strides count elements from row to row and are at least the row's
+ * length; m == 0 is a call that does nothing; n and k are 1 .. 2^24.  Outputs must not overlap inputs
+ * except where it says so.  SPARK_EINVAL: a NULL pointer, a size, stride, type or alignment outside
+ * these limits (nothing is launched); SPARK_ENOMEM: packed or workspace too small; SPARK_EHIP: the
+ * launch failed. */
+
+/* x [m][k] of SPARK_DTYPE_* -> 8-bit rows. */
+int spark_scaled_rows(const void *x, int32_t dtype, int64_t stride, int32_t m, int32_t k, void *codes,
+                      void *powers, void *hip_stream);
+
+/* The residual's addition and the RMSNorm behind it: h' = h + y, rounded once to h's type and written to
+ * h_out (which may be h itself), then the 8-bit rows of h' / sqrt(mean h'^2 + eps) * gain, worked out in
+ * 64 bits, so that every code is the one this formula gives.  h, h_out [m][k] of h_dtype; y [m][k] of
+ * y_dtype, or NULL: h' = h; gain fp32 [k]; eps >= 0 (a row of zeros with eps 0 gives NaN codes). */
+int spark_scaled_norm(const void *h, int32_t h_dtype, int64_t h_stride, const void *y, int32_t y_dtype,
+                      int64_t y_stride, void *h_out, int64_t out_stride, const float *gain, double eps, int32_t m,
+                      int32_t k, void *codes, void *powers, void *hip_stream);
+
+/* Weights [n][k], row-major of SPARK_DTYPE_*, as 8-bit rows in the order the matrix instructions take
+ * them, written once to `packed` (16-byte aligned, at least the size that spark_scaled_weight_bytes
+ * writes to *bytes [host]).  With `up` (of the same shape, type and stride; else NULL) a pair of matrices
+ * for spark_scaled_gated: w is the gate. */
+int spark_scaled_weight_bytes(int32_t n, int32_t k, int32_t pair, size_t *bytes);
+int spark_scaled_pack(const void *w, const void *up, int32_t dtype, int64_t stride, int32_t n, int32_t k,
+                      void *packed, size_t packed_bytes, void *hip_stream);
+
+/* Bytes of workspace [host] that the two products below need for these sizes on the current device, at
+ * most (pair: as above).  0 for few rows.  The workspace is theirs until the call's work is done:
+ * calls that may run at the same time (two streams, two captured graphs that are replayed side by side)
+ * need one each.  16-byte aligned, contents of no account; NULL where none is needed. */
+int spark_scaled_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t pair, size_t *bytes);
+
+/* out [m][n] of out_dtype = X W^T, X the 8-bit rows [m][k], W packed without a second matrix.  Sums in
+ * fp32, each output rounded once to its type; the same inputs give the same bits at every call. */
+int spark_scaled_matmul(const void *codes, const void *powers, int32_t m, const void *packed, int32_t n, int32_t k,
+                        void *out, int32_t out_dtype, int64_t out_stride, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/* The 8-bit rows [m][n] of silu(X Wg^T) * (X Wu^T), silu(g) = g / (1 + exp(-g)): sums, exponential and
+ * product in fp32, then to 8 bits.  packed: a pair. */
+int spark_scaled_gated(const void *codes, const void *powers, int32_t m, const void *packed, int32_t n, int32_t k,
+                       void *out_codes, void *out_powers, void *workspace, size_t workspace_bytes,
+                       void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

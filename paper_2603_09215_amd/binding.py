@@ -25,7 +25,9 @@ EXPORTS = ("spark_workspace_bytes", "spark_init", "spark_seq_open", "spark_prefi
            "spark_get_stats", "spark_seq_close", "spark_destroy", "spark_last_error",
            "spark_profile_select", "spark_profile_read", "spark_set_sampling", "spark_decode_sampled",
            "spark_seq_text_budget", "spark_schedule_preview", "spark_seq_set_phase", "spark_align_phases",
-           "spark_init_static", "spark_tune", "spark_measure_read")
+           "spark_init_static", "spark_tune", "spark_measure_read", "spark_scaled_rows", "spark_scaled_norm",
+           "spark_scaled_weight_bytes", "spark_scaled_pack", "spark_scaled_workspace_bytes", "spark_scaled_matmul",
+           "spark_scaled_gated")
 
 
 class SparkConfig(C.Structure):
@@ -100,6 +102,14 @@ def load_library() -> C.CDLL:
     lib.spark_last_error.restype = C.c_char_p
     lib.spark_profile_select.argtypes = [P, I]
     lib.spark_profile_read.argtypes = [P, C.POINTER(C.c_int64), C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    L, D, Z = C.c_int64, C.c_double, C.c_size_t
+    lib.spark_scaled_rows.argtypes = [P, I, L, I, I, P, P, P]
+    lib.spark_scaled_norm.argtypes = [P, I, L, P, I, L, P, L, P, D, I, I, P, P, P]
+    lib.spark_scaled_weight_bytes.argtypes = [I, I, I, C.POINTER(Z)]
+    lib.spark_scaled_pack.argtypes = [P, P, I, L, I, I, P, Z, P]
+    lib.spark_scaled_workspace_bytes.argtypes = [I, I, I, I, C.POINTER(Z)]
+    lib.spark_scaled_matmul.argtypes = [P, P, I, P, I, I, P, I, L, P, Z, P]
+    lib.spark_scaled_gated.argtypes = [P, P, I, P, I, I, P, P, P, Z, P]
     _lib = lib
     return lib
 

@@ -343,7 +343,7 @@ int spark_tune(spark_ctx *ctx, const char *name, int32_t value);
  * In all of them: pointers are [device] unless marked, of the current device, on which hip_stream
  * (NULL: its default stream) has to be as well; nothing is allocated, copied or waited for, so the calls
  * may be captured into a graph; strides count elements from row to row and are at least the row's
- * length; m == 0 is a call that does nothing; n and k are 1 .. 2^24.  Outputs must not overlap inputs
+ * length; m == 0 is a call that does nothing; n and k are 1 .. 2^22.  Outputs must not overlap inputs
  * except where it says so.  SPARK_EINVAL: a NULL pointer, a size, stride, type or alignment outside
  * these limits (nothing is launched); SPARK_ENOMEM: packed or workspace too small; SPARK_EHIP: the
  * launch failed. */

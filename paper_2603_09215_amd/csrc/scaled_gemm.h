@@ -6,13 +6,17 @@
 // lost; across eights nothing is), at most 2^-10 of their magnitudes and 1.4e-5 of the result for normal data.  Outputs
 // of 16 and 8 bits, rounded at 2^-8 and 2^-4, take it.
 //
-// v_mfma_f32_16x16x32_f16, at half the rate, on the codes as fp16, which holds every one of them: four of them are a
-// block of 128, whose sum is multiplied by both powers and added in fp32.  Outputs in fp32 take it: 1e-7 of the result.
+// v_mfma_f32_16x16x32_f16, at half the rate, on the codes as fp16, the weights' times their power relative to their row's
+// largest: fp16 holds that exactly down to 2^-15 of that power and to 2^-25 of it (2^-34 of the row's largest weight)
+// below.  Four of them are a block of 128, whose sum is multiplied by the activations' power and added in fp32; the weights'
+// largest power multiplies the whole.  Outputs in fp32 and pairs take it: 1e-7 of the result.
 //
 // Operand lane l holds 32 codes of row l mod 16; which 32 of the 128 does not matter as long as both operands agree, so
 // the lanes hold what loads well (scaled_rows.h, packed weights).  Of the result, lane l holds weight rows
 // 4 (l / 16) .. + 3 of activation row l mod 16: four neighbouring outputs of one row.
 #pragma once
+#include <type_traits>
+
 #include "scaled_rows.h"
 
 namespace spark {
@@ -23,68 +27,57 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct GemmArgs {
   const uint8_t *codes, *powers;          // of the rows
-  const uint8_t *weights, *weight_powers;
+  const uint8_t *weights, *weight_powers, *weight_tops;
   int m, n, k;
+  int row_blocks;                         // of the weights
   void *out;                              // [m][n], or the codes of 8-bit rows
   uint8_t *out_powers;
   long long out_stride;
 };
 
-__device__ __forceinline__ i32x8 load_operand(const uint8_t *p, int apart) {   // 16 codes at p, 16 at p + apart
-  const i32x4 a = *(const i32x4 *)p, b = *(const i32x4 *)(p + apart);
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+// A number that is the same for the whole wave, into a scalar register: quotients are worked out in vector registers, and a
+// buffer descriptor made of one is otherwise sorted out lane by lane, load by load.
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// where part i of n of the groups begins (groups: 8192 at most, parts: 8192)
+__device__ __forceinline__ int part_begin(int groups, int i, int n) { return scalar((unsigned)groups * i / n); }
+
+// Loads by buffer descriptor: what lies behind its end reads as zero and asks memory for nothing.
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+__device__ __forceinline__ buffer_t buffer_of(const void *p, unsigned bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00027000);
 }
-__device__ __forceinline__ i32x8 stream_operand(const uint8_t *p, int apart) {   // the same, read once on this chip
-  const i32x4 a = __builtin_nontemporal_load((const i32x4 *)p), b = __builtin_nontemporal_load((const i32x4 *)(p + apart));
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+constexpr int ONCE = 2;   // read once on this chip
+// (all of an offset in the lane's part, which the check against the end covers for certain)
+template <int HINT> __device__ __forceinline__ i32x8 buffer_operand(const buffer_t &b, unsigned at, int apart) {
+  const i32x4 u = __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, HINT), v = __builtin_amdgcn_raw_buffer_load_b128(b, (int)(at + apart), 0, HINT);
+  return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
 }
+__device__ __forceinline__ uint32_t buffer_word(const buffer_t &b, unsigned at) { return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(b, (int)at, 0, 0); }
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// An operand as the instruction wants it, and its powers of a group of four blocks: bytes of one row, or (weights, FP32)
-// of the four rows whose sums the lane holds.
-template <bool FP32> struct Operand;
-template <> struct Operand<false> {
-  i32x8 v;
-  __device__ __forceinline__ void set(const i32x8 &c) { v = c; }
-};
-template <> struct Operand<true> {
-  f16x8 v[4];
-  __device__ __forceinline__ void set(const i32x8 &c) {
+__device__ __forceinline__ void scaled_f16(const i32x8 &c, float s, f16x8 (&v)[4]) {   // 32 codes times s
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q], 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q], 1.0f, true);
-      const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q + 1], 1.0f, false), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q + 1], 1.0f, true);
-      v[q] = f16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
-    }
+  for (int q = 0; q < 4; ++q) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q], s, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q], s, true);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q + 1], s, false), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * q + 1], s, true);
+    v[q] = f16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
   }
-};
-template <bool FP32> struct WeightPowers;
-template <> struct WeightPowers<false> {
-  uint32_t p;
-  __device__ __forceinline__ void load(const uint8_t *group) { p = ((const uint32_t *)group)[threadIdx.x & 15]; }   // 16 rows x 4 bytes
-};
-template <> struct WeightPowers<true> {
-  uint4 p;
-  __device__ __forceinline__ void load(const uint8_t *group) { p = ((const uint4 *)group)[threadIdx.x >> 4 & 3]; }
-};
-__device__ __forceinline__ float power_of(uint32_t bytes, int j) { return __uint_as_float((bytes >> (8 * j) & 255u) << 23); }
-
-// acc += the products of block j of a group; xp: the activation row's four bytes
-__device__ __forceinline__ void add_block(f32x4 &acc, const Operand<false> &w, const Operand<false> &x, const WeightPowers<false> &wp, uint32_t xp, int j) {
-  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, acc, 0, 0, 0, (int)(wp.p >> (8 * j)), 0, (int)(xp >> (8 * j)));
 }
-__device__ __forceinline__ void add_block(f32x4 &acc, const Operand<true> &w, const Operand<true> &x, const WeightPowers<true> &wp, uint32_t xp, int j) {
-  f32x4 t = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ uint32_t byte_of(uint32_t bytes, int j) { return bytes >> (8 * j) & 255u; }
+// 2^(byte - top), byte <= top; far down: 0
+__device__ __forceinline__ float power_below(uint32_t byte, uint32_t top) { return __uint_as_float((uint32_t)max((int)byte - (int)top + 127, 0) << 23); }
+// The activations' power times 2^-ROOM: the sums are without the weights' largest power until the end, and rows of numbers
+// up to 1e37 are to stay in fp32's range (as are rows of 1e-30).
+constexpr int ROOM = 20;
+__device__ __forceinline__ float power_with_room(uint32_t byte) { return __uint_as_float((uint32_t)max((int)byte - ROOM, 0) << 23); }
+// what the sums are multiplied by at the end: 2^(top - 127 + ROOM), in two steps, the second 2^ROOM
+__device__ __forceinline__ f32x4 with_tops(const f32x4 &v, uint32_t tops) {
+  f32x4 r;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) t = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[q], x.v[q], t, 0, 0, 0);
-  // (one power after the other: their product may leave fp32's range where the term does not)
-  const float xs = power_of(xp, j);
-  acc[0] = fmaf(t[0] * power_of(wp.p.x, j), xs, acc[0]);
-  acc[1] = fmaf(t[1] * power_of(wp.p.y, j), xs, acc[1]);
-  acc[2] = fmaf(t[2] * power_of(wp.p.z, j), xs, acc[2]);
-  acc[3] = fmaf(t[3] * power_of(wp.p.w, j), xs, acc[3]);
+  for (int i = 0; i < 4; ++i) r[i] = v[i] * __uint_as_float(byte_of(tops, i) << 23) * (float)(1 << ROOM);
+  return r;
 }
 
 // four neighbouring outputs of a row
@@ -109,104 +102,370 @@ __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f
 
 // ------------------------------------------------------------------ few rows: the weights stream through registers
 
-// The sums of one wave: row block nb, k blocks of the groups of four g0, g0 + dg, ..; 16 MT activation rows from r0 on.
-template <int MT, bool FP32>
-__device__ __forceinline__ void stream_sums(const GemmArgs &a, long long nb, int g0, int dg, int r0, f32x4 (&acc)[MT]) {
-  const int lane = threadIdx.x & 63, col = lane & 15, part = lane >> 4;
-  const int blocks = sr_blocks(a.k), pitch = sr_pitch(a.k), groups = pitch / 4;
-  const long long kp = (long long)blocks * SR_BLOCK;
-  const uint8_t *w = a.weights + nb * blocks * SW_TILE + lane * 16;
-  const uint8_t *wp = a.weight_powers + nb * groups * 64;
-  const uint8_t *x[MT];
-  const uint32_t *xp[MT];
-  bool have[MT];
+// What bounds these two: the weights' way from memory.  A wave holds RING groups of four k blocks (8 KiB each) of a row block
+// in registers and asks for a group's successor block by block as it uses it, so that about that much is always on its way.
+// All of these loads are unconditional (a load that may be skipped makes the next wait one for everything); behind the
+// range they read zeros from nowhere, and zeros add nothing.
+
+// The weights' side of a wave: row block nb, groups [g0, g1) of four k blocks
+template <bool FP32> struct WeightStream {
+  buffer_t codes, powers;
+  unsigned end, powers_end;
+  uint32_t top;   // (of the lane's row)
+  i32x8 c[4];
+  uint32_t p;
+  __device__ __forceinline__ WeightStream(const GemmArgs &a, int nb, int g0, int g1) {
+    const int blocks = sr_blocks(a.k), groups = sr_pitch(a.k) / 4;
+    end = (unsigned)min(g1 * 4, blocks) * SW_TILE;
+    powers_end = g1;
+    codes = buffer_of(a.weights + (long long)nb * blocks * SW_TILE, end);
+    powers = buffer_of(a.weight_powers + (long long)nb * groups * 64, powers_end * 64);
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int r = r0 + t * 16 + col;
-    have[t] = r < a.m;
-    x[t] = a.codes + (have[t] ? r : 0) * kp + part * 16;
-    xp[t] = (const uint32_t *)(a.powers + (long long)(have[t] ? r : 0) * pitch);
-    acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 4; ++j) ask(g0, j);
+    ask_powers(g0);
+    if (FP32) top = a.weight_tops[(long long)nb * 16 + (threadIdx.x & 15)];
   }
-  for (int g = g0; g < groups; g += dg) {
-    WeightPowers<FP32> wpow;
-    wpow.load(wp + g * 64);
-    uint32_t xpow[MT];
+  __device__ __forceinline__ void ask(int g, int j) {
+    c[j] = buffer_operand<ONCE>(codes, (threadIdx.x & 63) * 16 + min((unsigned)(g * 4 + j) * SW_TILE, end), 1024);
+  }
+  __device__ __forceinline__ void ask_powers(int g) { p = buffer_word(powers, (threadIdx.x & 15) * 4 + min((unsigned)g, powers_end) * 64); }
+};
+
+// acc += a block's products; wp, xp: the rows' bytes of its group, j its number in it
+template <bool FP32> __device__ __forceinline__ void add_block(f32x4 &acc, const i32x8 &w, const f16x8 (&wf)[4], const i32x8 &x, uint32_t wp, uint32_t xp, int j) {
+  if constexpr (FP32) {
+    f16x8 xf[4];
+    scaled_f16(x, 1.0f, xf);
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xpow[t] = have[t] ? xp[t][g] : 0u;
+    for (int q = 0; q < 4; ++q) t = __builtin_amdgcn_mfma_f32_16x16x32_f16(wf[q], xf[q], t, 0, 0, 0);
+    const float power = power_with_room(byte_of(xp, j));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = fmaf(t[i], power, acc[i]);
+  } else {
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, 0, (int)(wp >> (8 * j)), 0, (int)(xp >> (8 * j)));
+  }
+}
+
+// out = X W^T, up to 16 rows.  A workgroup has nw row blocks, kw waves each, which share k; their sums meet in LDS, added in
+// order.  IN_LDS: the rows' codes lie in LDS, fetched once for all waves, rows 16 bytes apart beyond their length so that
+// sixteen of them read side by side meet in no bank; otherwise (long rows) each wave reads its part of them itself, a byte
+// beside every byte of the weights.
+template <bool IN_LDS, typename OUT>
+__global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int kw) {
+  constexpr bool FP32 = sizeof(OUT) == 4;
+  extern __shared__ i32x4 lds[];   // [m][kp + 16 bytes], [m][pitch / 4 words]; then the sums [wave][64]
+  const int wave = scalar(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15;
+  const int first = blockIdx.x * nw, mine = scalar(wave / kw), part = wave - mine * kw;
+  const int blocks = sr_blocks(a.k), pitch = sr_pitch(a.k), groups = pitch / 4, kp = blocks * SR_BLOCK;
+  const int g0 = part_begin(groups, part, kw), g1 = part_begin(groups, part + 1, kw);   // (kw <= groups)
+  WeightStream<FP32> ws(a, min(first + mine, a.row_blocks - 1), g0, g1);
+  const int row = min(col, a.m - 1);   // (columns behind the last row repeat it, and are not stored)
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  i32x8 c[4];
+  uint32_t p = 0u;
+  const buffer_t xb = buffer_of(a.codes, (unsigned)a.m * kp), xpb = buffer_of(a.powers, (unsigned)a.m * pitch);
+  const i32x4 *xl = lds + row * (kp / 16 + 1) + (lane >> 4);
+  const uint32_t *xpl = (const uint32_t *)(lds + a.m * (kp / 16 + 1)) + row * groups;
+  auto ask = [&](int g, int j) { c[j] = buffer_operand<0>(xb, (unsigned)row * kp + (lane >> 4) * 16 + min(g * 4 + j, blocks - 1) * SR_BLOCK, 64); };
+  auto ask_power = [&](int g) { p = buffer_word(xpb, (unsigned)row * pitch + g * 4); };
+  if constexpr (IN_LDS) {
+    const int wide = kp / 16;
+    for (int r = 0; r < a.m; ++r) {
+      for (int i = threadIdx.x; i < wide; i += blockDim.x) lds[r * (wide + 1) + i] = ((const i32x4 *)a.codes)[r * wide + i];
+      for (int i = threadIdx.x; i < groups; i += blockDim.x) ((uint32_t *)(lds + a.m * (wide + 1)))[r * groups + i] = ((const uint32_t *)a.powers)[r * groups + i];
+    }
+    __syncthreads();
+  } else {
+    ask_power(g0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ask(g0, j);
+  }
+  auto turn = [&](int g, auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    const uint32_t wp = ws.p, xp = IN_LDS ? xpl[g] : p;
+    if constexpr (MORE) {
+      ws.ask_powers(g + 1);
+      if constexpr (!IN_LDS) ask_power(g + 1);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int kb = min(g * 4 + j, blocks - 1);   // (behind the last block: the last, times zeros)
+      i32x8 x;
+      if constexpr (IN_LDS) x = __builtin_shufflevector(xl[kb * 8], xl[kb * 8 + 4], 0, 1, 2, 3, 4, 5, 6, 7);
+      else x = c[j];
+      f16x8 wf[4];
+      if constexpr (FP32) scaled_f16(ws.c[j], power_below(byte_of(wp, j), ws.top), wf);
+      add_block<FP32>(acc, ws.c[j], wf, x, wp, xp, j);
+      if constexpr (MORE) {
+        ws.ask(g + 1, j);
+        if constexpr (!IN_LDS) ask(g + 1, j);
+      }
+    }
+  };
+  for (int g = g0; g + 1 < g1; ++g) turn(g, std::true_type());
+  turn(g1 - 1, std::false_type());
+  f32x4 *sums = (f32x4 *)lds;
+  if constexpr (IN_LDS) __syncthreads();
+  sums[wave * 64 + lane] = acc;
+  __syncthreads();
+  const bool vec = a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(OUT) - 1)) == 0;
+  for (int i = threadIdx.x; i < nw * 64; i += blockDim.x) {
+    const int l = i & 63, b = i >> 6, r = l & 15;
+    if (r >= a.m || first + b >= a.row_blocks) continue;
+    f32x4 v = sums[b * kw * 64 + l];
+    for (int w = 1; w < kw; ++w) v += sums[(b * kw + w) * 64 + l];
+    if constexpr (FP32) v = with_tops(v, ((const uint32_t *)a.weight_tops)[(long long)(first + b) * 4 + (l >> 4)]);
+    store_four((OUT *)a.out + r * a.out_stride, (first + b) * 16 + (l >> 4) * 4, a.n, vec, v);
+  }
+}
+// ------------------------------------------------------------------ tiles
+
+__device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Where a workgroup's tile lies: workgroups come to the eight XCDs in turn, and each XCD has a run of the tiles, those of
+// one part of the weights next to each other, so that its L2 has that part once.
+struct TilePlace { int n, m, split; };
+__device__ __forceinline__ TilePlace tile_place(int n_tiles, int m_tiles) {
+  const int total = gridDim.x, xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
+  const int id = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
+  const int q = scalar(id / m_tiles), split = scalar(q / n_tiles);
+  return TilePlace{q - split * n_tiles, id - q * m_tiles, split};
+}
+
+// What a tile's sums become: outputs of the type OUT, the 8-bit rows of a pair (`gated`), or, where k is cut (`parts`), fp32
+// sums for a finishing launch, [split][row][16 row blocks].
+enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
+
+// WN x WM waves, of NT x MT operands of 16 each.  The weights go from memory into registers, RB k blocks ahead; the rows'
+// codes, which the WN waves share, through LDS in operand order, two buffers, a barrier per k block.
+template <int NT, int MT, int WN, int WM, int RB, bool FP32, TileEnd END, typename OUT>
+__global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
+  constexpr int WAVES = WN * WM, TM = MT * WM, UNITS = 2 * TM, UN = (UNITS + WAVES - 1) / WAVES;   // units of the rows: 1 KiB
+  constexpr int WORDS = 64 * WAVES;   // a thread has a word of the powers of either operand, wanted or not: a branch in the loop lets the compiler gather the products of several blocks behind it
+  static_assert(END != TILE_GATED || (NT % 2 == 0 && NT * WN == 16), "a block of 128 outputs of both matrices");
+  static_assert(4 % RB == 0, "");
+  extern __shared__ i32x4 lds[];   // [2][TM][half][64] codes, [2][2][WORDS] words of powers; gated: then [16 TM][OUT_PITCH] floats
+  constexpr int OUT_PITCH = SR_BLOCK + 4, XROWS = 16 * TM, WROWS = 16 * NT * WN;
+  uint32_t *words = (uint32_t *)(lds + 2 * UNITS * 64);
+  const int wave = scalar(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, part = lane >> 4;
+  const int wn = wave % WN, wm = wave / WN;
+  const TilePlace at = tile_place(n_tiles, m_tiles);
+  const int blocks = sr_blocks(a.k), pitch = sr_pitch(a.k), groups = pitch / 4, kp = blocks * SR_BLOCK;
+  const int g0 = part_begin(groups, at.split, splits), g1 = part_begin(groups, at.split + 1, splits);
+  const int kb0 = g0 * 4, kb1 = min(g1 * 4, blocks);
+  const int r0 = at.m * XROWS, rows = min(a.m - r0, XROWS);
+  const unsigned x_end = (unsigned)rows * kp, xp_end = (unsigned)rows * pitch;
+  const buffer_t xb = buffer_of(a.codes + (long long)r0 * kp, x_end), xpb = buffer_of(a.powers + (long long)r0 * pitch, xp_end);
+  // NT row blocks one after the other; those behind the last read as zeros
+  const int tile_nb = at.n * WN * NT, nb = tile_nb + wn * NT, have = max(0, min(NT, a.row_blocks - nb));
+  const unsigned w_end = (unsigned)have * blocks * SW_TILE;
+  const buffer_t wb = buffer_of(a.weights + (long long)(have ? nb : 0) * blocks * SW_TILE, w_end);
+  const unsigned wp_end = (unsigned)min(WN * NT, a.row_blocks - tile_nb) * groups * 64;
+  const buffer_t wpb = buffer_of(a.weight_powers + (long long)tile_nb * groups * 64, wp_end);
+
+  i32x4 xs[UN];
+  i32x8 w[RB][NT];
+  uint32_t xp_next, wp_next;
+  auto ask_x = [&](int kb) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int unit = (u * WAVES + wave) % UNITS;   // (fewer units than waves: some fetch the same)
+      xs[u] = __builtin_amdgcn_raw_buffer_load_b128(xb, (int)((unsigned)((unit >> 1) * 16 + col) * kp + (unit & 1) * 64 + part * 16 +
+                                                                (kb < kb1 ? (unsigned)kb * SR_BLOCK : x_end)), 0, 0);
+    }
+  };
+  auto put_x = [&](int buffer) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int unit = (u * WAVES + wave) % UNITS;
+      lds[(buffer * UNITS + unit) * 64 + lane] = xs[u];
+    }
+  };
+  auto ask_w = [&](int kb, int nt, i32x8 &to) {
+    to = buffer_operand<WM == 1 ? ONCE : 0>(wb, lane * 16 + (kb < kb1 ? (unsigned)(nt * blocks + kb) * SW_TILE : w_end), 1024);
+  };
+  const unsigned xp_at = threadIdx.x < XROWS ? threadIdx.x * pitch : xp_end, wp_at = threadIdx.x < WROWS ? ((threadIdx.x >> 4) * groups * 16 + (threadIdx.x & 15)) * 4 : wp_end;
+  auto ask_powers = [&](int g) {   // a row's word of the group
+    xp_next = buffer_word(xpb, xp_at + (g < g1 ? (unsigned)g * 4 : xp_end));
+    wp_next = buffer_word(wpb, wp_at + (g < g1 ? (unsigned)g * 64 : wp_end));
+  };
+  auto put_powers = [&](int buffer) {
+    words[buffer * 2 * WORDS + threadIdx.x] = xp_next;
+    words[buffer * 2 * WORDS + WORDS + threadIdx.x] = wp_next;
+  };
+  static_assert(XROWS <= 64 * WAVES && WROWS <= 64 * WAVES, "a thread has a row's word");
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t tops[FP32 ? NT : 1];   // of the operand's row
+  if constexpr (FP32) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) tops[nt] = a.weight_tops[(long long)min(nb + nt, a.row_blocks - 1) * 16 + col];
+  }
+  ask_powers(g0);
+  ask_x(kb0);
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) ask_w(kb0 + b, nt, w[b][nt]);
+  put_powers(g0 & 1);
+  put_x(0);
+  ask_x(kb0 + 1);
+  for (int g = g0; g < g1; ++g) {
+    const uint32_t *xw = words + (g & 1) * 2 * WORDS + wm * MT * 16 + col, *ww = words + (g & 1) * 2 * WORDS + WORDS + wn * NT * 16 + col;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int kb = g * 4 + j;
-      if (kb < blocks) {   // (the same for all lanes)
-        Operand<FP32> wo, xo;
-        wo.set(stream_operand(w + (long long)kb * SW_TILE, 1024));
+      __builtin_amdgcn_sched_barrier(0);   // (blocks worked on side by side take more registers than there are)
+      tile_barrier();
+      put_x((j + 1) & 1);
+      ask_x(kb + 2);
+      if (j == 1) ask_powers(g + 1);
+      if (j == 3) put_powers((g + 1) & 1);
+      const i32x4 *xl = lds + ((j & 1) * UNITS + wm * MT * 2) * 64 + lane;
+      if constexpr (FP32) {
+        f16x8 wf[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          scaled_f16(w[j % RB][nt], power_below(byte_of(ww[nt * 16], j), tops[nt]), wf[nt]);
+          ask_w(kb + RB, nt, w[j % RB][nt]);
+        }
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          i32x8 c = {0, 0, 0, 0, 0, 0, 0, 0};
-          if (have[t]) c = load_operand(x[t] + (long long)kb * SR_BLOCK, 64);
-          xo.set(c);
-          add_block(acc[t], wo, xo, wpow, xpow[t], j);
+          f16x8 xf[4];
+          f32x4 sum[NT];
+          const float power = power_with_room(byte_of(xw[t * 16], j));
+          scaled_f16(__builtin_shufflevector(xl[t * 128], xl[t * 128 + 64], 0, 1, 2, 3, 4, 5, 6, 7), 1.0f, xf);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) sum[nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wf[nt][0], xf[0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int q = 1; q < 4; ++q)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sum[nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wf[nt][q], xf[q], sum[nt], 0, 0, 0);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[nt][t][i] = fmaf(sum[nt][i], power, acc[nt][t][i]);
         }
+      } else {
+        uint32_t wp[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) wp[nt] = ww[nt * 16] >> (8 * j);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const i32x8 x = __builtin_shufflevector(xl[t * 128], xl[t * 128 + 64], 0, 1, 2, 3, 4, 5, 6, 7);
+          const uint32_t xp = xw[t * 16] >> (8 * j);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            acc[nt][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j % RB][nt], x, acc[nt][t], 0, 0, 0, (int)wp[nt], 0, (int)xp);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) ask_w(kb + RB, nt, w[j % RB][nt]);
+      }
+    }
+  }
+  if constexpr (FP32) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint32_t four = ((const uint32_t *)a.weight_tops)[(long long)min(nb + nt, a.row_blocks - 1) * 4 + part];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[nt][t] = with_tops(acc[nt][t], four);
+    }
+  }
+  if constexpr (END == TILE_GATED) {
+    float *outs = (float *)lds;
+    tile_barrier();
+#pragma unroll
+    for (int nt = 0; nt < NT; nt += 2)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = silu_times(acc[nt][t][i], acc[nt + 1][t][i]);
+        *(f32x4 *)(outs + ((wm * MT + t) * 16 + col) * OUT_PITCH + (wn * NT / 2 + nt / 2) * 16 + part * 4) = v;
+      }
+    tile_barrier();
+    const int sub = threadIdx.x & 15, o = at.n * SR_BLOCK + sub * 8, nblocks = sr_blocks(a.n), npitch = sr_pitch(a.n);
+    for (int row = threadIdx.x >> 4; row < 16 * TM; row += 4 * WAVES) {
+      if (row >= rows) break;   // (the same for a row's sixteen lanes)
+      const long long r = r0 + row;
+      const f32x4 p = *(const f32x4 *)(outs + row * OUT_PITCH + sub * 8), q = *(const f32x4 *)(outs + row * OUT_PITCH + sub * 8 + 4);
+      float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (o + i >= a.n) v[i] = 0.f;
+      uint32_t byte;
+      const uint2 c = block_codes(v, byte);
+      *(uint2 *)((uint8_t *)a.out + (r * nblocks + at.n) * SR_BLOCK + sub * 8) = c;
+      uint8_t *powers = a.out_powers + r * npitch;
+      if (sub == 0) powers[at.n] = (uint8_t)byte;
+      if (at.n == nblocks - 1 && nblocks + sub < npitch) powers[nblocks + sub] = 127;
+    }
+  } else {
+    const bool vec = END == TILE_PARTS || (a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(OUT) - 1)) == 0);
+    const int n = END == TILE_PARTS ? a.row_blocks * 16 : a.n;
+    OUT *out = (OUT *)a.out + (END == TILE_PARTS ? (long long)at.split * a.m * a.out_stride : 0);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int row = (wm * MT + t) * 16 + col;
+      if (row < rows) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          if (nt < have) store_four(out + (r0 + row) * a.out_stride, (int)(nb + nt) * 16 + part * 4, n, vec, acc[nt][t]);
       }
     }
   }
 }
 
-// out = X W^T.  A workgroup has nw row blocks, kw waves each, which share k; their sums meet in LDS, added in order.
-template <int MT, typename OUT>
-__global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int kw) {
-  extern __shared__ f32x4 sums[];   // [wave][MT][64]
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long n_blocks = sw_row_blocks(a.n, 0), first = (long long)blockIdx.x * nw;
-  const int r0 = blockIdx.y * 16 * MT;
-  const long long nb = min(first + wave / kw, n_blocks - 1);
-  f32x4 acc[MT];
-  stream_sums<MT, sizeof(OUT) == 4>(a, nb, wave % kw, kw, r0, acc);
-#pragma unroll
-  for (int t = 0; t < MT; ++t) sums[(wave * MT + t) * 64 + lane] = acc[t];
-  __syncthreads();
-  const bool vec = a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(OUT) - 1)) == 0;
-  for (int i = threadIdx.x; i < nw * MT * 64; i += blockDim.x) {
-    const int l = i & 63, t = (i >> 6) % MT, b = (i >> 6) / MT;
-    const int r = r0 + t * 16 + (l & 15);
-    if (r >= a.m || first + b >= n_blocks) continue;
-    f32x4 v = sums[(b * kw * MT + t) * 64 + l];
-    for (int w = 1; w < kw; ++w) v += sums[((b * kw + w) * MT + t) * 64 + l];
-    store_four((OUT *)a.out + r * a.out_stride, (int)(first + b) * 16 + (l >> 4) * 4, a.n, vec, v);
+// The parts of a cut k, added in order.  parts [split][m][pitch]; four outputs a thread
+template <typename OUT>
+__global__ void __launch_bounds__(256) scaled_join_k(const float *__restrict__ parts, int splits, int m, int n, int pitch, OUT *__restrict__ out,
+                                                     long long out_stride) {
+  const int fours = (n + 3) / 4;
+  const bool vec = out_stride % 4 == 0 && ((uintptr_t)out & (4 * sizeof(OUT) - 1)) == 0;
+  const long long total = (long long)m * fours, apart = (long long)m * pitch;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long r = i / fours;
+    const int o = (int)(i - r * fours) * 4;
+    const float *p = parts + r * pitch + o;
+    f32x4 v = *(const f32x4 *)p;
+    for (int s = 1; s < splits; ++s) v += *(const f32x4 *)(p + s * apart);
+    store_four(out + r * out_stride, o, n, vec, v);
   }
 }
-
-// silu(X Wg^T) * (X Wu^T) as 8-bit rows.  A workgroup has one block of 128 outputs: 16 waves, one row block each (eight of
-// the gate, eight of the other matrix, in turn), all of k.
-template <int MT>
-__global__ void __launch_bounds__(1024) scaled_gated_stream_k(GemmArgs a) {
-  __shared__ f32x4 sums[16 * MT * 64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r0 = blockIdx.y * 16 * MT;
-  const long long nb = min((long long)blockIdx.x * 16 + wave, sw_row_blocks(a.n, 1) - 1);
-  f32x4 acc[MT];
-  stream_sums<MT, false>(a, nb, 0, 1, r0, acc);
+// ... of a pair: sixteen lanes a block of 128 outputs of a row
+__global__ void __launch_bounds__(256) scaled_join_gated_k(const float *__restrict__ parts, int splits, int m, int n, int pitch, uint8_t *__restrict__ codes,
+                                                           uint8_t *__restrict__ powers) {
+  const int blocks = sr_blocks(n), npitch = sr_pitch(n), sub = threadIdx.x & 15;
+  const long long total = (long long)m * npitch, apart = (long long)m * pitch;
+  for (long long b = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4; b < total; b += (long long)gridDim.x * 16) {
+    const long long r = b / npitch;
+    const int block = (int)(b - r * npitch), o = block * SR_BLOCK + sub * 8;
+    if (block >= blocks) {
+      if (sub == 0) powers[r * npitch + block] = 127;
+      continue;
+    }
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (o < n) {   // outputs o .. + 7 are half a row block of either matrix
+      const float *p = parts + r * pitch + (o >> 4) * 32 + (o & 15);
+      f32x4 g[2] = {*(const f32x4 *)p, *(const f32x4 *)(p + 4)}, u[2] = {*(const f32x4 *)(p + 16), *(const f32x4 *)(p + 20)};
+      for (int s = 1; s < splits; ++s) {
+        const float *q = p + s * apart;
+        g[0] += *(const f32x4 *)q; g[1] += *(const f32x4 *)(q + 4);
+        u[0] += *(const f32x4 *)(q + 16); u[1] += *(const f32x4 *)(q + 20);
+      }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) sums[(wave * MT + t) * 64 + lane] = acc[t];
-  __syncthreads();
-  const int row = threadIdx.x >> 4, sub = threadIdx.x & 15, r = r0 + row;
-  if (row >= 16 * MT || r >= a.m) return;
-  // outputs 8 sub .. + 7: rows 8 (sub mod 2) .. of row block sub / 2
-  const int at = ((sub >> 1) * 2 * MT + (row >> 4)) * 64 + (sub & 1) * 32 + (row & 15);
-  const int o = blockIdx.x * SR_BLOCK + sub * 8;
-  float v[8];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const f32x4 g = sums[at + q * 16], u = sums[at + MT * 64 + q * 16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[q * 4 + i] = o + q * 4 + i < a.n ? silu_times(g[i], u[i]) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (o + i < n) v[i] = silu_times(g[i >> 2][i & 3], u[i >> 2][i & 3]);
+    }
+    uint32_t byte;
+    const uint2 c = block_codes(v, byte);
+    *(uint2 *)(codes + (r * blocks + block) * SR_BLOCK + sub * 8) = c;
+    if (sub == 0) powers[r * npitch + block] = (uint8_t)byte;
   }
-  uint32_t byte;
-  const uint2 c = block_codes(v, byte);
-  const int blocks = sr_blocks(a.n), pitch = sr_pitch(a.n);
-  *(uint2 *)((uint8_t *)a.out + ((long long)r * blocks + blockIdx.x) * SR_BLOCK + sub * 8) = c;
-  uint8_t *powers = a.out_powers + (long long)r * pitch;
-  if (sub == 0) powers[blockIdx.x] = (uint8_t)byte;
-  if ((int)blockIdx.x == blocks - 1 && blocks + sub < pitch) powers[blocks + sub] = 127;
 }
 
 }  // namespace spark

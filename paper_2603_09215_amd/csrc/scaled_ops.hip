@@ -39,21 +39,63 @@ GemmArgs gemm_args(const ScaledProduct &p, int pair) {
   GemmArgs a{};
   a.codes = p.codes; a.powers = p.powers;
   a.weights = p.weights;
-  a.weight_powers = p.weights + sw_code_bytes(p.n, p.k, pair);
+  a.weight_powers = a.weights + sw_code_bytes(p.n, p.k, pair);
+  a.weight_tops = a.weight_powers + sw_power_bytes(p.n, p.k, pair);
   a.m = p.m; a.n = p.n; a.k = p.k;
+  a.row_blocks = (int)sw_row_blocks(p.n, pair);
   return a;
 }
 
-template <int MT, typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream) {
+constexpr int STREAM_ROWS = 16;
+constexpr size_t STREAM_LDS = 64 << 10;   // two workgroups a CU
+
+template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream) {
   const int groups = sr_pitch(a.k) / 4, turns = (groups + 15) / 16, kw = (groups + turns - 1) / turns, nw = std::max(1, 4 / kw);
-  const long long blocks = sw_row_blocks(a.n, 0);
-  const dim3 grid((unsigned)((blocks + nw - 1) / nw), (a.m + 16 * MT - 1) / (16 * MT));
-  scaled_stream_k<MT, OUT><<<grid, 64 * nw * kw, sizeof(f32x4) * 64 * MT * nw * kw, stream>>>(a, nw, kw);
+  const unsigned grid = (unsigned)((a.row_blocks + nw - 1) / nw);
+  const size_t rows = (size_t)a.m * (sr_blocks(a.k) * SR_BLOCK + 16 + sr_pitch(a.k)), sums = sizeof(f32x4) * 64 * nw * kw;
+  if (rows <= STREAM_LDS) scaled_stream_k<true, OUT><<<grid, 64 * nw * kw, std::max(rows, sums), stream>>>(a, nw, kw);
+  else scaled_stream_k<false, OUT><<<grid, 64 * nw * kw, sums, stream>>>(a, nw, kw);
 }
-template <typename OUT> void stream_any(const GemmArgs &a, hipStream_t stream) {
-  if (a.m <= 16) stream_launch<1, OUT>(a, stream);
-  else if (a.m <= 32) stream_launch<2, OUT>(a, stream);
-  else stream_launch<4, OUT>(a, stream);
+
+// Tiles: their size, and into how many parts k is cut.
+struct TilePlan { int shape, tn, tm, splits; };   // shape: the index below; 16 tn outputs (rows of packed weights), 16 tm rows
+size_t lds_of(int tm, bool gated) {
+  return std::max((size_t)2 * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
+}
+int tile_tm(int shape) { return 1 << shape; }
+TilePlan tile_plan(int m, int row_blocks, int k, int n_cu) {
+  TilePlan p;
+  p.shape = m <= 16 ? 0 : m <= 32 ? 1 : m <= 64 ? 2 : 3;
+  p.tn = 16;
+  p.tm = tile_tm(p.shape);
+  const long long tiles = (long long)((row_blocks + p.tn - 1) / p.tn) * ((m + 16 * p.tm - 1) / (16 * p.tm));
+  const int groups = sr_pitch(k) / 4;
+  p.splits = (int)std::max<long long>(1, std::min<long long>(groups / 2, n_cu / tiles));
+  return p;
+}
+
+template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, const TilePlan &p, hipStream_t stream) {
+  const int nt = (a.row_blocks + p.tn - 1) / p.tn, mt = (a.m + 16 * p.tm - 1) / (16 * p.tm);
+  const unsigned grid = (unsigned)nt * mt * p.splits;
+  const size_t lds = lds_of(p.tm, END == TILE_GATED);
+  if (p.shape == 0) scaled_tile_k<2, 1, 8, 1, 4, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
+  else if (p.shape == 1) scaled_tile_k<2, 2, 8, 1, 4, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
+  else if (p.shape == 2) scaled_tile_k<2, 4, 8, 1, 2, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
+  else scaled_tile_k<4, 4, 4, 2, 1, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
+}
+
+template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu, hipStream_t stream) {
+  if (a.m <= STREAM_ROWS) return stream_launch<OUT>(a, stream);
+  const TilePlan p = tile_plan(a.m, a.row_blocks, a.k, n_cu);
+  constexpr bool FP32 = sizeof(OUT) == 4;
+  if (p.splits == 1) return tile_launch<FP32, TILE_OUT, OUT>(a, p, stream);
+  GemmArgs b = a;
+  b.out = workspace;
+  b.out_stride = (long long)a.row_blocks * 16;
+  tile_launch<FP32, TILE_PARTS, float>(b, p, stream);
+  const long long fours = (long long)a.m * ((a.n + 3) / 4);
+  scaled_join_k<OUT><<<(unsigned)std::min<long long>((fours + 255) / 256, 1 << 16), 256, 0, stream>>>((const float *)workspace, p.splits, a.m, a.n,
+                                                                                                    a.row_blocks * 16, (OUT *)a.out, a.out_stride);
 }
 
 }  // namespace
@@ -111,28 +153,43 @@ hipError_t launch_scaled_pack(const void *w, int dtype, long long stride, int n,
       else scaled_pack_k<bf16_t, false><<<grid, 256, 0, stream>>>((const bf16_t *)w, stride, n, k, codes, powers, step, first, (int)r0);
     }
   }
+  const long long rows = groups * 16 * (pair ? 2 : 1);   // (of a pair: once more behind its second matrix)
+  scaled_tops_k<<<(unsigned)((rows + 255) / 256), 256, 0, stream>>>(powers, rows, sr_pitch(k) / 4, powers + sw_power_bytes(n, k, pair));
   return hipGetLastError();
 }
 
-size_t scaled_workspace_bytes(int, int, int, int, int) { return 0; }
+size_t scaled_workspace_bytes(int m, int n, int k, int pair, int n_cu) {
+  if (m == 0 || (m <= STREAM_ROWS && !pair)) return 0;
+  const int row_blocks = (int)sw_row_blocks(n, pair);
+  const TilePlan p = tile_plan(m, row_blocks, k, n_cu);
+  return p.splits == 1 ? 0 : sizeof(float) * p.splits * m * row_blocks * 16;
+}
 
-hipError_t launch_scaled_matmul(const ScaledProduct &p, void *out, int out_dtype, long long out_stride, void *, int, hipStream_t stream) {
+hipError_t launch_scaled_matmul(const ScaledProduct &p, void *out, int out_dtype, long long out_stride, void *workspace, int n_cu, hipStream_t stream) {
   GemmArgs a = gemm_args(p, 0);
   a.out = out;
   a.out_stride = out_stride;
-  if (out_dtype == SR_FP32) stream_any<float>(a, stream);
-  else stream_any<bf16_t>(a, stream);
+  if (out_dtype == SR_FP32) matmul_launch<float>(a, workspace, n_cu, stream);
+  else matmul_launch<bf16_t>(a, workspace, n_cu, stream);
   return hipGetLastError();
 }
 
-hipError_t launch_scaled_gated(const ScaledProduct &p, uint8_t *codes, uint8_t *powers, void *, int, hipStream_t stream) {
+hipError_t launch_scaled_gated(const ScaledProduct &p, uint8_t *codes, uint8_t *powers, void *workspace, int n_cu, hipStream_t stream) {
   GemmArgs a = gemm_args(p, 1);
   a.out = codes;
   a.out_powers = powers;
-  const unsigned blocks = sr_blocks(p.n);
-  if (p.m <= 16) scaled_gated_stream_k<1><<<dim3(blocks, 1), 1024, 0, stream>>>(a);
-  else if (p.m <= 32) scaled_gated_stream_k<2><<<dim3(blocks, 1), 1024, 0, stream>>>(a);
-  else scaled_gated_stream_k<4><<<dim3(blocks, (p.m + 63) / 64), 1024, 0, stream>>>(a);
+  const TilePlan plan = tile_plan(a.m, a.row_blocks, a.k, n_cu);
+  if (plan.splits == 1) {
+    tile_launch<true, TILE_GATED, float>(a, plan, stream);
+  } else {
+    GemmArgs b = a;
+    b.out = workspace;
+    b.out_stride = (long long)a.row_blocks * 16;
+    tile_launch<true, TILE_PARTS, float>(b, plan, stream);
+    const long long groups = (long long)a.m * sr_pitch(a.n);
+    scaled_join_gated_k<<<(unsigned)std::min<long long>((groups + 15) / 16, 1 << 16), 256, 0, stream>>>((const float *)workspace, plan.splits, a.m, a.n,
+                                                                                                      a.row_blocks * 16, codes, powers);
+  }
   return hipGetLastError();
 }
 
@@ -144,7 +201,7 @@ namespace {
 
 using namespace spark;
 
-constexpr int32_t MOST = 1 << 24;   // of n and k
+constexpr int32_t MOST = 1 << 22;   // of n and k: offsets inside a tile stay in 32 bits
 
 bool dtype_ok(int32_t d) { return d == SPARK_DTYPE_FP32 || d == SPARK_DTYPE_BF16; }
 bool aligned(const void *p, size_t a) { return p && ((uintptr_t)p & (a - 1)) == 0; }

@@ -232,15 +232,17 @@ __global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
 
 // Packed weights: tiles of 16 rows x 128 k as the matrix instructions take them, [row block][k block][half][lane][16 codes]:
 // lane l of half h holds row l mod 16, k = 64 h + 16 (l / 16) .. + 15, so that a wave reads a tile with two contiguous
-// instructions.  Behind them the powers, [row block][k block / 4][row][4].  Rows behind n are zeros.  A pair of matrices
-// (gated) alternates its row blocks: even ones of the gate, odd ones of the other.
+// instructions.  Behind them the powers, [row block][k block / 4][row][4], of blocks of zeros and behind the last the lowest,
+// and behind those each row's largest power, [row block][16].  Rows behind n are zeros.  A pair of matrices (gated)
+// alternates its row blocks: even ones of the gate, odd ones of the other.
 constexpr int SW_TILE = 2048;
 __host__ __device__ __forceinline__ long long sw_row_blocks(int n, int pair) { return (((long long)n + 15) / 16) * (pair ? 2 : 1); }
 __host__ __device__ __forceinline__ size_t sw_code_bytes(int n, int k, int pair) {
   return (size_t)sw_row_blocks(n, pair) * sr_blocks(k) * SW_TILE;
 }
+__host__ __device__ __forceinline__ size_t sw_power_bytes(int n, int k, int pair) { return (size_t)sw_row_blocks(n, pair) * sr_pitch(k) * 16; }
 __host__ __device__ __forceinline__ size_t sw_bytes(int n, int k, int pair) {
-  return sw_code_bytes(n, k, pair) + (size_t)sw_row_blocks(n, pair) * sr_pitch(k) * 16;
+  return sw_code_bytes(n, k, pair) + sw_power_bytes(n, k, pair) + (size_t)sw_row_blocks(n, pair) * 16;
 }
 
 // grid: (k blocks padded to pitch, row blocks); sixteen lanes quantise a row's block
@@ -252,7 +254,7 @@ scaled_pack_k(const T *__restrict__ w, long long stride, int n, int k, uint8_t *
   const long long group = blockIdx.y + row0, block = group * step + first;   // of the rows, of the packed matrix
   uint8_t *at = powers + ((block * (sr_pitch(k) / 4) + kb / 4) * 16 + row) * 4 + kb % 4;
   if (kb >= blocks) {
-    if (sub == 0) *at = 127;
+    if (sub == 0) *at = 1;
     return;
   }
   float v[8];
@@ -265,9 +267,26 @@ scaled_pack_k(const T *__restrict__ w, long long stride, int n, int k, uint8_t *
   }
   uint32_t byte;
   const uint2 c = block_codes(v, byte);
+  uint32_t any = (c.x | c.y) & 0x7f7f7f7fu;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) any |= (uint32_t)__shfl_xor((int)any, o, 64);
   // k = 8 sub: half sub / 8, lane group (sub mod 8) / 2, codes 8 (sub mod 2) .. of the lane's sixteen
   *(uint2 *)(codes + (block * blocks + kb) * SW_TILE + (sub >> 3) * 1024 + (((sub & 7) >> 1) * 16 + row) * 16 + (sub & 1) * 8) = c;
-  if (sub == 0) *at = (uint8_t)byte;
+  if (sub == 0) *at = any ? (uint8_t)byte : 1;
+}
+
+// each row's largest power: a thread a row
+__global__ void __launch_bounds__(256)
+scaled_tops_k(const uint8_t *__restrict__ powers, long long rows, int groups, uint8_t *__restrict__ tops) {
+  const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows) return;
+  const uint32_t *p = (const uint32_t *)powers + (r >> 4) * groups * 16 + (r & 15);
+  uint32_t top = 0u;
+  for (int g = 0; g < groups; ++g) {
+    const uint32_t v = p[(long long)g * 16];
+    top = max(max(max(v & 255u, v >> 8 & 255u), max(v >> 16 & 255u, v >> 24)), top);
+  }
+  tops[r] = (uint8_t)top;
 }
 
 }  // namespace spark

@@ -48,19 +48,19 @@ def _stride(t) -> int:
 
 class _on:
     """the device of a call's tensors, current while the call is made; its current stream"""
-    __slots__ = ("guard",)
+    __slots__ = ("device", "guard")
 
-    def __init__(self, *tensors):
-        dev = tensors[0].device
-        for t in tensors[1:]:
-            if t is not None and t.device != dev:
+    def __init__(self, first, *others):
+        self.device = first.get_device()
+        for t in others:
+            if t is not None and t.get_device() != self.device:
                 _refuse("the tensors are on different devices")
-        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
+        self.guard = torch.cuda.device(self.device) if self.device != torch.cuda.current_device() else None
 
     def __enter__(self):
         if self.guard is not None:
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.device)   # (torch.cuda.current_stream() takes 3 us)
 
     def __exit__(self, *a):
         if self.guard is not None:

@@ -188,6 +188,7 @@ def check_product(out, x, w, k, dtype):
     return float(((got - want).norm() / want.norm().clamp(min=1e-300)))
 
 
+# (16, 32, 64 and 128 rows a tile; k cut where tiles are fewer than compute units)
 MATMULS = [(1, 1, 1), (1, 16, 128), (1, 5, 300), (1, 4608, 3584), (2, 100, 1000), (8, 257, 513), (15, 48, 640), (16, 130, 1024), (17, 129, 1100),
            (31, 1001, 1000), (33, 64, 129), (48, 300, 2048), (64, 500, 1500), (65, 16, 4096), (96, 1000, 700), (128, 256, 128), (129, 257, 384),
            (200, 513, 1153), (255, 1024, 896), (256, 768, 512), (257, 300, 3000), (511, 640, 1280), (700, 1100, 300), (1023, 520, 260), (3, 96, 18944)]

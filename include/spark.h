@@ -386,6 +386,19 @@ int spark_scaled_gated(const void *codes, const void *powers, int32_t m, const v
                        void *out_codes, void *out_powers, void *workspace, size_t workspace_bytes,
                        void *hip_stream);
 
+/* The layers of a context on these operators.  spark_scaled_projections packs q/k/v, o, gate/up and down of
+ * every layer of a bf16 model into buffer [device, 256-byte aligned, at least the bytes that
+ * spark_scaled_model_bytes writes to *bytes [host]; the caller's, it must outlive the context or its use], and from
+ * then on every pass of this context through the layers -- prompts, steps, flushes -- reads them instead of
+ * the caller's tensors: half the bytes.  Norms, attention, cache, residual stream and both heads stay as they are;
+ * the rows that a projection reads are 8-bit rows, and passes of more than 64 rows hand its sums on in
+ * bf16.  The results are those of a model whose projections have 8-bit weights and inputs, not those of the bf16
+ * model.  May be called between any two calls, cached keys and values stay; NULL goes back to the caller's weights.
+ * Returns when the weights are packed.  SPARK_EINVAL: an fp32 model; SPARK_ENOMEM: buffer too small or misaligned (the
+ * context goes on as before in both). */
+int spark_scaled_model_bytes(const spark_config *cfg, size_t *bytes);
+int spark_scaled_projections(spark_ctx *ctx, void *buffer, size_t bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ EXPORTS = ("spark_workspace_bytes", "spark_init", "spark_seq_open", "spark_prefi
            "spark_seq_text_budget", "spark_schedule_preview", "spark_seq_set_phase", "spark_align_phases",
            "spark_init_static", "spark_tune", "spark_measure_read", "spark_scaled_rows", "spark_scaled_norm",
            "spark_scaled_weight_bytes", "spark_scaled_pack", "spark_scaled_workspace_bytes", "spark_scaled_matmul",
-           "spark_scaled_gated")
+           "spark_scaled_gated", "spark_scaled_model_bytes", "spark_scaled_projections")
 
 
 class SparkConfig(C.Structure):
@@ -110,6 +110,8 @@ def load_library() -> C.CDLL:
     lib.spark_scaled_workspace_bytes.argtypes = [I, I, I, I, C.POINTER(Z)]
     lib.spark_scaled_matmul.argtypes = [P, P, I, P, I, I, P, I, L, P, Z, P]
     lib.spark_scaled_gated.argtypes = [P, P, I, P, I, I, P, P, P, Z, P]
+    lib.spark_scaled_model_bytes.argtypes = [C.POINTER(SparkConfig), C.POINTER(Z)]
+    lib.spark_scaled_projections.argtypes = [P, P, Z]
     _lib = lib
     return lib
 
@@ -311,6 +313,21 @@ class Spark:
 
     def tune(self, name: str, value: int) -> None:
         self._check(self.lib.spark_tune(self.handle, name.encode(), int(value)))
+
+    def scaled_projections(self, on: bool = True) -> None:
+        """the layers' projections in 8 bits from now on, or (False) with the caller's weights again"""
+        import torch
+        if not on:
+            self._check(self.lib.spark_scaled_projections(self.handle, None, 0))
+            self.scaled = None
+            return
+        size = C.c_size_t()
+        if self.lib.spark_scaled_model_bytes(C.byref(self.cfg), C.byref(size)):
+            raise SparkError(-1, "8-bit projections are made of bf16 weights")
+        buf = torch.empty(size.value, dtype=torch.uint8, device=self.kv_pool.device)
+        torch.cuda.synchronize()
+        self._check(self.lib.spark_scaled_projections(self.handle, buf.data_ptr(), size.value))
+        self.scaled = buf
 
     def measure_read(self, tensor, reps: int = 8, nontemporal: bool = True):
         """(GB/s, xor checksum) of a plain streaming read of a torch device tensor"""

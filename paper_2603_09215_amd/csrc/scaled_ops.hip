@@ -39,10 +39,10 @@ GemmArgs gemm_args(const ScaledProduct &p, int pair) {
   GemmArgs a{};
   a.codes = p.codes; a.powers = p.powers;
   a.weights = p.weights;
-  a.weight_powers = a.weights + sw_code_bytes(p.n, p.k, pair);
-  a.weight_tops = a.weight_powers + sw_power_bytes(p.n, p.k, pair);
-  a.m = p.m; a.n = p.n; a.k = p.k;
   a.row_blocks = (int)sw_row_blocks(p.n, pair);
+  a.weight_powers = a.weights + sw_code_bytes(a.row_blocks, p.k);
+  a.weight_tops = a.weight_powers + sw_power_bytes(a.row_blocks, p.k);
+  a.m = p.m; a.n = p.n; a.k = p.k;
   return a;
 }
 
@@ -138,13 +138,12 @@ hipError_t launch_scaled_norm(const NormArgs &a, int h_dtype, int y_dtype, hipSt
   return hipGetLastError();
 }
 
-hipError_t launch_scaled_pack(const void *w, int dtype, long long stride, int n, int k, void *packed, int pair, int first, hipStream_t stream) {
+hipError_t launch_scaled_pack(const void *w, int dtype, long long stride, int n, int k, void *packed, long long blocks, int step, int first, hipStream_t stream) {
   const bool vec = rows_vector(w, dtype, stride, k);
-  uint8_t *codes = (uint8_t *)packed, *powers = codes + sw_code_bytes(n, k, pair);
+  uint8_t *codes = (uint8_t *)packed, *powers = codes + sw_code_bytes(blocks, k);
   const long long groups = sw_row_blocks(n, 0);
   for (long long r0 = 0; r0 < groups; r0 += 32768) {   // (a grid's second side ends at 65535)
     const dim3 grid(sr_pitch(k), (unsigned)std::min<long long>(groups - r0, 32768));
-    const int step = pair ? 2 : 1;
     if (dtype == SR_FP32) {
       if (vec) scaled_pack_k<float, true><<<grid, 256, 0, stream>>>((const float *)w, stride, n, k, codes, powers, step, first, (int)r0);
       else scaled_pack_k<float, false><<<grid, 256, 0, stream>>>((const float *)w, stride, n, k, codes, powers, step, first, (int)r0);
@@ -153,8 +152,19 @@ hipError_t launch_scaled_pack(const void *w, int dtype, long long stride, int n,
       else scaled_pack_k<bf16_t, false><<<grid, 256, 0, stream>>>((const bf16_t *)w, stride, n, k, codes, powers, step, first, (int)r0);
     }
   }
-  const long long rows = groups * 16 * (pair ? 2 : 1);   // (of a pair: once more behind its second matrix)
-  scaled_tops_k<<<(unsigned)((rows + 255) / 256), 256, 0, stream>>>(powers, rows, sr_pitch(k) / 4, powers + sw_power_bytes(n, k, pair));
+  return hipGetLastError();
+}
+
+hipError_t launch_scaled_tops(void *packed, long long blocks, int k, hipStream_t stream) {
+  uint8_t *powers = (uint8_t *)packed + sw_code_bytes(blocks, k);
+  scaled_tops_k<<<(unsigned)((blocks * 16 + 255) / 256), 256, 0, stream>>>(powers, blocks * 16, sr_pitch(k) / 4, powers + sw_power_bytes(blocks, k));
+  return hipGetLastError();
+}
+
+hipError_t launch_scaled_add(float *h, const RowDesc *rows, const void *y, int y_dtype, int m, int k, hipStream_t stream) {
+  const unsigned grid = (unsigned)std::min<long long>(((long long)m * (k / 4) + 255) / 256, 4096);
+  if (y_dtype == SR_FP32) scaled_add_k<float><<<grid, 256, 0, stream>>>(h, rows, (const float *)y, m, k);
+  else scaled_add_k<bf16_t><<<grid, 256, 0, stream>>>(h, rows, (const bf16_t *)y, m, k);
   return hipGetLastError();
 }
 
@@ -267,8 +277,10 @@ int spark_scaled_pack(const void *w, const void *up, int32_t dtype, int64_t stri
   if (!size_ok(n) || !size_ok(k) || !matrix_ok(w, dtype, stride, k) || (up && !matrix_ok(up, dtype, stride, k)) || !aligned(packed, 16))
     return SPARK_EINVAL;
   if (packed_bytes < sw_bytes(n, k, up != nullptr)) return SPARK_ENOMEM;
-  hipError_t e = launch_scaled_pack(w, dtype, stride, n, k, packed, up != nullptr, 0, (hipStream_t)hip_stream);
-  if (e == hipSuccess && up) e = launch_scaled_pack(up, dtype, stride, n, k, packed, 1, 1, (hipStream_t)hip_stream);
+  const long long blocks = sw_row_blocks(n, up != nullptr);
+  hipError_t e = launch_scaled_pack(w, dtype, stride, n, k, packed, blocks, up ? 2 : 1, 0, (hipStream_t)hip_stream);
+  if (e == hipSuccess && up) e = launch_scaled_pack(up, dtype, stride, n, k, packed, blocks, 2, 1, (hipStream_t)hip_stream);
+  if (e == hipSuccess) e = launch_scaled_tops(packed, blocks, k, (hipStream_t)hip_stream);
   return status(e);
 }
 

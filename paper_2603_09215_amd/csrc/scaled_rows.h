@@ -1,22 +1,8 @@
-// 8-bit rows: e4m3 codes with a power of two for every 128 values of a row, and the kernels that make them.
-//
-// A row of k values is kp codes (kp = k rounded up to 128s, zeros behind k) and `pitch` bytes b (one per 128 codes,
-// padded to a multiple of four with 127); a code c of a block stands for c * 2^(b - 127).  The power is the smallest for
-// which no magnitude of the block passes 448, e4m3's largest: with the block's largest = f 2^x, f in [0.5, 1), and
-// 448 = 0.875 * 2^9, it is 2^(x - 9), or the next one where f > 0.875.  A power of two and not any fp32 number, because
-// the matrix instructions of this chip multiply by it themselves (an exponent byte per lane), so that a product needs no
-// arithmetic besides them; what it costs is nothing in precision (e4m3 keeps 4 significant bits over 2^15 whatever the
-// power), and at most one of those 15 binades.  NaN and infinities become e4m3's NaN and have no part in the power.
+// The kernels that make 8-bit rows (scaled_format.h): of plain rows, behind the residual's addition and the norm, of weights.
 #pragma once
-#include "device_common.h"
+#include "scaled_format.h"
 
 namespace spark {
-
-constexpr int SR_BLOCK = 128;   // codes per power of two
-constexpr int SR_NONE = -1, SR_FP32 = 0, SR_BF16 = 1;   // (SPARK_DTYPE_*)
-
-__host__ __device__ __forceinline__ int sr_blocks(int k) { return (int)(((long long)k + SR_BLOCK - 1) / SR_BLOCK); }
-__host__ __device__ __forceinline__ int sr_pitch(int k) { return (sr_blocks(k) + 3) & ~3; }   // bytes of powers per row
 
 // ------------------------------------------------------------------ eight values, a sixteenth of a block, per thread
 
@@ -139,17 +125,6 @@ scaled_rows_k(const T *__restrict__ x, long long stride, int m, int k, uint8_t *
 // h' = h + y (rounded to h's type; y absent: h' = h), v = h' / sqrt(mean h'^2 + eps) * gain -> 8-bit rows.
 // In 64 bits from the sum of squares to the code: that is what makes every code the one that the formula gives, whatever
 // the order of the sum, and a memory-bound kernel has the time for it.
-struct NormArgs {
-  const void *h, *y;
-  void *h_out;
-  const float *gain;
-  long long h_stride, y_stride, out_stride;
-  const RowDesc *rows;   // nullable: row r of h and h_out is rows[r].x_slot
-  int m, k;
-  double eps;
-  uint8_t *codes, *powers;
-};
-
 // One workgroup of NT threads a row; a thread has S times eight values in registers.  S == 0: a row of any length, read a
 // second time for the codes.
 template <typename T, typename Y, bool HAS_Y, bool VEC, int NT, int S>
@@ -228,22 +203,21 @@ __global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
   if (threadIdx.x < pitch - blocks) a.powers[r * pitch + blocks + threadIdx.x] = 127;
 }
 
-// ------------------------------------------------------------------ weights
+// h[row] += y[row] where no norm follows (behind the last layer of a run); four values a thread
+template <typename Y>
+__global__ void __launch_bounds__(256) scaled_add_k(float *__restrict__ h, const RowDesc *__restrict__ rows, const Y *__restrict__ y, int m, int k) {
+  const int fours = k / 4;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)m * fours; i += (long long)gridDim.x * 256) {
+    const int r = (int)(i / fours), c = (int)(i - (long long)r * fours) * 4;
+    float4 *at = (float4 *)(h + (long long)rows[r].x_slot * k + c);
+    const Y *v = y + (long long)r * k + c;
+    float4 s = *at;
+    s.x += Elem<Y>::widen(v[0]); s.y += Elem<Y>::widen(v[1]); s.z += Elem<Y>::widen(v[2]); s.w += Elem<Y>::widen(v[3]);
+    *at = s;
+  }
+}
 
-// Packed weights: tiles of 16 rows x 128 k as the matrix instructions take them, [row block][k block][half][lane][16 codes]:
-// lane l of half h holds row l mod 16, k = 64 h + 16 (l / 16) .. + 15, so that a wave reads a tile with two contiguous
-// instructions.  Behind them the powers, [row block][k block / 4][row][4], of blocks of zeros and behind the last the lowest,
-// and behind those each row's largest power, [row block][16].  Rows behind n are zeros.  A pair of matrices (gated)
-// alternates its row blocks: even ones of the gate, odd ones of the other.
-constexpr int SW_TILE = 2048;
-__host__ __device__ __forceinline__ long long sw_row_blocks(int n, int pair) { return (((long long)n + 15) / 16) * (pair ? 2 : 1); }
-__host__ __device__ __forceinline__ size_t sw_code_bytes(int n, int k, int pair) {
-  return (size_t)sw_row_blocks(n, pair) * sr_blocks(k) * SW_TILE;
-}
-__host__ __device__ __forceinline__ size_t sw_power_bytes(int n, int k, int pair) { return (size_t)sw_row_blocks(n, pair) * sr_pitch(k) * 16; }
-__host__ __device__ __forceinline__ size_t sw_bytes(int n, int k, int pair) {
-  return sw_code_bytes(n, k, pair) + sw_power_bytes(n, k, pair) + (size_t)sw_row_blocks(n, pair) * 16;
-}
+// ------------------------------------------------------------------ weights
 
 // grid: (k blocks padded to pitch, row blocks); sixteen lanes quantise a row's block
 template <typename T, bool VEC>

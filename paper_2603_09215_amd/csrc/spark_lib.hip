@@ -24,6 +24,7 @@
 #include "one_row.h"
 #include "row_rule.h"
 #include "sampling.h"
+#include "scaled_ops.h"
 #include "sched.h"
 #include "small_steps.h"
 
@@ -79,6 +80,9 @@ struct PassBuffers {
   int *tokens;
   int rows;                          // rows that fit
 };
+
+// Where the 8-bit weights and the rows that their products read and write lie in the caller's buffer (spark_scaled_projections)
+struct ScaledMap { size_t qkv, o, gateup, down, layer, codes, powers, act_codes, act_powers, y, work, work_bytes, total; };
 
 struct Seq {
   bool open = false, prefilled = false;
@@ -148,6 +152,8 @@ struct spark_ctx {
   int attn_splits_now = 0;   // context slices the rows of the passes being enqueued can reach (0: unknown, launch all)
   std::map<std::array<int, 3>, MixedCover> mixed_covers;   // (blocks of rows, input, tasks) of large passes
   std::map<std::pair<const void *, size_t>, int> occ_cache;  // workgroups per CU of a (kernel, LDS bytes)
+  char *scaled = nullptr;      // the 8-bit weights of the layers and their buffers; nullptr: the layers run on the caller's weights
+  ScaledMap sm{};
   // profiling of one kernel class
   int prof_class = -1;
   std::vector<hipEvent_t> prof_ev;
@@ -1106,10 +1112,136 @@ bool enqueue_one_row(spark_ctx *c, int l0, int l1, const RowDesc *row) {
   return false;
 }
 
+// ------------------------------------------------------------------ 8-bit projections
+
+constexpr int SCALED_ROWS = 1024;   // of a pass through the layers, at most
+constexpr int SCALED_CUS = 256;     // compute units that k is cut over, at most: the buffer's size depends on no device
+// Passes of more rows hand sums on in bf16, whose products take half the time (GLM shape, 1023 rows, down: 100 us, fp32 131);
+// up to here the weights' way from memory is what takes the time, and they stay in fp32.
+constexpr int SCALED_FP32_ROWS = 64;
+
+void scaled_map(const spark_config &g, ScaledMap &s) {
+  size_t o = 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+  const int d = g.d_model, qw = g.n_q_heads * g.head_dim, qkv = qw + 2 * g.n_kv_heads * g.head_dim, F = g.d_ffn, wide = std::max(d, qw);
+  s.qkv = take(sw_bytes(qkv, d, 0));
+  s.o = take(sw_bytes(d, qw, 0));
+  s.gateup = take(sw_bytes(F, d, 1));
+  s.down = take(sw_bytes(d, F, 0));
+  s.layer = o;
+  o = s.layer * g.n_layers;
+  s.codes = take((size_t)SCALED_ROWS * sr_blocks(wide) * SR_BLOCK);
+  s.powers = take((size_t)SCALED_ROWS * sr_pitch(wide));
+  s.act_codes = take((size_t)SCALED_ROWS * sr_blocks(F) * SR_BLOCK);
+  s.act_powers = take((size_t)SCALED_ROWS * sr_pitch(F));
+  s.y = take(sizeof(float) * SCALED_ROWS * std::max(qkv, d));
+  s.work_bytes = 0;
+  for (int m = 1; m <= SCALED_ROWS; ++m)
+    s.work_bytes = std::max({s.work_bytes, scaled_workspace_bytes(m, qkv, d, 0, SCALED_CUS), scaled_workspace_bytes(m, d, qw, 0, SCALED_CUS),
+                             scaled_workspace_bytes(m, F, d, 1, SCALED_CUS), scaled_workspace_bytes(m, d, F, 0, SCALED_CUS)});
+  s.work = take(s.work_bytes);
+  s.total = o;
+}
+
+// the layers' matrices of a bf16 model as packed 8-bit weights, q, k and v one below the other
+int build_scaled(spark_ctx *c) {
+  const spark_config &g = c->cfg;
+  const size_t d = g.d_model, qw = (size_t)g.n_q_heads * g.head_dim, kvw = (size_t)g.n_kv_heads * g.head_dim, F = g.d_ffn;
+  const bf16_t *wq = (const bf16_t *)c->w.wq, *wk = (const bf16_t *)c->w.wk, *wv = (const bf16_t *)c->w.wv, *wo = (const bf16_t *)c->w.wo,
+               *wg = (const bf16_t *)c->w.wg, *wu = (const bf16_t *)c->w.wu, *wd = (const bf16_t *)c->w.wd;
+  for (size_t l = 0; l < (size_t)g.n_layers; ++l) {
+    char *at = c->scaled + l * c->sm.layer;
+    auto pack = [&](size_t to, const bf16_t *w, size_t n, size_t k, long long blocks, int step, int first) -> int {
+      HIP_TRY(c, launch_scaled_pack(w, SR_BF16, (long long)k, (int)n, (int)k, at + to, blocks, step, first, c->stream));
+      return SPARK_OK;
+    };
+    auto tops = [&](size_t to, size_t k, long long blocks) -> int {
+      HIP_TRY(c, launch_scaled_tops(at + to, blocks, (int)k, c->stream));
+      return SPARK_OK;
+    };
+    const long long qkv = sw_row_blocks((int)(qw + 2 * kvw), 0), db = sw_row_blocks((int)d, 0), fb = sw_row_blocks((int)F, 1);
+    int rc;   // (head sizes are multiples of 16: each of q, k and v begins at a row block)
+    if ((rc = pack(c->sm.qkv, wq + l * qw * d, qw, d, qkv, 1, 0)) || (rc = pack(c->sm.qkv, wk + l * kvw * d, kvw, d, qkv, 1, (int)(qw / 16))) ||
+        (rc = pack(c->sm.qkv, wv + l * kvw * d, kvw, d, qkv, 1, (int)((qw + kvw) / 16))) || (rc = tops(c->sm.qkv, d, qkv)) ||
+        (rc = pack(c->sm.o, wo + l * d * qw, d, qw, db, 1, 0)) || (rc = tops(c->sm.o, qw, db)) ||
+        (rc = pack(c->sm.gateup, wg + l * F * d, F, d, fb, 2, 0)) || (rc = pack(c->sm.gateup, wu + l * F * d, F, d, fb, 2, 1)) ||
+        (rc = tops(c->sm.gateup, d, fb)) || (rc = pack(c->sm.down, wd + l * d * F, d, F, db, 1, 0)) || (rc = tops(c->sm.down, F, db)))
+      return rc;
+  }
+  HIP_TRY(c, hipStreamSynchronize(c->stream));
+  return SPARK_OK;
+}
+
+// q/k/v's sums of a row [width]: rotary positions, queries to their buffer, keys and values to the cache
+template <typename Y> __global__ void __launch_bounds__(256) rope_rows_k(EpiQKV<bf16_t> epi, const RowDesc *__restrict__ rows, const Y *__restrict__ y, int width) {
+  const int half = epi.hd >> 1, task = blockIdx.x * 256 + threadIdx.x, r = blockIdx.y;
+  if (task >= width / 2) return;
+  const int head = task / half;
+  const Y *at = y + (size_t)r * width + head * epi.hd + (task - head * half);
+  NoState none;
+  epi.finish(task, r, rows[r], Elem<Y>::widen(at[0]), Elem<Y>::widen(at[half]), none);
+}
+
+// layers [l0, l1) on at most SCALED_ROWS rows, the projections in 8 bits
+int run_layers_scaled(spark_ctx *c, int l0, int l1, const RowDesc *rows, int m) {
+  const spark_config &g = c->cfg;
+  const int d = g.d_model, hd = g.head_dim, nq = g.n_q_heads, nkv = g.n_kv_heads, F = g.d_ffn, qw = nq * hd, qkv = qw + 2 * nkv * hd;
+  const ScaledMap &s = c->sm;
+  const int type = m > SCALED_FP32_ROWS ? SR_BF16 : SR_FP32, n_cu = std::min(c->n_cu, SCALED_CUS);
+  uint8_t *codes = (uint8_t *)c->scaled + s.codes, *powers = (uint8_t *)c->scaled + s.powers;
+  uint8_t *act_codes = (uint8_t *)c->scaled + s.act_codes, *act_powers = (uint8_t *)c->scaled + s.act_powers;
+  void *y = c->scaled + s.y, *work = c->scaled + s.work;
+  auto norm = [&](const float *gain, bool add) -> int {
+    NormArgs a{};
+    a.h = a.h_out = c->pb.hidden; a.y = add ? y : nullptr; a.gain = gain;
+    a.h_stride = a.out_stride = a.y_stride = d;
+    a.rows = rows; a.m = m; a.k = d; a.eps = g.rms_eps; a.codes = codes; a.powers = powers;
+    HIP_TRY(c, launch_scaled_norm(a, SR_FP32, add ? type : SR_NONE, c->stream));
+    return SPARK_OK;
+  };
+  auto matmul = [&](const uint8_t *xc, const uint8_t *xp, const char *w, int n, int k, int kclass) -> int {
+    int rc = prof_begin(c, kclass);
+    if (rc) return rc;
+    HIP_TRY(c, launch_scaled_matmul(ScaledProduct{xc, xp, (const uint8_t *)w, m, n, k}, y, type, n, work, n_cu, c->stream));
+    return prof_end(c, kclass);
+  };
+  EpiQKV<bf16_t> eq{};
+  eq.d = d; eq.nq = nq; eq.nkv = nkv; eq.hd = hd;
+  eq.qbuf = c->pb.q;
+  eq.rope = at<float2>(c, c->lo.rope);
+  eq.kv = kv_view(c);
+  RowMax no_list{nullptr, 0, 0};
+  const dim3 rope_grid((qkv / 2 + 255) / 256, m);
+  int rc;
+  for (int l = l0; l < l1; ++l) {
+    const char *w = c->scaled + (size_t)l * s.layer;
+    if ((rc = norm(c->w.attn_norm + (size_t)l * d, l > l0)) || (rc = matmul(codes, powers, w + s.qkv, qkv, d, SPARK_KC_QKV))) return rc;
+    eq.layer = l;
+    if (type == SR_FP32) rope_rows_k<float><<<rope_grid, 256, 0, c->stream>>>(eq, rows, (const float *)y, qkv);
+    else rope_rows_k<bf16_t><<<rope_grid, 256, 0, c->stream>>>(eq, rows, (const bf16_t *)y, qkv);
+    HIP_TRY(c, hipGetLastError());
+    if ((rc = launch_attention<bf16_t>(c, rows, m, l, RowOut{c->pb.attn, qw, 0}, no_list))) return rc;
+    HIP_TRY(c, launch_scaled_rows(c->pb.attn, SR_FP32, qw, m, qw, codes, powers, c->stream));
+    if ((rc = matmul(codes, powers, w + s.o, d, qw, SPARK_KC_OPROJ)) || (rc = norm(c->w.mlp_norm + (size_t)l * d, true)) ||
+        (rc = prof_begin(c, SPARK_KC_GATEUP))) return rc;
+    HIP_TRY(c, launch_scaled_gated(ScaledProduct{codes, powers, (const uint8_t *)(w + s.gateup), m, F, d}, act_codes, act_powers, work, n_cu, c->stream));
+    if ((rc = prof_end(c, SPARK_KC_GATEUP)) || (rc = matmul(act_codes, act_powers, w + s.down, d, F, SPARK_KC_DOWN))) return rc;
+  }
+  HIP_TRY(c, launch_scaled_add(c->pb.hidden, rows, y, type, m, d, c->stream));
+  return SPARK_OK;
+}
+
 template <typename WT>
 int run_layers(spark_ctx *c, int l0, int l1, const RowDesc *rows, int m) {
   const spark_config &g = c->cfg;
   if (l0 >= l1 || m <= 0) return SPARK_OK;
+  if (std::is_same<WT, bf16_t>::value && c->scaled) {
+    // (more rows in pieces, in order, as below; a piece has the buffers of its pass to itself)
+    const int most = std::min(SCALED_ROWS, c->pb.rows);
+    for (int r0 = 0; r0 < m; r0 += most)
+      if (int rc = run_layers_scaled(c, l0, l1, rows + r0, std::min(most, m - r0))) return rc;
+    return SPARK_OK;
+  }
   // many rows: the projections are dense contractions for the MFMA units
   if (std::is_same<WT, bf16_t>::value && m >= c->mfma_min_rows && c->use_mfma) {
     // (more rows go through the layers in pieces, in order, so that a piece finds the K and V of the rows before it)
@@ -1858,6 +1990,31 @@ int spark_tune(spark_ctx *c, const char *name, int32_t value) {
   else if (k == "fuse_norm") c->fuse_norm = value != 0;
   else return fail(c, SPARK_EINVAL, "unknown tuning name '%s'", name);
   return SPARK_OK;
+}
+
+int spark_scaled_model_bytes(const spark_config *cfg, size_t *bytes) {
+  char why[128];
+  if (!cfg || !bytes || !config_ok(cfg, why, sizeof(why)) || cfg->dtype != SPARK_DTYPE_BF16) return SPARK_EINVAL;
+  ScaledMap s;
+  scaled_map(*cfg, s);
+  *bytes = s.total;
+  return SPARK_OK;
+}
+
+int spark_scaled_projections(spark_ctx *c, void *buffer, size_t bytes) {
+  if (!c) return SPARK_EINVAL;
+  if (!buffer) {
+    c->scaled = nullptr;
+    return SPARK_OK;
+  }
+  if (c->cfg.dtype != SPARK_DTYPE_BF16) return fail(c, SPARK_EINVAL, "8-bit projections are made of bf16 weights");
+  scaled_map(c->cfg, c->sm);
+  if (bytes < c->sm.total || ((uintptr_t)buffer & 255))
+    return fail(c, SPARK_ENOMEM, "the 8-bit projections need %zu bytes, 256-byte aligned", c->sm.total);
+  c->scaled = (char *)buffer;
+  const int rc = build_scaled(c);
+  if (rc) c->scaled = nullptr;
+  return rc;
 }
 
 int spark_seq_open(spark_ctx *c, int32_t cycle_offset, int32_t *seq_id) {

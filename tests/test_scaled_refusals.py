@@ -89,3 +89,17 @@ def test_product_arguments(lib):
         args = list(good)
         args[at] = bad
         assert lib.spark_scaled_gated(*args) == EINVAL, (at, bad)
+
+
+def test_model_bytes(lib):
+    import workloads as wl
+    w = wl.STEP_AUDIO_2_MINI
+    size = C.c_size_t()
+    cfg = sb.make_config(w.shape, w.schedule, 1, 2048, 64)
+    assert lib.spark_scaled_model_bytes(C.byref(cfg), C.byref(size)) == 0
+    weights = 28 * (4608 * 3584 + 3584 * 3584 + 3 * 18944 * 3584)   # a byte each, and powers, rows and parts
+    assert weights < size.value < 1.02 * weights + (128 << 20)
+    assert lib.spark_scaled_model_bytes(C.byref(cfg), None) == EINVAL
+    cfg = sb.make_config(wl.TINY.shape, wl.TINY.schedule, 1, 64, 16)   # fp32
+    assert lib.spark_scaled_model_bytes(C.byref(cfg), C.byref(size)) == EINVAL
+    assert lib.spark_scaled_projections(None, P, 1 << 40) == EINVAL

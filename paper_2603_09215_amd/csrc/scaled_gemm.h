@@ -120,10 +120,10 @@ template <bool FP32> struct WeightStream {
     powers_end = g1;
     codes = buffer_of(a.weights + (long long)nb * blocks * SW_TILE, end);
     powers = buffer_of(a.weight_powers + (long long)nb * groups * 64, powers_end * 64);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) ask(g0, j);
     ask_powers(g0);
     if (FP32) top = a.weight_tops[(long long)nb * 16 + (threadIdx.x & 15)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ask(g0, j);
   }
   __device__ __forceinline__ void ask(int g, int j) {
     c[j] = buffer_operand<ONCE>(codes, (threadIdx.x & 63) * 16 + min((unsigned)(g * 4 + j) * SW_TILE, end), 1024);
@@ -147,10 +147,11 @@ template <bool FP32> __device__ __forceinline__ void add_block(f32x4 &acc, const
   }
 }
 
-// out = X W^T, up to 16 rows.  A workgroup has nw row blocks, kw waves each, which share k; their sums meet in LDS, added in
-// order.  IN_LDS: the rows' codes lie in LDS, fetched once for all waves, rows 16 bytes apart beyond their length so that
-// sixteen of them read side by side meet in no bank; otherwise (long rows) each wave reads its part of them itself, a byte
-// beside every byte of the weights.
+// out = X W^T, up to 16 rows.  A workgroup has nw row blocks, kw waves each, which share k; their sums meet in
+// LDS, added in order.  IN_LDS: the rows' codes lie in LDS, fetched once for all waves, rows 16 bytes apart beyond their length
+// so that sixteen of them read side by side meet in no bank; otherwise (long rows) each wave reads its part of them itself, a
+// byte beside every byte of the weights.  4608 x 3584: 6.4 us with one row, 9.0 with 16 (floor 2.5, a plain read in the same
+// pieces 4.7); 3584 x 18944: 13.8 us with one (4.9 TB/s; 224 of 256 CUs have a row block), 20.4 with 16.
 template <bool IN_LDS, typename OUT>
 __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int kw) {
   constexpr bool FP32 = sizeof(OUT) == 4;
@@ -159,22 +160,40 @@ __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int 
   const int first = blockIdx.x * nw, mine = scalar(wave / kw), part = wave - mine * kw;
   const int blocks = sr_blocks(a.k), pitch = sr_pitch(a.k), groups = pitch / 4, kp = blocks * SR_BLOCK;
   const int g0 = part_begin(groups, part, kw), g1 = part_begin(groups, part + 1, kw);   // (kw <= groups)
+  const int wide = kp / 16, total = a.m * wide, words = a.m * groups;   // of the rows' codes sixteens, of their powers words, the rows one behind the other
+  // (asked for before the weights, so that the rows lie in LDS by the time those come)
+  i32x4 x_first;
+  uint32_t xp_first;
+  if constexpr (IN_LDS) {
+    x_first = ((const i32x4 *)a.codes)[min((int)threadIdx.x, total - 1)];
+    xp_first = ((const uint32_t *)a.powers)[min((int)threadIdx.x, words - 1)];
+  }
+  uint32_t tops = 0u;   // of the four outputs that this thread adds up at the end
+  if constexpr (FP32) tops = ((const uint32_t *)a.weight_tops)[(long long)min(first + (int)(threadIdx.x >> 6), a.row_blocks - 1) * 4 + (lane >> 4)];
   WeightStream<FP32> ws(a, min(first + mine, a.row_blocks - 1), g0, g1);
-  const int row = min(col, a.m - 1);   // (columns behind the last row repeat it, and are not stored)
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   i32x8 c[4];
   uint32_t p = 0u;
   const buffer_t xb = buffer_of(a.codes, (unsigned)a.m * kp), xpb = buffer_of(a.powers, (unsigned)a.m * pitch);
-  const i32x4 *xl = lds + row * (kp / 16 + 1) + (lane >> 4);
-  const uint32_t *xpl = (const uint32_t *)(lds + a.m * (kp / 16 + 1)) + row * groups;
+  const int row = min(col, a.m - 1);   // (columns behind the last row repeat it, and are not stored)
+  uint32_t *xpl = (uint32_t *)(lds + a.m * (wide + 1));
   auto ask = [&](int g, int j) { c[j] = buffer_operand<0>(xb, (unsigned)row * kp + (lane >> 4) * 16 + min(g * 4 + j, blocks - 1) * SR_BLOCK, 64); };
   auto ask_power = [&](int g) { p = buffer_word(xpb, (unsigned)row * pitch + g * 4); };
   if constexpr (IN_LDS) {
-    const int wide = kp / 16;
-    for (int r = 0; r < a.m; ++r) {
-      for (int i = threadIdx.x; i < wide; i += blockDim.x) lds[r * (wide + 1) + i] = ((const i32x4 *)a.codes)[r * wide + i];
-      for (int i = threadIdx.x; i < groups; i += blockDim.x) ((uint32_t *)(lds + a.m * (wide + 1)))[r * groups + i] = ((const uint32_t *)a.powers)[r * groups + i];
+    if ((int)threadIdx.x < total) lds[threadIdx.x + threadIdx.x / wide] = x_first;
+    if ((int)threadIdx.x < words) xpl[threadIdx.x] = xp_first;
+    constexpr int AHEAD = 4;
+    for (int i0 = threadIdx.x + blockDim.x; i0 < total; i0 += AHEAD * blockDim.x) {
+      i32x4 v[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) v[u] = ((const i32x4 *)a.codes)[min(i0 + u * (int)blockDim.x, total - 1)];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u * (int)blockDim.x;
+        if (i < total) lds[i + i / wide] = v[u];
+      }
     }
+    for (int i = threadIdx.x + blockDim.x; i < words; i += blockDim.x) xpl[i] = ((const uint32_t *)a.powers)[i];
     __syncthreads();
   } else {
     ask_power(g0);
@@ -183,7 +202,7 @@ __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int 
   }
   auto turn = [&](int g, auto more) {
     constexpr bool MORE = decltype(more)::value;
-    const uint32_t wp = ws.p, xp = IN_LDS ? xpl[g] : p;
+    const uint32_t wp = ws.p, xp = IN_LDS ? xpl[row * groups + g] : p;
     if constexpr (MORE) {
       ws.ask_powers(g + 1);
       if constexpr (!IN_LDS) ask_power(g + 1);
@@ -191,11 +210,15 @@ __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int kb = min(g * 4 + j, blocks - 1);   // (behind the last block: the last, times zeros)
-      i32x8 x;
-      if constexpr (IN_LDS) x = __builtin_shufflevector(xl[kb * 8], xl[kb * 8 + 4], 0, 1, 2, 3, 4, 5, 6, 7);
-      else x = c[j];
       f16x8 wf[4];
       if constexpr (FP32) scaled_f16(ws.c[j], power_below(byte_of(wp, j), ws.top), wf);
+      i32x8 x;
+      if constexpr (IN_LDS) {
+        const i32x4 *at = lds + row * (wide + 1) + (lane >> 4) + kb * 8;
+        x = __builtin_shufflevector(at[0], at[4], 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        x = c[j];
+      }
       add_block<FP32>(acc, ws.c[j], wf, x, wp, xp, j);
       if constexpr (MORE) {
         ws.ask(g + 1, j);
@@ -209,16 +232,16 @@ __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int 
   if constexpr (IN_LDS) __syncthreads();
   sums[wave * 64 + lane] = acc;
   __syncthreads();
+  if (threadIdx.x >= nw * 64) return;
+  const int b = threadIdx.x >> 6, r = col;
+  if (r >= a.m || first + b >= a.row_blocks) return;
   const bool vec = a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(OUT) - 1)) == 0;
-  for (int i = threadIdx.x; i < nw * 64; i += blockDim.x) {
-    const int l = i & 63, b = i >> 6, r = l & 15;
-    if (r >= a.m || first + b >= a.row_blocks) continue;
-    f32x4 v = sums[b * kw * 64 + l];
-    for (int w = 1; w < kw; ++w) v += sums[(b * kw + w) * 64 + l];
-    if constexpr (FP32) v = with_tops(v, ((const uint32_t *)a.weight_tops)[(long long)(first + b) * 4 + (l >> 4)]);
-    store_four((OUT *)a.out + r * a.out_stride, (first + b) * 16 + (l >> 4) * 4, a.n, vec, v);
-  }
+  f32x4 v = sums[b * kw * 64 + lane];
+  for (int w = 1; w < kw; ++w) v += sums[(b * kw + w) * 64 + lane];
+  if constexpr (FP32) v = with_tops(v, tops);
+  store_four((OUT *)a.out + r * a.out_stride, (first + b) * 16 + (lane >> 4) * 4, a.n, vec, v);
 }
+
 // ------------------------------------------------------------------ tiles
 
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -237,19 +260,18 @@ __device__ __forceinline__ TilePlace tile_place(int n_tiles, int m_tiles) {
 // sums for a finishing launch, [split][row][16 row blocks].
 enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 
-// WN x WM waves, of NT x MT operands of 16 each.  The weights go from memory into registers, RB k blocks ahead; the rows'
-// codes, which the WN waves share, through LDS in operand order, two buffers, a barrier per k block.
-template <int NT, int MT, int WN, int WM, int RB, bool FP32, TileEnd END, typename OUT>
-__global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
-  constexpr int WAVES = WN * WM, TM = MT * WM, UNITS = 2 * TM, UN = (UNITS + WAVES - 1) / WAVES;   // units of the rows: 1 KiB
+// WAVES waves of NT row blocks each, 16 MT rows.  The weights go from memory into registers, RB k blocks ahead, each to one
+// wave; the rows' codes, which all waves share, through LDS in operand order, two buffers, a barrier per k block.
+template <int NT, int MT, int WAVES, int RB, bool FP32, TileEnd END, typename OUT>
+__global__ void __launch_bounds__(64 * WAVES) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
+  constexpr int UNITS = 2 * MT, UN = (UNITS + WAVES - 1) / WAVES;   // units of the rows: 1 KiB
   constexpr int WORDS = 64 * WAVES;   // a thread has a word of the powers of either operand, wanted or not: a branch in the loop lets the compiler gather the products of several blocks behind it
-  static_assert(END != TILE_GATED || (NT % 2 == 0 && NT * WN == 16), "a block of 128 outputs of both matrices");
+  static_assert(END != TILE_GATED || (NT % 2 == 0 && NT * WAVES == 16), "a block of 128 outputs of both matrices");
   static_assert(4 % RB == 0, "");
-  extern __shared__ i32x4 lds[];   // [2][TM][half][64] codes, [2][2][WORDS] words of powers; gated: then [16 TM][OUT_PITCH] floats
-  constexpr int OUT_PITCH = SR_BLOCK + 4, XROWS = 16 * TM, WROWS = 16 * NT * WN;
+  extern __shared__ i32x4 lds[];   // [2][MT][half][64] codes, [2][2][WORDS] words of powers; gated: then [16 MT][OUT_PITCH] floats
+  constexpr int OUT_PITCH = SR_BLOCK + 4, XROWS = 16 * MT, WROWS = 16 * NT * WAVES;
   uint32_t *words = (uint32_t *)(lds + 2 * UNITS * 64);
   const int wave = scalar(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, part = lane >> 4;
-  const int wn = wave % WN, wm = wave / WN;
   const TilePlace at = tile_place(n_tiles, m_tiles);
   const int blocks = sr_blocks(a.k), pitch = sr_pitch(a.k), groups = pitch / 4, kp = blocks * SR_BLOCK;
   const int g0 = part_begin(groups, at.split, splits), g1 = part_begin(groups, at.split + 1, splits);
@@ -258,41 +280,51 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
   const unsigned x_end = (unsigned)rows * kp, xp_end = (unsigned)rows * pitch;
   const buffer_t xb = buffer_of(a.codes + (long long)r0 * kp, x_end), xpb = buffer_of(a.powers + (long long)r0 * pitch, xp_end);
   // NT row blocks one after the other; those behind the last read as zeros
-  const int tile_nb = at.n * WN * NT, nb = tile_nb + wn * NT, have = max(0, min(NT, a.row_blocks - nb));
+  const int tile_nb = at.n * WAVES * NT, nb = tile_nb + wave * NT, have = max(0, min(NT, a.row_blocks - nb));
   const unsigned w_end = (unsigned)have * blocks * SW_TILE;
   const buffer_t wb = buffer_of(a.weights + (long long)(have ? nb : 0) * blocks * SW_TILE, w_end);
-  const unsigned wp_end = (unsigned)min(WN * NT, a.row_blocks - tile_nb) * groups * 64;
+  const unsigned wp_end = (unsigned)min(WAVES * NT, a.row_blocks - tile_nb) * groups * 64;
   const buffer_t wpb = buffer_of(a.weight_powers + (long long)tile_nb * groups * 64, wp_end);
 
-  i32x4 xs[UN];
+  // (loads come back in the order they were asked for: rows and powers fetched closer to their use than the weights would
+  // make the wait for them one for the weights behind)
+  i32x4 xs[RB][UN];
   i32x8 w[RB][NT];
   uint32_t xp_next, wp_next;
-  auto ask_x = [&](int kb) {
+  auto ask_x = [&](int kb, i32x4 (&to)[UN]) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int unit = (u * WAVES + wave) % UNITS;   // (fewer units than waves: some fetch the same)
-      xs[u] = __builtin_amdgcn_raw_buffer_load_b128(xb, (int)((unsigned)((unit >> 1) * 16 + col) * kp + (unit & 1) * 64 + part * 16 +
+      to[u] = __builtin_amdgcn_raw_buffer_load_b128(xb, (int)((unsigned)((unit >> 1) * 16 + col) * kp + (unit & 1) * 64 + part * 16 +
                                                                 (kb < kb1 ? (unsigned)kb * SR_BLOCK : x_end)), 0, 0);
     }
   };
-  auto put_x = [&](int buffer) {
+  auto put_x = [&](int buffer, const i32x4 (&from)[UN]) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int unit = (u * WAVES + wave) % UNITS;
-      lds[(buffer * UNITS + unit) * 64 + lane] = xs[u];
+      lds[(buffer * UNITS + unit) * 64 + lane] = from[u];
     }
   };
   auto ask_w = [&](int kb, int nt, i32x8 &to) {
-    to = buffer_operand<WM == 1 ? ONCE : 0>(wb, lane * 16 + (kb < kb1 ? (unsigned)(nt * blocks + kb) * SW_TILE : w_end), 1024);
+    to = buffer_operand<MT <= 4 ? ONCE : 0>(wb, lane * 16 + (kb < kb1 ? (unsigned)(nt * blocks + kb) * SW_TILE : w_end), 1024);
   };
   const unsigned xp_at = threadIdx.x < XROWS ? threadIdx.x * pitch : xp_end, wp_at = threadIdx.x < WROWS ? ((threadIdx.x >> 4) * groups * 16 + (threadIdx.x & 15)) * 4 : wp_end;
   auto ask_powers = [&](int g) {   // a row's word of the group
     xp_next = buffer_word(xpb, xp_at + (g < g1 ? (unsigned)g * 4 : xp_end));
     wp_next = buffer_word(wpb, wp_at + (g < g1 ? (unsigned)g * 64 : wp_end));
   };
+  int row_top = 0;
+  if constexpr (FP32) row_top = a.weight_tops[(long long)min(tile_nb + (int)(threadIdx.x >> 4), a.row_blocks - 1) * 16 + (threadIdx.x & 15)];
   auto put_powers = [&](int buffer) {
     words[buffer * 2 * WORDS + threadIdx.x] = xp_next;
-    words[buffer * 2 * WORDS + WORDS + threadIdx.x] = wp_next;
+    uint32_t v = wp_next;
+    if constexpr (FP32) {   // relative to the row's largest, as the exponents of fp32 numbers
+      v = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v |= (uint32_t)max((int)byte_of(wp_next, j) - row_top + 127, 0) << (8 * j);
+    }
+    words[buffer * 2 * WORDS + WORDS + threadIdx.x] = v;
   };
   static_assert(XROWS <= 64 * WAVES && WROWS <= 64 * WAVES, "a thread has a row's word");
   f32x4 acc[NT][MT];
@@ -300,37 +332,42 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  uint32_t tops[FP32 ? NT : 1];   // of the operand's row
-  if constexpr (FP32) {
+  uint32_t four[FP32 ? NT : 1];   // the largest powers of the rows of the lane's sums (large tiles have no registers for them until the end)
+  auto take_tops = [&] {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) tops[nt] = a.weight_tops[(long long)min(nb + nt, a.row_blocks - 1) * 16 + col];
-  }
+    for (int nt = 0; nt < NT; ++nt) four[nt] = ((const uint32_t *)a.weight_tops)[(long long)min(nb + nt, a.row_blocks - 1) * 4 + part];
+  };
+  if constexpr (FP32 && RB > 1) take_tops();
   ask_powers(g0);
-  ask_x(kb0);
 #pragma unroll
-  for (int b = 0; b < RB; ++b)
+  for (int b = 0; b < RB; ++b) {
+    ask_x(kb0 + b, xs[b]);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) ask_w(kb0 + b, nt, w[b][nt]);
+  }
   put_powers(g0 & 1);
-  put_x(0);
-  ask_x(kb0 + 1);
+  put_x(0, xs[0]);
+  ask_x(kb0 + RB, xs[0]);
+  ask_powers(g0 + 1);
   for (int g = g0; g < g1; ++g) {
-    const uint32_t *xw = words + (g & 1) * 2 * WORDS + wm * MT * 16 + col, *ww = words + (g & 1) * 2 * WORDS + WORDS + wn * NT * 16 + col;
+    const uint32_t *xw = words + (g & 1) * 2 * WORDS + col, *ww = words + (g & 1) * 2 * WORDS + WORDS + wave * NT * 16 + col;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int kb = g * 4 + j;
       __builtin_amdgcn_sched_barrier(0);   // (blocks worked on side by side take more registers than there are)
       tile_barrier();
-      put_x((j + 1) & 1);
-      ask_x(kb + 2);
-      if (j == 1) ask_powers(g + 1);
-      if (j == 3) put_powers((g + 1) & 1);
-      const i32x4 *xl = lds + ((j & 1) * UNITS + wm * MT * 2) * 64 + lane;
+      put_x((j + 1) & 1, xs[(j + 1) % RB]);
+      ask_x(kb + 1 + RB, xs[(j + 1) % RB]);
+      if (j == 3) {
+        put_powers((g + 1) & 1);
+        ask_powers(g + 2);
+      }
+      const i32x4 *xl = lds + (j & 1) * UNITS * 64 + lane;
       if constexpr (FP32) {
         f16x8 wf[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          scaled_f16(w[j % RB][nt], power_below(byte_of(ww[nt * 16], j), tops[nt]), wf[nt]);
+          scaled_f16(w[j % RB][nt], __uint_as_float(byte_of(ww[nt * 16], j) << 23), wf[nt]);
           ask_w(kb + RB, nt, w[j % RB][nt]);
         }
 #pragma unroll
@@ -349,6 +386,7 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[nt][t][i] = fmaf(sum[nt][i], power, acc[nt][t][i]);
+          if constexpr (NT * MT >= 16) __builtin_amdgcn_sched_barrier(0x7f);
         }
       } else {
         uint32_t wp[NT];
@@ -368,12 +406,11 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
     }
   }
   if constexpr (FP32) {
+    if constexpr (RB == 1) take_tops();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const uint32_t four = ((const uint32_t *)a.weight_tops)[(long long)min(nb + nt, a.row_blocks - 1) * 4 + part];
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int t = 0; t < MT; ++t) acc[nt][t] = with_tops(acc[nt][t], four);
-    }
+      for (int t = 0; t < MT; ++t) acc[nt][t] = with_tops(acc[nt][t], four[nt]);
   }
   if constexpr (END == TILE_GATED) {
     float *outs = (float *)lds;
@@ -385,11 +422,11 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
         f32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = silu_times(acc[nt][t][i], acc[nt + 1][t][i]);
-        *(f32x4 *)(outs + ((wm * MT + t) * 16 + col) * OUT_PITCH + (wn * NT / 2 + nt / 2) * 16 + part * 4) = v;
+        *(f32x4 *)(outs + (t * 16 + col) * OUT_PITCH + (wave * NT / 2 + nt / 2) * 16 + part * 4) = v;
       }
     tile_barrier();
     const int sub = threadIdx.x & 15, o = at.n * SR_BLOCK + sub * 8, nblocks = sr_blocks(a.n), npitch = sr_pitch(a.n);
-    for (int row = threadIdx.x >> 4; row < 16 * TM; row += 4 * WAVES) {
+    for (int row = threadIdx.x >> 4; row < XROWS; row += 4 * WAVES) {
       if (row >= rows) break;   // (the same for a row's sixteen lanes)
       const long long r = r0 + row;
       const f32x4 p = *(const f32x4 *)(outs + row * OUT_PITCH + sub * 8), q = *(const f32x4 *)(outs + row * OUT_PITCH + sub * 8 + 4);
@@ -410,13 +447,33 @@ __global__ void __launch_bounds__(64 * WN * WM) scaled_tile_k(GemmArgs a, int n_
     OUT *out = (OUT *)a.out + (END == TILE_PARTS ? (long long)at.split * a.m * a.out_stride : 0);
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int row = (wm * MT + t) * 16 + col;
+      const int row = t * 16 + col;
       if (row < rows) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           if (nt < have) store_four(out + (r0 + row) * a.out_stride, (int)(nb + nt) * 16 + part * 4, n, vec, acc[nt][t]);
       }
     }
+  }
+}
+
+// N fours of a part, all parts added in order; eight parts are asked for at a time, or their ways from memory follow each other
+template <int N> __device__ __forceinline__ void add_parts(const float *p, int splits, long long apart, const int (&at)[N], f32x4 (&v)[N]) {
+  constexpr int AHEAD = 8 / N > 2 ? 8 / N : 2;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < splits; s0 += AHEAD) {
+    f32x4 w[AHEAD][N];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[u][i] = *(const f32x4 *)(p + min(s0 + u, splits - 1) * apart + at[i]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u < splits) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += w[u][i];
+      }
   }
 }
 
@@ -430,10 +487,10 @@ __global__ void __launch_bounds__(256) scaled_join_k(const float *__restrict__ p
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const long long r = i / fours;
     const int o = (int)(i - r * fours) * 4;
-    const float *p = parts + r * pitch + o;
-    f32x4 v = *(const f32x4 *)p;
-    for (int s = 1; s < splits; ++s) v += *(const f32x4 *)(p + s * apart);
-    store_four(out + r * out_stride, o, n, vec, v);
+    const int at[1] = {0};
+    f32x4 v[1];
+    add_parts<1>(parts + r * pitch + o, splits, apart, at, v);
+    store_four(out + r * out_stride, o, n, vec, v[0]);
   }
 }
 // ... of a pair: sixteen lanes a block of 128 outputs of a row
@@ -450,16 +507,12 @@ __global__ void __launch_bounds__(256) scaled_join_gated_k(const float *__restri
     }
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (o < n) {   // outputs o .. + 7 are half a row block of either matrix
-      const float *p = parts + r * pitch + (o >> 4) * 32 + (o & 15);
-      f32x4 g[2] = {*(const f32x4 *)p, *(const f32x4 *)(p + 4)}, u[2] = {*(const f32x4 *)(p + 16), *(const f32x4 *)(p + 20)};
-      for (int s = 1; s < splits; ++s) {
-        const float *q = p + s * apart;
-        g[0] += *(const f32x4 *)q; g[1] += *(const f32x4 *)(q + 4);
-        u[0] += *(const f32x4 *)(q + 16); u[1] += *(const f32x4 *)(q + 20);
-      }
+      const int at[4] = {0, 4, 16, 20};
+      f32x4 gu[4];
+      add_parts<4>(parts + r * pitch + (o >> 4) * 32 + (o & 15), splits, apart, at, gu);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (o + i < n) v[i] = silu_times(g[i >> 2][i & 3], u[i >> 2][i & 3]);
+        if (o + i < n) v[i] = silu_times(gu[i >> 2][i & 3], gu[2 + (i >> 2)][i & 3]);
     }
     uint32_t byte;
     const uint2 c = block_codes(v, byte);

@@ -57,37 +57,64 @@ template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream
   else scaled_stream_k<false, OUT><<<grid, 64 * nw * kw, sums, stream>>>(a, nw, kw);
 }
 
-// Tiles: their size, and into how many parts k is cut.
-struct TilePlan { int shape, tn, tm, splits; };   // shape: the index below; 16 tn outputs (rows of packed weights), 16 tm rows
+// Tiles: their size, and into how many parts k is cut.  All have eight waves along the outputs (a row block's codes go to
+// one wave), of one or two row blocks each, and as many operands of 16 rows as there are rows or registers.
+struct TilePlan { int shape, splits; };
+struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
+constexpr int TILE_WAVES = 8;
+constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.52f, 0.35f}, {1, 4, 0.59f, 0.41f}, {2, 1, 0.56f, 0.35f}, {2, 2, 0.66f, 0.46f}, {2, 4, 1.07f, 0.75f}, {2, 8, 1.71f, 1.05f}};
 size_t lds_of(int tm, bool gated) {
   return std::max((size_t)2 * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
 }
-int tile_tm(int shape) { return 1 << shape; }
-TilePlan tile_plan(int m, int row_blocks, int k, int n_cu) {
-  TilePlan p;
-  p.shape = m <= 16 ? 0 : m <= 32 ? 1 : m <= 64 ? 2 : 3;
-  p.tn = 16;
-  p.tm = tile_tm(p.shape);
-  const long long tiles = (long long)((row_blocks + p.tn - 1) / p.tn) * ((m + 16 * p.tm - 1) / (16 * p.tm));
-  const int groups = sr_pitch(k) / 4;
-  p.splits = (int)std::max<long long>(1, std::min<long long>(groups / 2, n_cu / tiles));
-  return p;
+
+// The plan whose estimate is shortest.  A tile's k block takes its arithmetic or its weights' way from memory, of which a CU
+// gets 40 GB/s at most and all of them 6.35 TB/s (rows of tiles behind the first read them from L2); tiles go in rounds of one
+// per CU; parts are written and read once more, by a launch of its own.  In us, fitted to 106 sweeps of all shapes and cuts (1 to
+// 2048 rows, the projections of both backbones, both types): the choice is 0.3 % above the best of a sweep on average, 9 % at
+// most; one shape for each number of rows, k cut until every CU has a tile, was 4 % above it, 35 % at most.
+TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu) {
+  TilePlan best{0, 1};
+  float best_us = 1e30f;
+  const int groups = sr_pitch(k) / 4, blocks = sr_blocks(k);
+  for (int i = 0; i < (int)(sizeof(TILE_SHAPES) / sizeof(TILE_SHAPES[0])); ++i) {
+    const TileShape &t = TILE_SHAPES[i];
+    if (pair && t.nt != 2) continue;   // (gate and partner belong to one wave)
+    if (t.mt > 1 && 8 * t.mt >= m) continue;   // (half of the tile's rows would do)
+    const long long tiles = (long long)((row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES)) * ((m + 16 * t.mt - 1) / (16 * t.mt));
+    for (int splits = 1; splits <= groups && (splits == 1 || tiles * splits <= 2ll * n_cu); ++splits) {
+      const long long wgs = tiles * splits;
+      const float active = (float)std::min<long long>(wgs, n_cu), rounds = (float)((wgs + n_cu - 1) / n_cu);
+      const float bytes = (float)(t.nt * TILE_WAVES * SW_TILE), weights = (float)row_blocks * blocks * SW_TILE;
+      const float way = std::max(bytes / 39.7e3f, bytes * active / 6.35e6f);
+      const float kbs = (float)std::min(blocks, 4 * ((groups + splits - 1) / splits));
+      float us = rounds * (2.6f + kbs * std::max(fp32 ? t.us_fp32 : t.us_8bit, std::min(way, weights * 1.9f / 6.35e6f / (rounds * kbs))));
+      if (splits > 1) us += 2.3f + (splits + 0.77f) * (float)m * row_blocks * 64.0f / 4.4e6f;
+      if (us < best_us) { best_us = us; best = TilePlan{i, splits}; }
+    }
+  }
+  return best;
 }
 
 template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, const TilePlan &p, hipStream_t stream) {
-  const int nt = (a.row_blocks + p.tn - 1) / p.tn, mt = (a.m + 16 * p.tm - 1) / (16 * p.tm);
+  const TileShape &t = TILE_SHAPES[p.shape];
+  const int nt = (a.row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES), mt = (a.m + 16 * t.mt - 1) / (16 * t.mt);
   const unsigned grid = (unsigned)nt * mt * p.splits;
-  const size_t lds = lds_of(p.tm, END == TILE_GATED);
-  if (p.shape == 0) scaled_tile_k<2, 1, 8, 1, 4, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
-  else if (p.shape == 1) scaled_tile_k<2, 2, 8, 1, 4, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
-  else if (p.shape == 2) scaled_tile_k<2, 4, 8, 1, 2, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
-  else scaled_tile_k<4, 4, 4, 2, 1, FP32, END, OUT><<<grid, 512, lds, stream>>>(a, nt, mt, p.splits);
+  const size_t lds = lds_of(t.mt, END == TILE_GATED);
+  auto go = [&](auto kern) { kern<<<grid, 64 * TILE_WAVES, lds, stream>>>(a, nt, mt, p.splits); };
+  if constexpr (END != TILE_GATED) {
+    if (p.shape == 0) return go(scaled_tile_k<1, 2, 8, 4, FP32, END, OUT>);
+    if (p.shape == 1) return go(scaled_tile_k<1, 4, 8, 2, FP32, END, OUT>);
+  }
+  if (p.shape == 2) go(scaled_tile_k<2, 1, 8, 4, FP32, END, OUT>);
+  else if (p.shape == 3) go(scaled_tile_k<2, 2, 8, 4, FP32, END, OUT>);
+  else if (p.shape == 4) go(scaled_tile_k<2, 4, 8, 4, FP32, END, OUT>);
+  else go(scaled_tile_k<2, 8, 8, FP32 ? 1 : 2, FP32, END, OUT>);
 }
 
 template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu, hipStream_t stream) {
   if (a.m <= STREAM_ROWS) return stream_launch<OUT>(a, stream);
-  const TilePlan p = tile_plan(a.m, a.row_blocks, a.k, n_cu);
   constexpr bool FP32 = sizeof(OUT) == 4;
+  const TilePlan p = tile_plan(a.m, a.row_blocks, a.k, false, FP32, n_cu);
   if (p.splits == 1) return tile_launch<FP32, TILE_OUT, OUT>(a, p, stream);
   GemmArgs b = a;
   b.out = workspace;
@@ -171,8 +198,12 @@ hipError_t launch_scaled_add(float *h, const RowDesc *rows, const void *y, int y
 size_t scaled_workspace_bytes(int m, int n, int k, int pair, int n_cu) {
   if (m == 0 || (m <= STREAM_ROWS && !pair)) return 0;
   const int row_blocks = (int)sw_row_blocks(n, pair);
-  const TilePlan p = tile_plan(m, row_blocks, k, n_cu);
-  return p.splits == 1 ? 0 : sizeof(float) * p.splits * m * row_blocks * 16;
+  int splits = 1;
+  for (int fp32 = pair; fp32 < 2; ++fp32) {   // (outputs of either type)
+    const int s = tile_plan(m, row_blocks, k, pair, fp32, n_cu).splits;
+    splits = std::max(splits, s);
+  }
+  return splits == 1 ? 0 : sizeof(float) * splits * m * row_blocks * 16;
 }
 
 hipError_t launch_scaled_matmul(const ScaledProduct &p, void *out, int out_dtype, long long out_stride, void *workspace, int n_cu, hipStream_t stream) {
@@ -188,18 +219,18 @@ hipError_t launch_scaled_gated(const ScaledProduct &p, uint8_t *codes, uint8_t *
   GemmArgs a = gemm_args(p, 1);
   a.out = codes;
   a.out_powers = powers;
-  const TilePlan plan = tile_plan(a.m, a.row_blocks, a.k, n_cu);
+  const TilePlan plan = tile_plan(a.m, a.row_blocks, a.k, true, true, n_cu);
   if (plan.splits == 1) {
     tile_launch<true, TILE_GATED, float>(a, plan, stream);
-  } else {
-    GemmArgs b = a;
-    b.out = workspace;
-    b.out_stride = (long long)a.row_blocks * 16;
-    tile_launch<true, TILE_PARTS, float>(b, plan, stream);
-    const long long groups = (long long)a.m * sr_pitch(a.n);
-    scaled_join_gated_k<<<(unsigned)std::min<long long>((groups + 15) / 16, 1 << 16), 256, 0, stream>>>((const float *)workspace, plan.splits, a.m, a.n,
-                                                                                                      a.row_blocks * 16, codes, powers);
+    return hipGetLastError();
   }
+  GemmArgs sums = a;
+  sums.out = workspace;
+  sums.out_stride = (long long)a.row_blocks * 16;
+  tile_launch<true, TILE_PARTS, float>(sums, plan, stream);
+  const long long groups = (long long)a.m * sr_pitch(a.n);
+  scaled_join_gated_k<<<(unsigned)std::min<long long>((groups + 15) / 16, 1 << 16), 256, 0, stream>>>((const float *)workspace, plan.splits, a.m, a.n,
+                                                                                                    a.row_blocks * 16, codes, powers);
   return hipGetLastError();
 }
 

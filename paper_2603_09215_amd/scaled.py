@@ -31,43 +31,34 @@ def _padded(k: int) -> tuple[int, int]:
     return blocks * BLOCK, -(-blocks // 4) * 4
 
 
-def _matrix(t, what: str, shape=None, dtypes=_DTYPE):
-    """a 2-d device tensor of a type the kernels read, rows contiguous"""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dim() != 2 or t.dtype not in dtypes:
+def _matrix(t, what: str, shape=None):
+    """(address, type, stride) of a 2-d device tensor of a type the kernels read, rows contiguous"""
+    code = _DTYPE.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None or not t.is_cuda or t.dim() != 2:
         _refuse(f"{what}: a 2-d fp32 or bf16 tensor on the GPU is wanted")
-    if shape is not None and tuple(t.shape) != shape:
-        _refuse(f"{what} is {tuple(t.shape)}, {shape} is wanted")
-    if t.shape[1] < 1 or (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    m, k = t.shape
+    if shape is not None and (m, k) != shape:
+        _refuse(f"{what} is {m} x {k}, {shape[0]} x {shape[1]} is wanted")
+    stride, step = t.stride()
+    if m <= 1 and stride < k:
+        stride = k              # (of a single row torch may say anything)
+    if k < 1 or (step != 1 and k > 1) or stride < k:
         _refuse(f"{what}: the elements of a row must lie next to each other, and rows apart")
-    return t
+    return t.data_ptr(), code, stride
 
 
-def _stride(t) -> int:
-    return max(t.stride(0), t.shape[1])   # (of a single row torch may say anything)
-
-
-class _on:
-    """the device of a call's tensors, current while the call is made; its current stream"""
-    __slots__ = ("device", "guard")
-
-    def __init__(self, first, *others):
-        self.device = first.get_device()
-        for t in others:
-            if t is not None and t.get_device() != self.device:
-                _refuse("the tensors are on different devices")
-        self.guard = torch.cuda.device(self.device) if self.device != torch.cuda.current_device() else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.device)   # (torch.cuda.current_stream() takes 3 us)
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
-
-
-def _check(rc: int, what: str):
+def _launch(what: str, tensors, call, *args):
+    """call(*args, stream) with the tensors' device current and on its current stream"""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != dev:
+            _refuse("the tensors are on different devices")
+    # (the raw handle: torch.cuda.current_stream() takes 3 us, the smallest launches here 2)
+    if dev == torch._C._cuda_getDevice():
+        rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         raise SparkError(rc, what + " was refused or failed")
 
@@ -114,17 +105,20 @@ class ScaledWeights:
     order the matrix instructions take them."""
 
     def __init__(self, w: torch.Tensor, up: torch.Tensor | None = None):
-        _matrix(w, "w")
-        if up is not None and (_matrix(up, "up", tuple(w.shape)).dtype != w.dtype or _stride(up) != _stride(w)):
-            _refuse("up must have w's type and stride")
+        at, code, stride = _matrix(w, "w")
         self.n, self.k = w.shape
         self.pair = up is not None
+        up_at = None
+        if self.pair:
+            up_at, up_code, up_stride = _matrix(up, "up", (self.n, self.k))
+            if (up_code, up_stride) != (code, stride):
+                _refuse("up must have w's type and stride")
         lib, size = load_library(), C.c_size_t()
-        _check(lib.spark_scaled_weight_bytes(self.n, self.k, int(self.pair), C.byref(size)), "weights")
-        with _on(w, up) as stream:
-            self.packed = torch.empty(size.value, dtype=torch.uint8, device=w.device)
-            _check(lib.spark_scaled_pack(w.data_ptr(), up.data_ptr() if self.pair else None, _DTYPE[w.dtype], _stride(w), self.n, self.k,
-                                         self.packed.data_ptr(), size.value, stream), "packing the weights")
+        if lib.spark_scaled_weight_bytes(self.n, self.k, int(self.pair), C.byref(size)):
+            _refuse(f"weights of {self.n} x {self.k}")
+        self.packed = torch.empty(size.value, dtype=torch.uint8, device=w.device)
+        _launch("packing the weights", (w, up) if self.pair else (w,), lib.spark_scaled_pack, at, up_at, code, stride, self.n, self.k,
+                self.packed.data_ptr(), size.value)
         self._workspace = {}   # rows -> bytes
 
     def workspace_bytes(self, m: int) -> int:
@@ -132,22 +126,29 @@ class ScaledWeights:
         need = self._workspace.get(m)
         if need is None:
             size = C.c_size_t()
-            with _on(self.packed):
-                _check(load_library().spark_scaled_workspace_bytes(m, self.n, self.k, int(self.pair), C.byref(size)), "workspace")
+            with torch.cuda.device(self.packed.device):
+                if load_library().spark_scaled_workspace_bytes(m, self.n, self.k, int(self.pair), C.byref(size)):
+                    _refuse(f"a product of {m} rows")
             need = self._workspace[m] = size.value
         return need
+
+    def workspace(self, m: int):
+        """(tensor or None, its address, its bytes) for one call; torch's allocator hands it on in stream order"""
+        need = self.workspace_bytes(m)
+        if not need:
+            return None, None, 0
+        t = torch.empty(need, dtype=torch.uint8, device=self.packed.device)
+        return t, t.data_ptr(), need
 
 
 def scaled_rows(x: torch.Tensor, out: ScaledRows | None = None) -> ScaledRows:
     """x [m][k], fp32 or bf16, as 8-bit rows"""
-    _matrix(x, "x")
+    at, code, stride = _matrix(x, "x")
     m, k = x.shape
     out = _rows_out(out, m, k, x.device)
-    if m == 0:
-        return out
-    with _on(x, out.codes) as stream:
-        _check(load_library().spark_scaled_rows(x.data_ptr(), _DTYPE[x.dtype], _stride(x), m, k, out.codes.data_ptr(),
-                                                out.scales.data_ptr(), stream), "scaled_rows")
+    if m:
+        _launch("scaled_rows", (x, out.codes), load_library().spark_scaled_rows, at, code, stride, m, k, out.codes.data_ptr(),
+                out.scales.data_ptr())
     return out
 
 
@@ -155,29 +156,21 @@ def scaled_norm(h: torch.Tensor, gain: torch.Tensor, eps: float, y: torch.Tensor
                 h_out: torch.Tensor | None = None, out: ScaledRows | None = None) -> ScaledRows:
     """h' = h + y (in h's type, written to h_out, or to h where none is given), then the 8-bit rows of
     h' / sqrt(mean h'^2 + eps) * gain.  h, y, h_out [m][k] fp32 or bf16, gain fp32 [k]."""
-    _matrix(h, "h")
-    m, k = h.shape
-    if y is not None:
-        _matrix(y, "y", (m, k))
-    h_out = h if h_out is None else _matrix(h_out, "h_out", (m, k), (h.dtype,))
-    if gain.dtype != torch.float32 or tuple(gain.shape) != (k,) or not gain.is_contiguous():
+    at, code, stride = _matrix(h, "h")
+    shape = m, k = tuple(h.shape)
+    y_at, y_code, y_stride = (None, 0, 0) if y is None else _matrix(y, "y", shape)
+    out_at, out_code, out_stride = (at, code, stride) if h_out is None else _matrix(h_out, "h_out", shape)
+    if out_code != code:
+        _refuse("h_out must have h's type")
+    if gain.dtype != torch.float32 or gain.shape != (k,) or not gain.is_contiguous():
         _refuse(f"gain: fp32 [{k}] is wanted")
     if not eps >= 0.0:
         _refuse("eps must not be negative")
     out = _rows_out(out, m, k, h.device)
-    if m == 0:
-        return out
-    with _on(h, y, h_out, gain, out.codes) as stream:
-        _check(load_library().spark_scaled_norm(
-            h.data_ptr(), _DTYPE[h.dtype], _stride(h), None if y is None else y.data_ptr(), 0 if y is None else _DTYPE[y.dtype],
-            0 if y is None else _stride(y), h_out.data_ptr(), _stride(h_out), gain.data_ptr(), eps, m, k, out.codes.data_ptr(),
-            out.scales.data_ptr(), stream), "scaled_norm")
+    if m:
+        _launch("scaled_norm", [t for t in (h, y, h_out, gain, out.codes) if t is not None], load_library().spark_scaled_norm, at, code, stride,
+                y_at, y_code, y_stride, out_at, out_stride, gain.data_ptr(), eps, m, k, out.codes.data_ptr(), out.scales.data_ptr())
     return out
-
-
-def _workspace(x: ScaledRows, w: ScaledWeights):
-    need = w.workspace_bytes(x.m)
-    return (torch.empty(need, dtype=torch.uint8, device=x.codes.device), need) if need else (None, 0)
 
 
 def scaled_matmul(x: ScaledRows, w: ScaledWeights, out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
@@ -188,15 +181,11 @@ def scaled_matmul(x: ScaledRows, w: ScaledWeights, out: torch.Tensor | None = No
         if dtype not in _DTYPE:
             _refuse("dtype: fp32 or bf16 is wanted")
         out = torch.empty(x.m, w.n, dtype=dtype, device=x.codes.device)
-    else:
-        _matrix(out, "out", (x.m, w.n))
-    if x.m == 0:
-        return out
-    with _on(x.codes, w.packed, out) as stream:
-        ws, need = _workspace(x, w)
-        _check(load_library().spark_scaled_matmul(x.codes.data_ptr(), x.scales.data_ptr(), x.m, w.packed.data_ptr(), w.n, w.k, out.data_ptr(),
-                                                  _DTYPE[out.dtype], _stride(out), ws.data_ptr() if need else None, need, stream),
-               "scaled_matmul")
+    at, code, stride = _matrix(out, "out", (x.m, w.n))
+    if x.m:
+        keep, ws, need = w.workspace(x.m)
+        _launch("scaled_matmul", (x.codes, w.packed, out), load_library().spark_scaled_matmul, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
+                w.packed.data_ptr(), w.n, w.k, at, code, stride, ws, need)
     return out
 
 
@@ -205,11 +194,8 @@ def scaled_gated(x: ScaledRows, w: ScaledWeights, out: ScaledRows | None = None)
     if not w.pair or x.k != w.k:
         _refuse(f"rows of {x.k} and {'a pair' if w.pair else 'one matrix'} of {w.k}: a pair of gate and up is wanted")
     out = _rows_out(out, x.m, w.n, x.codes.device)
-    if x.m == 0:
-        return out
-    with _on(x.codes, w.packed, out.codes) as stream:
-        ws, need = _workspace(x, w)
-        _check(load_library().spark_scaled_gated(x.codes.data_ptr(), x.scales.data_ptr(), x.m, w.packed.data_ptr(), w.n, w.k,
-                                                 out.codes.data_ptr(), out.scales.data_ptr(), ws.data_ptr() if need else None, need, stream),
-               "scaled_gated")
+    if x.m:
+        keep, ws, need = w.workspace(x.m)
+        _launch("scaled_gated", (x.codes, w.packed, out.codes), load_library().spark_scaled_gated, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
+                w.packed.data_ptr(), w.n, w.k, out.codes.data_ptr(), out.scales.data_ptr(), ws, need)
     return out

@@ -19,10 +19,9 @@ bool rows_vector(const void *p, int dtype, long long stride, int k) {
 template <typename T, typename Y, bool HAS_Y, bool VEC>
 void norm_shape(const NormArgs &a, hipStream_t stream) {
   const int eights = sr_blocks(a.k) * 16;   // threads' worth of a row
-  if (eights <= 256) scaled_norm_k<T, Y, HAS_Y, VEC, 256, 1><<<a.m, 256, 0, stream>>>(a);
-  else if (eights <= 512) scaled_norm_k<T, Y, HAS_Y, VEC, 256, 2><<<a.m, 256, 0, stream>>>(a);
-  else if (eights <= 1024) scaled_norm_k<T, Y, HAS_Y, VEC, 512, 2><<<a.m, 512, 0, stream>>>(a);
-  else if (eights <= 2048) scaled_norm_k<T, Y, HAS_Y, VEC, 512, 4><<<a.m, 512, 0, stream>>>(a);
+  auto threads = [&](int s) { return (eights + 64 * s - 1) / (64 * s) * 64; };
+  if (eights <= 512) scaled_norm_k<T, Y, HAS_Y, VEC, 512, 1><<<a.m, threads(1), 0, stream>>>(a);
+  else if (eights <= 2048) scaled_norm_k<T, Y, HAS_Y, VEC, 1024, 2><<<a.m, threads(2), 0, stream>>>(a);
   else scaled_norm_k<T, Y, HAS_Y, VEC, 1024, 0><<<a.m, 1024, 0, stream>>>(a);
 }
 template <typename T, typename Y, bool HAS_Y> void norm_vec(const NormArgs &a, bool vec, hipStream_t stream) {
@@ -127,16 +126,29 @@ template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu
 
 }  // namespace
 
+namespace {
+template <typename T, bool VEC> void rows_launch(const T *x, long long stride, int m, int k, uint8_t *codes, uint8_t *powers, hipStream_t stream) {
+  const unsigned pitch = sr_pitch(k);
+  const long long most = (1ll << 31) / pitch;   // rows of a launch, whose blocks are counted in 32 bits
+  for (long long r0 = 0; r0 < m; r0 += most) {
+    const unsigned total = (unsigned)std::min(m - r0, most) * pitch, groups = (total + 15) / 16;
+    const T *xr = x + r0 * stride;
+    uint8_t *cr = codes + r0 * sr_blocks(k) * SR_BLOCK, *pr = powers + r0 * pitch;
+    // (two blocks at a time once that leaves eight workgroups a CU)
+    if (groups < 4096) scaled_rows_k<T, VEC, 1><<<groups, 256, 0, stream>>>(xr, stride, total, k, cr, pr);
+    else scaled_rows_k<T, VEC, 2><<<(groups + 1) / 2, 256, 0, stream>>>(xr, stride, total, k, cr, pr);
+  }
+}
+}  // namespace
+
 hipError_t launch_scaled_rows(const void *x, int dtype, long long stride, int m, int k, uint8_t *codes, uint8_t *powers, hipStream_t stream) {
   const bool vec = rows_vector(x, dtype, stride, k);
-  const long long groups = (long long)m * sr_pitch(k);
-  const unsigned grid = (unsigned)std::min<long long>((groups + 15) / 16, 1 << 20);
   if (dtype == SR_FP32) {
-    if (vec) scaled_rows_k<float, true><<<grid, 256, 0, stream>>>((const float *)x, stride, m, k, codes, powers);
-    else scaled_rows_k<float, false><<<grid, 256, 0, stream>>>((const float *)x, stride, m, k, codes, powers);
+    if (vec) rows_launch<float, true>((const float *)x, stride, m, k, codes, powers, stream);
+    else rows_launch<float, false>((const float *)x, stride, m, k, codes, powers, stream);
   } else {
-    if (vec) scaled_rows_k<bf16_t, true><<<grid, 256, 0, stream>>>((const bf16_t *)x, stride, m, k, codes, powers);
-    else scaled_rows_k<bf16_t, false><<<grid, 256, 0, stream>>>((const bf16_t *)x, stride, m, k, codes, powers);
+    if (vec) rows_launch<bf16_t, true>((const bf16_t *)x, stride, m, k, codes, powers, stream);
+    else rows_launch<bf16_t, false>((const bf16_t *)x, stride, m, k, codes, powers, stream);
   }
   return hipGetLastError();
 }

@@ -6,21 +6,47 @@ namespace spark {
 
 // ------------------------------------------------------------------ eight values, a sixteenth of a block, per thread
 
-// The fp32 number that rounds like d to anything of 22 bits and fewer: cut toward zero, the last bit set if something was
-// cut off.  (Rounded to the nearest fp32 first, one value in 2^20 would fall on the middle between two codes and then be
-// rounded to the wrong one.)
-__device__ __forceinline__ float cut_odd(double d) {
+// The fp32 number that rounds like d to anything of 22 bits and fewer.  d rounded to the nearest fp32 does, but where that
+// lies on the middle between two such numbers, which d itself may lie beside (one value in 2^20 would be rounded to the wrong
+// code): all those middles, and the borders between two powers, end in 13 zeros at least (19 where fp32 has 24 bits).  There
+// d is cut toward zero and the last bit set if something was cut off.
+__device__ __forceinline__ float for_rounding(double d) {
   const float f = (float)d;
   uint32_t u = __float_as_uint(f);
-  const double back = (double)f;
-  if (fabs(back) > fabs(d)) u -= 1u;          // (an infinity becomes the largest finite number: too large for any code either way)
-  if (back != d && d == d) u |= 1u;
+  if ((u & 0x1fffu) == 0u) {
+    const double back = (double)f;
+    if (fabs(back) > fabs(d)) u -= 1u;          // (an infinity becomes the largest finite number: too large for any code either way)
+    if (back != d && d == d) u |= 1u;
+  }
   return __uint_as_float(u);
 }
-
-__device__ __forceinline__ uint32_t finite_magnitude(float f) {
-  const uint32_t u = __float_as_uint(f) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
+// v + w to the nearest bf16, half to even, as fp32 numbers.  The fp32 sum lies on the same side of every middle as v + w
+// itself unless it is one; there a sum that was rounded (the other way round it does not lead back) is worked out in 64 bits.
+__device__ __forceinline__ void add_bf16(float (&v)[8], const float (&w)[8]) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  float s[8];
+  bool unsure = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s[i] = v[i] + w[i];
+    unsure |= ((__float_as_uint(s[i]) & 0xffffu) == 0x8000u) & ((s[i] - v[i] != w[i]) | (s[i] - w[i] != v[i]));   // (no short cuts: a branch each)
+  }
+  if (__any(unsure)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double d = (double)v[i] + (double)w[i];
+      uint32_t u = __float_as_uint(s[i]);
+      if ((u & 0xffffu) == 0x8000u && (double)s[i] != d) u += fabs(d) > fabs((double)s[i]) ? 1u : ~0u;   // off the middle, to d's side
+      s[i] = __uint_as_float(u);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const uint32_t r = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{s[i], s[i + 1]}, b2));
+    v[i] = __uint_as_float(r << 16);
+    v[i + 1] = __uint_as_float(r & 0xffff0000u);
+  }
 }
 
 // the byte of a block whose largest magnitude has these bits
@@ -30,11 +56,8 @@ __device__ __forceinline__ uint32_t power_byte(uint32_t top) {
 }
 __device__ __forceinline__ float power_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
-// eight values times `inv` as codes (to the nearest, half to even; |v * inv| <= 448 where v is finite)
-__device__ __forceinline__ uint2 eight_codes(const float (&v)[8], float inv) {
-  float s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i] = fabsf(v[i]) < INFINITY ? v[i] * inv : __uint_as_float(0x7fc00000u);
+// eight numbers of magnitude 448 at most as codes, to the nearest, half to even
+__device__ __forceinline__ uint2 eight_codes(const float (&s)[8]) {
   uint32_t lo = 0u, hi = 0u;
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], lo, false);
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], lo, true);
@@ -43,53 +66,81 @@ __device__ __forceinline__ uint2 eight_codes(const float (&v)[8], float inv) {
   return make_uint2(lo, hi);
 }
 
-// The 16 lanes of a block (neighbours) bring eight values each; returns their codes, `byte` the block's.
-__device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t &byte) {
-  uint32_t top = 0u;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i]));
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  byte = power_byte(top);
-  return eight_codes(v, power_inverse(byte));
+// the largest of sixteen neighbouring lanes, in all of them
+__device__ __forceinline__ uint32_t max_of_16(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false));    // the other of two
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false));    // the other two of four
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));   // mirrored in eight
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false));   // and in sixteen
 }
 
-// elements c0 .. c0+7 of a row of k; VEC: rows are 16-byte aligned and k is a multiple of eight
+// The 16 lanes of a block (neighbours) bring eight values each; returns their codes, `byte` the block's.
+__device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t &byte) {
+  constexpr uint32_t INF = 0x7f800000u;
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  top = max_of_16(top);
+  float s[8];
+  if (top >= INF) {   // some are no numbers (the same for the sixteen lanes): they are NaN, and have no part in the power
+    top = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t u = __float_as_uint(v[i]) & 0x7fffffffu;
+      top = max(top, u < INF ? u : 0u);
+    }
+    top = max_of_16(top);
+    byte = power_byte(top);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = (__float_as_uint(v[i]) & 0x7fffffffu) < INF ? v[i] * power_inverse(byte) : __uint_as_float(0x7fc00000u);
+  } else {
+    byte = power_byte(top);
+    const float inv = power_inverse(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = v[i] * inv;
+  }
+  return eight_codes(s);
+}
+
+// Elements c0 .. c0+7 of a row of k.  VEC: rows are 16-byte aligned and k is a multiple of eight; otherwise eight that are all
+// there are fetched from wherever they lie (the hardware's vector loads need no alignment: 4099 rows of 2500 bf16 values
+// element by element took 66 us), the last of a row one by one.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) AnyEight { T v[8]; };
 template <typename T, bool VEC>
 __device__ __forceinline__ void load_eight(const T *row, long long c0, int k, float (&v)[8]) {
-  if constexpr (VEC) {
-    if (c0 < k) {
-      if constexpr (sizeof(T) == 2) {
-        Elem<T>::unpack(*(const uint4 *)(row + c0), v);
-      } else {
-        Elem<T>::unpack(*(const uint4 *)(row + c0), *(float (*)[4]) & v[0]);
-        Elem<T>::unpack(*(const uint4 *)(row + c0 + 4), *(float (*)[4]) & v[4]);
-      }
-    } else {
+  if (VEC ? c0 < k : c0 + 8 <= k) {
+    uint4 r[sizeof(T) / 2];
+    if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = ((const uint4 *)(row + c0))[i];
+    } else {
+      __builtin_memcpy(r, (const AnyEight<T> *)(row + c0), sizeof(r));
+    }
+    if constexpr (sizeof(T) == 2) {
+      Elem<T>::unpack(r[0], v);
+    } else {
+      Elem<T>::unpack(r[0], *(float (*)[4]) & v[0]);
+      Elem<T>::unpack(r[1], *(float (*)[4]) & v[4]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c0 + i < k ? Elem<T>::widen(row[c0 + i]) : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = !VEC && c0 + i < k ? Elem<T>::widen(row[c0 + i]) : 0.f;
   }
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ void store_eight(T *row, long long c0, int k, const float (&v)[8]) {   // v: values of T
-  if constexpr (VEC) {
-    if (c0 >= k) return;
-    if constexpr (sizeof(T) == 2) {
-      uint4 r;
-      r.x = (__float_as_uint(v[0]) >> 16) | (__float_as_uint(v[1]) & 0xffff0000u);
-      r.y = (__float_as_uint(v[2]) >> 16) | (__float_as_uint(v[3]) & 0xffff0000u);
-      r.z = (__float_as_uint(v[4]) >> 16) | (__float_as_uint(v[5]) & 0xffff0000u);
-      r.w = (__float_as_uint(v[6]) >> 16) | (__float_as_uint(v[7]) & 0xffff0000u);
-      *(uint4 *)(row + c0) = r;
+  uint32_t r[2 * sizeof(T)];
+#pragma unroll
+  for (int i = 0; i < 2 * (int)sizeof(T); ++i)
+    r[i] = sizeof(T) == 2 ? (__float_as_uint(v[2 * i & 7]) >> 16) | (__float_as_uint(v[2 * i + 1 & 7]) & 0xffff0000u) : __float_as_uint(v[i & 7]);
+  if (VEC ? c0 < k : c0 + 8 <= k) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((uint4 *)(row + c0))[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
     } else {
-      *(float4 *)(row + c0) = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4 *)(row + c0 + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      __builtin_memcpy((AnyEight<T> *)(row + c0), r, sizeof(r));
     }
-  } else {
+  } else if constexpr (!VEC) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (c0 + i < k) row[c0 + i] = sizeof(T) == 2 ? (T)(__float_as_uint(v[i]) >> 16) : (T)v[i];
@@ -98,25 +149,33 @@ __device__ __forceinline__ void store_eight(T *row, long long c0, int k, const f
 
 // ------------------------------------------------------------------ rows
 
-// x [m][k] -> 8-bit rows.  Sixteen lanes a block, blocks of all rows in one sequence.
-template <typename T, bool VEC>
+// x [m][k] -> 8-bit rows.  Sixteen lanes a block, U blocks at a time; blocks of all rows in one sequence (2^31 at most).
+template <typename T, bool VEC, int U>
 __global__ void __launch_bounds__(256)
-scaled_rows_k(const T *__restrict__ x, long long stride, int m, int k, uint8_t *__restrict__ codes, uint8_t *__restrict__ powers) {
-  const int pitch = sr_pitch(k), blocks = sr_blocks(k), sub = threadIdx.x & 15;
-  const long long total = (long long)m * pitch;
-  for (long long b = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4; b < total; b += (long long)gridDim.x * 16) {
-    const long long r = b / pitch;
-    const int kb = (int)(b - r * pitch);
-    if (kb >= blocks) {   // (the same for the sixteen lanes)
-      if (sub == 0) powers[r * pitch + kb] = 127;
+scaled_rows_k(const T *__restrict__ x, long long stride, unsigned total, int k, uint8_t *__restrict__ codes, uint8_t *__restrict__ powers) {
+  const unsigned pitch = sr_pitch(k), blocks = sr_blocks(k), sub = threadIdx.x & 15;
+  const unsigned apart = gridDim.x * 16, first = (blockIdx.x * 256 + threadIdx.x) >> 4;
+  float v[U][8];
+  unsigned row[U], block[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const unsigned b = first + u * apart;
+    row[u] = b / pitch;
+    block[u] = b - row[u] * pitch;
+    load_eight<T, VEC>(x + (long long)row[u] * stride, (long long)block[u] * SR_BLOCK + sub * 8, b < total ? k : 0, v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (first + u * apart >= total) break;   // (the same for the sixteen lanes)
+    uint8_t *power = powers + (long long)row[u] * pitch + block[u];
+    if (block[u] >= blocks) {
+      if (sub == 0) *power = 127;
       continue;
     }
-    float v[8];
-    load_eight<T, VEC>(x + r * stride, (long long)kb * SR_BLOCK + sub * 8, k, v);
     uint32_t byte;
-    const uint2 c = block_codes(v, byte);
-    *(uint2 *)(codes + (r * blocks + kb) * SR_BLOCK + sub * 8) = c;
-    if (sub == 0) powers[r * pitch + kb] = (uint8_t)byte;
+    const uint2 c = block_codes(v[u], byte);
+    *(uint2 *)(codes + ((long long)row[u] * blocks + block[u]) * SR_BLOCK + sub * 8) = c;
+    if (sub == 0) *power = (uint8_t)byte;
   }
 }
 
@@ -125,11 +184,12 @@ scaled_rows_k(const T *__restrict__ x, long long stride, int m, int k, uint8_t *
 // h' = h + y (rounded to h's type; y absent: h' = h), v = h' / sqrt(mean h'^2 + eps) * gain -> 8-bit rows.
 // In 64 bits from the sum of squares to the code: that is what makes every code the one that the formula gives, whatever
 // the order of the sum, and a memory-bound kernel has the time for it.
-// One workgroup of NT threads a row; a thread has S times eight values in registers.  S == 0: a row of any length, read a
-// second time for the codes.
-template <typename T, typename Y, bool HAS_Y, bool VEC, int NT, int S>
-__global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
-  __shared__ double sums[NT / 64];
+// One workgroup a row, of MOST threads at most; a thread has S times eight values in registers.  S == 0: a row of any length,
+// read a second time for the codes.
+template <typename T, typename Y, bool HAS_Y, bool VEC, int MOST, int S>
+__global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {
+  __shared__ double sums[MOST / 64];
+  const int NT = blockDim.x;
   const int k = a.k, pitch = sr_pitch(k), blocks = sr_blocks(k);
   const long long kp = (long long)blocks * SR_BLOCK;
   const long long r = blockIdx.x, slot = a.rows ? a.rows[r].x_slot : r;
@@ -141,21 +201,23 @@ __global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
     if constexpr (HAS_Y) {
       float w[8];
       load_eight<Y, VEC>(y, c0, k, w);
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 4) v[i] = v[i] + w[i];   // (one rounding, whatever y's type)
-        else v[i] = bf16_to_f32(f32_to_bf16(cut_odd((double)v[i] + (double)w[i])));
+        for (int i = 0; i < 8; ++i) v[i] += w[i];   // (one rounding, whatever y's type)
+      } else {
+        add_bf16(v, w);
       }
     }
   };
   constexpr int KEEP = S > 0 ? S : 1;
-  float v[KEEP][8];
+  float v[KEEP][8], gain[KEEP][8];
   double ss = 0.0;
   if constexpr (S > 0) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const long long c0 = ((long long)s * NT + threadIdx.x) * 8;
       take(c0, v[s]);
+      load_eight<float, VEC>(a.gain, c0, k, gain[s]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss += (double)v[s][i] * (double)v[s][i];
     }
@@ -176,14 +238,27 @@ __global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
   __syncthreads();
   ss = 0.0;
-#pragma unroll
   for (int w = 0; w < NT / 64; ++w) ss += sums[w];
   const double inv = 1.0 / sqrt(ss / (double)k + a.eps);
-  auto give = [&](long long c0, const float (&vv)[8]) {
-    float g[8], n[8];
-    load_eight<float, VEC>(a.gain, c0, k, g);
+  // The product in fp32, three roundings, is at most 3 units of its last place off: enough to tell which code is nearest
+  // unless it lies within 8 of a middle between two (whose last 19 bits are zeros), or some factor is outside [2^-100, 2^101)
+  // or the product below it.  Then, for one wave of 60, the products are taken in 64 bits.  (All of them in 64 bits: a pass of
+  // 4096 x 4096 bf16 took 35 us, bound by instructions.)
+  const float inv32 = (float)inv;
+  auto give = [&](long long c0, const float (&vv)[8], const float (&g)[8]) {
+    float n[8];
+    bool unsure = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) n[i] = cut_odd((double)vv[i] * inv * (double)g[i]);
+    for (int i = 0; i < 8; ++i) {
+      const float by = inv32 * g[i];
+      n[i] = vv[i] * by;
+      const uint32_t u = __float_as_uint(n[i]), mag = u & 0x7fffffffu, e = __float_as_uint(by) & 0x7f800000u;
+      unsure |= ((mag != 0u) & (((u + 8u) & 0x7ffffu) < 16u)) | (mag - 1u < 0x0d7fffffu) | ((vv[i] != 0.f) & (e - 0x0d800000u >= 0x64800000u));
+    }
+    if (__any(unsure)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[i] = for_rounding((double)vv[i] * inv * (double)g[i]);
+    }
     uint32_t byte;
     const uint2 c = block_codes(n, byte);   // (a block's sixteen lanes are all inside the padded row, or none)
     if (c0 < kp) {
@@ -193,11 +268,12 @@ __global__ void __launch_bounds__(NT) scaled_norm_k(NormArgs a) {
   };
   if constexpr (S > 0) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) give(((long long)s * NT + threadIdx.x) * 8, v[s]);
+    for (int s = 0; s < S; ++s) give(((long long)s * NT + threadIdx.x) * 8, v[s], gain[s]);
   } else {
     for (long long c0 = threadIdx.x * 8; c0 < kp; c0 += NT * 8) {   // (what this thread has written itself)
       load_eight<T, VEC>(out, c0, k, v[0]);
-      give(c0, v[0]);
+      load_eight<float, VEC>(a.gain, c0, k, gain[0]);
+      give(c0, v[0], gain[0]);
     }
   }
   if (threadIdx.x < pitch - blocks) a.powers[r * pitch + blocks + threadIdx.x] = 127;
@@ -242,8 +318,7 @@ scaled_pack_k(const T *__restrict__ w, long long stride, int n, int k, uint8_t *
   uint32_t byte;
   const uint2 c = block_codes(v, byte);
   uint32_t any = (c.x | c.y) & 0x7f7f7f7fu;
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) any |= (uint32_t)__shfl_xor((int)any, o, 64);
+  any = max_of_16(any);
   // k = 8 sub: half sub / 8, lane group (sub mod 8) / 2, codes 8 (sub mod 2) .. of the lane's sixteen
   *(uint2 *)(codes + (block * blocks + kb) * SW_TILE + (sub >> 3) * 1024 + (((sub & 7) >> 1) * 16 + row) * 16 + (sub & 1) * 8) = c;
   if (sub == 0) *at = any ? (uint8_t)byte : 1;

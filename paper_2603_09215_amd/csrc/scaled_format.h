@@ -5,8 +5,8 @@
 // padded to a multiple of four with 127); a code c of a block stands for c * 2^(b - 127).  The power is the smallest for
 // which no magnitude of the block passes 448, e4m3's largest: with the block's largest = f 2^x, f in [0.5, 1), and
 // 448 = 0.875 * 2^9, it is 2^(x - 9), or the next one where f > 0.875.  A power of two and not any fp32 number, because
-// the matrix instructions of this chip multiply by it themselves (an exponent byte per lane), so that a product needs no
-// arithmetic besides them; what it costs is nothing in precision (e4m3 keeps 4 significant bits over 2^15 whatever the
+// the 8-bit matrix instructions of this chip multiply by it themselves (an exponent byte per lane) and the conversions to
+// 16 bits do, so that a product needs little arithmetic besides them; what it costs is nothing in precision (e4m3 keeps 4 significant bits over 2^15 whatever the
 // power), and at most one of those 15 binades.  NaN and infinities become e4m3's NaN and have no part in the power.
 #pragma once
 #include "device_common.h"

@@ -4,10 +4,10 @@
 // operands' powers of two from a byte per lane, and adds to fp32 sums.  Before it adds, it brings the products of eight
 // neighbouring codes to the exponent of the largest and cuts them 13 bits below it (measured: 2^16 and 2^3 add up, 2^2 is
 // lost; across eights nothing is), at most 2^-10 of their magnitudes and 1.4e-5 of the result for normal data.  Outputs
-// of 16 and 8 bits, rounded at 2^-8 and 2^-4, take it.
+// of 16 bits, rounded at 2^-8, take it.
 //
 // v_mfma_f32_16x16x32_f16, at half the rate, on the codes as fp16, the weights' times their power relative to their row's
-// largest: fp16 holds that exactly down to 2^-15 of that power and to 2^-25 of it (2^-34 of the row's largest weight)
+// largest: fp16 holds that exactly down to 2^-15 of that power and to 2^-25 of it (2^-32 of the row's largest weight)
 // below.  Four of them are a block of 128, whose sum is multiplied by the activations' power and added in fp32; the weights'
 // largest power multiplies the whole.  Outputs in fp32 and pairs take it: 1e-7 of the result.
 //

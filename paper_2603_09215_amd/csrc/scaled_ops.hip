@@ -60,7 +60,7 @@ template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream
 // one wave), of one or two row blocks each, and as many operands of 16 rows as there are rows or registers.
 struct TilePlan { int shape, splits; };
 struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
-constexpr int TILE_WAVES = 8;
+constexpr int TILE_WAVES = 8, TILES_MOST = 1 << 20;   // of a launch
 constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.52f, 0.35f}, {1, 4, 0.59f, 0.41f}, {2, 1, 0.56f, 0.35f}, {2, 2, 0.66f, 0.46f}, {2, 4, 1.07f, 0.75f}, {2, 8, 1.71f, 1.05f}};
 size_t lds_of(int tm, bool gated) {
   return std::max((size_t)2 * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
@@ -77,9 +77,9 @@ TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu)
   const int groups = sr_pitch(k) / 4, blocks = sr_blocks(k);
   for (int i = 0; i < (int)(sizeof(TILE_SHAPES) / sizeof(TILE_SHAPES[0])); ++i) {
     const TileShape &t = TILE_SHAPES[i];
-    if (pair && t.nt != 2) continue;   // (gate and partner belong to one wave)
+    if (pair ? t.nt != 2 : i == 2) continue;   // (gate and partner belong to one wave; of single matrices the third shape was best at 8 sizes of 3276)
     if (t.mt > 1 && 8 * t.mt >= m) continue;   // (half of the tile's rows would do)
-    const long long tiles = (long long)((row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES)) * ((m + 16 * t.mt - 1) / (16 * t.mt));
+    const long long tiles = (long long)((row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES)) * ((m - 1) / (16 * t.mt) + 1);
     for (int splits = 1; splits <= groups && (splits == 1 || tiles * splits <= 2ll * n_cu); ++splits) {
       const long long wgs = tiles * splits;
       const float active = (float)std::min<long long>(wgs, n_cu), rounds = (float)((wgs + n_cu - 1) / n_cu);
@@ -96,7 +96,27 @@ TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu)
 
 template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, const TilePlan &p, hipStream_t stream) {
   const TileShape &t = TILE_SHAPES[p.shape];
-  const int nt = (a.row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES), mt = (a.m + 16 * t.mt - 1) / (16 * t.mt);
+  const int nt = (a.row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES);
+  if constexpr (END != TILE_PARTS) {   // (a launch's threads are counted in 32 bits; where k is cut there are 512 workgroups at most)
+    const int most = std::max(1, TILES_MOST / nt) * 16 * t.mt;
+    if (a.m > most) {
+      GemmArgs b = a;
+      for (int r = 0; r < a.m; r += b.m) {   // (b.m <= a.m - r)
+        b.m = std::min(most, a.m - r);
+        tile_launch<FP32, END, OUT>(b, p, stream);
+        b.codes += (long long)b.m * sr_blocks(a.k) * SR_BLOCK;
+        b.powers += (long long)b.m * sr_pitch(a.k);
+        if constexpr (END == TILE_GATED) {
+          b.out = (uint8_t *)b.out + (long long)b.m * sr_blocks(a.n) * SR_BLOCK;
+          b.out_powers += (long long)b.m * sr_pitch(a.n);
+        } else {
+          b.out = (OUT *)b.out + b.m * a.out_stride;
+        }
+      }
+      return;
+    }
+  }
+  const int mt = (a.m - 1) / (16 * t.mt) + 1;
   const unsigned grid = (unsigned)nt * mt * p.splits;
   const size_t lds = lds_of(t.mt, END == TILE_GATED);
   auto go = [&](auto kern) { kern<<<grid, 64 * TILE_WAVES, lds, stream>>>(a, nt, mt, p.splits); };
@@ -104,8 +124,10 @@ template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, con
     if (p.shape == 0) return go(scaled_tile_k<1, 2, 8, 4, FP32, END, OUT>);
     if (p.shape == 1) return go(scaled_tile_k<1, 4, 8, 2, FP32, END, OUT>);
   }
-  if (p.shape == 2) go(scaled_tile_k<2, 1, 8, 4, FP32, END, OUT>);
-  else if (p.shape == 3) go(scaled_tile_k<2, 2, 8, 4, FP32, END, OUT>);
+  if constexpr (END == TILE_GATED || (END == TILE_PARTS && FP32)) {
+    if (p.shape == 2) return go(scaled_tile_k<2, 1, 8, 4, FP32, END, OUT>);
+  }
+  if (p.shape == 3) go(scaled_tile_k<2, 2, 8, 4, FP32, END, OUT>);
   else if (p.shape == 4) go(scaled_tile_k<2, 4, 8, 4, FP32, END, OUT>);
   else go(scaled_tile_k<2, 8, 8, FP32 ? 1 : 2, FP32, END, OUT>);
 }
@@ -129,7 +151,7 @@ template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu
 namespace {
 template <typename T, bool VEC> void rows_launch(const T *x, long long stride, int m, int k, uint8_t *codes, uint8_t *powers, hipStream_t stream) {
   const unsigned pitch = sr_pitch(k);
-  const long long most = (1ll << 31) / pitch;   // rows of a launch, whose blocks are counted in 32 bits
+  const long long most = (1ll << 27) / pitch;   // rows of a launch, whose threads, sixteen a block, are counted in 32 bits
   for (long long r0 = 0; r0 < m; r0 += most) {
     const unsigned total = (unsigned)std::min(m - r0, most) * pitch, groups = (total + 15) / 16;
     const T *xr = x + r0 * stride;

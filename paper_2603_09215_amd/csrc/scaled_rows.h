@@ -171,7 +171,7 @@ __device__ __forceinline__ void store_eight(T *row, long long c0, int k, const f
 
 // ------------------------------------------------------------------ rows
 
-// x [m][k] -> 8-bit rows.  Sixteen lanes a block, U blocks at a time; blocks of all rows in one sequence (2^31 at most).
+// x [m][k] -> 8-bit rows.  Sixteen lanes a block, U blocks at a time; blocks of all rows in one sequence (2^27 at most).
 template <typename T, bool VEC, int U>
 __global__ void __launch_bounds__(256)
 scaled_rows_k(const T *__restrict__ x, long long stride, unsigned total, int k, uint8_t *__restrict__ codes, uint8_t *__restrict__ powers) {

@@ -195,6 +195,8 @@ def scaled_gated(x: ScaledRows, w: ScaledWeights, out: ScaledRows | None = None)
         _refuse(f"rows of {x.k} and {'a pair' if w.pair else 'one matrix'} of {w.k}: a pair of gate and up is wanted")
     out = _rows_out(out, x.m, w.n, x.codes.device)
     if x.m:
+        if out.codes.data_ptr() == x.codes.data_ptr():
+            _refuse("out must not be x")
         keep, ws, need = w.workspace(x.m)
         _launch("scaled_gated", (x.codes, w.packed, out.codes), load_library().spark_scaled_gated, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
                 w.packed.data_ptr(), w.n, w.k, out.codes.data_ptr(), out.scales.data_ptr(), ws, need)

@@ -6,13 +6,17 @@ Products with an output in fp32 are sums in fp32: each block of 128 is taken to 
 fp32 half steps) of the magnitudes it adds, and so is each joining of up to 16 parts: an output of `blocks`
 is off by at most (blocks + 17) 2^-22 of the sum of magnitudes, and by half a step of its type, 2^-24.
 
-With an output in 16 or 8 bits the instruction cuts each product 13 bits below the largest of its eight, seven
+With an output in bf16 the instruction cuts each product 13 bits below the largest of its eight, seven
 of them at most: 2^-10 of the eights' magnitudes, and the sums of its sixteen eights are added with 2^-24 each:
-(2^-10 + 2^-20 blocks) of the magnitudes, and half a step of the type, 2^-8 or the code's.  Typically it is
-some 1e-5, so that of many codes no more than 1 % may differ from those of the 64-bit result.
+(2^-10 + 2^-20 blocks) of the magnitudes, and half a step of the type, 2^-8.
 
-Gated: the two sums as above, silu's slope is at most 1.1, and the fp32 exponential, division and
-products add at most 16 half steps; the code lies between the codes of both ends of that interval."""
+For outputs in fp32 and for pairs the weights are fp16 numbers times their row's largest power P: what lies below
+2^-14 P there is held to half a step of 2^-24 P, which is only of account in rows of very different blocks.
+
+Gated: the two sums as in fp32, silu's slope is at most 1.1, and the fp32 exponential, division and
+products add at most 16 half steps; the code lies between the codes of both ends of that interval.  The sums
+are some 1e-7 off and neighbouring codes 2^-3 or less apart, so that few codes lie so near to a middle that they may
+differ from those of the 64-bit result: of many no more than 0.1 %."""
 import pytest
 import torch
 
@@ -188,10 +192,12 @@ def check_product(out, x, w, k, dtype):
     return float(((got - want).norm() / want.norm().clamp(min=1e-300)))
 
 
-# (16, 32, 64 and 128 rows a tile; k cut where tiles are fewer than compute units)
 MATMULS = [(1, 1, 1), (1, 16, 128), (1, 5, 300), (1, 4608, 3584), (2, 100, 1000), (8, 257, 513), (15, 48, 640), (16, 130, 1024), (17, 129, 1100),
            (31, 1001, 1000), (33, 64, 129), (48, 300, 2048), (64, 500, 1500), (65, 16, 4096), (96, 1000, 700), (128, 256, 128), (129, 257, 384),
            (200, 513, 1153), (255, 1024, 896), (256, 768, 512), (257, 300, 3000), (511, 640, 1280), (700, 1100, 300), (1023, 520, 260), (3, 96, 18944)]
+# sizes whose plans have each shape of tile, over all of k and over parts of it
+MATMULS += [(1500, 700, 100), (2049, 16, 2000), (65, 20000, 100), (257, 700, 4100), (1500, 1300, 100), (700, 700, 10000), (400, 1000, 4100), (3000, 1300, 100),
+            (65, 2000, 10000), (1500, 1300, 2900)]
 
 
 @pytest.mark.parametrize("m,n,k", MATMULS)
@@ -235,6 +241,25 @@ def test_product_of_special_rows(ops, m):
         check_product(out, x, w, k, F32)
 
 
+@pytest.mark.parametrize("m", [1, 16, 40, 200])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_product_of_blocks_of_very_different_sizes(ops, m, dtype):
+    """weights whose blocks are 2^-10 to 2^-40 of their row's largest, with inputs that make them matter"""
+    n, k = 40, 640
+    x, w = activations(m, k, 5, spread=1.0), weights(n, k, 6, F32)
+    down = torch.tensor([0.0, 10, 16, 24, 40]).repeat_interleave(128)
+    w[:20] *= 2.0 ** -down
+    x[::2] *= 2.0 ** (down - 8)
+    hx, hw = held(x), held(w)
+    want, mags = ref.product(hx, hw)
+    err, half = product_bound(5, mags, dtype)
+    if dtype == F32:
+        top = 2.0 ** (ref.quantise(w.double())[1][:, :5].amax(1).double() - 127)
+        err = err + 2.0 ** -25 * top * hx.abs().sum(1, keepdim=True)
+    got = ops.scaled_matmul(ops.scaled_rows(x.cuda()), ops.ScaledWeights(w.cuda()), dtype=dtype).cpu().double()
+    assert bool(((got - want).abs() <= err + half * (want.abs() + err)).all())
+
+
 @pytest.mark.parametrize("m", [1, 32, 100, 400])
 def test_product_is_the_same_every_time(ops, m):
     x, w = activations(m, 3584, 1).cuda(), weights(512, 3584, 2).cuda()
@@ -250,7 +275,7 @@ def check_gated(rows, x, wg, wu, n, k):
     hx = held(x)
     (g, gm), (u, um) = ref.product(hx, held(wg)), ref.product(hx, held(wu))
     blocks = ref.padded(k)[0]
-    dg, du = product_bound(blocks, gm, BF16)[0], product_bound(blocks, um, BF16)[0]
+    dg, du = product_bound(blocks, gm, F32)[0], product_bound(blocks, um, F32)[0]
     silu = g * torch.sigmoid(g)
     a = silu * u
     err = 1.1 * dg * (u.abs() + du) + silu.abs() * du + 16 * 2.0 ** -24 * a.abs() + 2.0 ** -140
@@ -273,13 +298,14 @@ def check_gated(rows, x, wg, wu, n, k):
     near_zero = a.abs() <= err
     if a.numel() >= 1000:
         want = ref.values(*ref.quantise(a))[:, :n]
-        assert float((got != want).double().mean()) <= 0.01
+        assert float((got != want).double().mean()) <= 0.001
     assert bool(((mag >= lo) & (mag <= hi)).all()), int(((mag < lo) | (mag > hi)).sum())
     assert bool(((got * a >= 0) | near_zero).all())
 
 
 GATED = [(1, 1, 1), (1, 128, 128), (1, 200, 1000), (1, 1000, 3584), (7, 129, 500), (16, 256, 512), (17, 384, 1030), (32, 100, 640), (33, 640, 300),
          (64, 130, 1024), (65, 512, 520), (100, 300, 2000), (128, 1024, 256), (130, 700, 384), (256, 256, 128), (300, 900, 640), (513, 130, 1100)]
+GATED += [(17, 16, 1500), (4099, 16, 100), (700, 16, 2900), (3000, 300, 100), (2049, 16, 2000), (1500, 1300, 100), (4099, 16, 2000)]   # (as above)
 
 
 @pytest.mark.parametrize("m,n,k", GATED)
@@ -373,6 +399,35 @@ def test_captured_and_replayed(ops, m):
             assert torch.equal(a, b)
 
 
+def test_more_rows_than_a_launch_takes(ops):
+    """2^27 + 3 rows, whose codes pass 32 bits and whose launches are cut: the same as of 2^22 rows at a time"""
+    m, piece = (1 << 27) + 3, 1 << 22
+    x = torch.randn(m, 1, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    w, pair = ops.ScaledWeights(weights(2, 1, 1).cuda()), ops.ScaledWeights(weights(2, 1, 2).cuda() * 50, weights(2, 1, 3).cuda())
+    rows = ops.scaled_rows(x)
+    out, act = ops.scaled_matmul(rows, w, dtype=BF16), ops.scaled_gated(rows, pair)
+    for r in range(0, m, piece):
+        part = ops.scaled_rows(x[r:r + piece])
+        act_part = ops.scaled_gated(part, pair)
+        for whole, cut in ((rows, part), (act, act_part)):
+            for a, b in ((whole.codes, cut.codes), (whole.scales, cut.scales)):
+                assert torch.equal(a.view(torch.uint8)[r:r + piece], b.view(torch.uint8)), r
+        assert torch.equal(out[r:r + piece], ops.scaled_matmul(part, w, dtype=BF16)), r
+
+
+def test_norm_of_more_rows_than_a_launch_takes(ops):
+    m, k, piece = (1 << 21) + 5, 40, 1 << 19
+    h, y = (torch.randn(m, k, device="cuda", generator=torch.Generator("cuda").manual_seed(s)).bfloat16() for s in (1, 2))
+    gain, out = torch.ones(k, device="cuda"), torch.empty_like(h)
+    rows = ops.scaled_norm(h, gain, 1e-6, y=y, h_out=out)
+    for r in range(0, m, piece):
+        o = torch.empty_like(h[r:r + piece])
+        part = ops.scaled_norm(h[r:r + piece], gain, 1e-6, y=y[r:r + piece], h_out=o)
+        assert torch.equal(o, out[r:r + piece]), r
+        for a, b in ((rows.codes, part.codes), (rows.scales, part.scales)):
+            assert torch.equal(a.view(torch.uint8)[r:r + piece], b.view(torch.uint8)), r
+
+
 def test_no_rows(ops):
     w, pair = ops.ScaledWeights(weights(20, 64, 1).cuda()), ops.ScaledWeights(weights(20, 64, 2).cuda(), weights(20, 64, 3).cuda())
     x = torch.empty(0, 64, device="cuda")
@@ -406,6 +461,7 @@ def test_values_and_refusals(ops):
     assert torch.equal(rows.values().cpu().double(), ref.values(*ref.quantise(x.cpu().double()))[:, :300])
     w = ops.ScaledWeights(weights(40, 300, 1).cuda())
     pair = ops.ScaledWeights(weights(40, 300, 1).cuda(), weights(40, 300, 2).cuda())
+    square = ops.ScaledWeights(weights(300, 300, 1).cuda(), weights(300, 300, 2).cuda())
     gain = torch.ones(300, device="cuda")
     short = ops.ScaledRows.empty(5, 200)
     for call in (lambda: ops.scaled_rows(x.cpu()), lambda: ops.scaled_rows(x.half()), lambda: ops.scaled_rows(x[0]), lambda: ops.scaled_rows(x.t()),
@@ -415,7 +471,7 @@ def test_values_and_refusals(ops):
                  lambda: ops.scaled_norm(x, gain, float("nan")),
                  lambda: ops.scaled_matmul(rows, pair), lambda: ops.scaled_matmul(short, w), lambda: ops.scaled_matmul(rows, w, dtype=torch.float16),
                  lambda: ops.scaled_matmul(rows, w, out=torch.empty(5, 41, device="cuda")), lambda: ops.scaled_gated(rows, w),
-                 lambda: ops.scaled_gated(rows, pair, out=short), lambda: ops.ScaledWeights(x.double()),
+                 lambda: ops.scaled_gated(rows, pair, out=short), lambda: ops.scaled_gated(rows, square, out=rows), lambda: ops.ScaledWeights(x.double()),
                  lambda: ops.ScaledWeights(x, x[:4]), lambda: ops.ScaledRows(rows.codes, rows.scales, 600)):
         with pytest.raises(SparkError):
             call()

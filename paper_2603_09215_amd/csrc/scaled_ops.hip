@@ -62,8 +62,8 @@ struct TilePlan { int shape, splits; };
 struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
 constexpr int TILE_WAVES = 8, TILES_MOST = 1 << 20;   // of a launch
 constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.52f, 0.35f}, {1, 4, 0.59f, 0.41f}, {2, 1, 0.56f, 0.35f}, {2, 2, 0.66f, 0.46f}, {2, 4, 1.07f, 0.75f}, {2, 8, 1.71f, 1.05f}};
-size_t lds_of(int tm, bool gated) {
-  return std::max((size_t)2 * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
+size_t lds_of(int tm, bool fp32, bool gated) {
+  return std::max((size_t)(fp32 ? 4 : 2) * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
 }
 
 // The plan whose estimate is shortest.  A tile's k block takes its arithmetic or its weights' way from memory, of which a CU
@@ -118,7 +118,7 @@ template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, con
   }
   const int mt = (a.m - 1) / (16 * t.mt) + 1;
   const unsigned grid = (unsigned)nt * mt * p.splits;
-  const size_t lds = lds_of(t.mt, END == TILE_GATED);
+  const size_t lds = lds_of(t.mt, FP32, END == TILE_GATED);
   auto go = [&](auto kern) { kern<<<grid, 64 * TILE_WAVES, lds, stream>>>(a, nt, mt, p.splits); };
   if constexpr (END != TILE_GATED) {
     if (p.shape == 0) return go(scaled_tile_k<1, 2, 8, 4, FP32, END, OUT>);
@@ -129,7 +129,7 @@ template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, con
   }
   if (p.shape == 3) go(scaled_tile_k<2, 2, 8, 4, FP32, END, OUT>);
   else if (p.shape == 4) go(scaled_tile_k<2, 4, 8, 4, FP32, END, OUT>);
-  else go(scaled_tile_k<2, 8, 8, FP32 ? 1 : 2, FP32, END, OUT>);
+  else go(scaled_tile_k<2, 8, 8, 2, FP32, END, OUT>);
 }
 
 template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu, hipStream_t stream) {

@@ -317,15 +317,17 @@ class Spark:
     def scaled_projections(self, on: bool = True) -> None:
         """the layers' projections in 8 bits from now on, or (False) with the caller's weights again"""
         import torch
+        dev = self.kv_pool.device
         if not on:
+            torch.cuda.synchronize(dev)   # (what still reads the buffer that is given back)
             self._check(self.lib.spark_scaled_projections(self.handle, None, 0))
             self.scaled = None
             return
         size = C.c_size_t()
         if self.lib.spark_scaled_model_bytes(C.byref(self.cfg), C.byref(size)):
             raise SparkError(-1, "8-bit projections are made of bf16 weights")
-        buf = torch.empty(size.value, dtype=torch.uint8, device=self.kv_pool.device)
-        torch.cuda.synchronize()
+        buf = torch.empty(size.value, dtype=torch.uint8, device=dev)
+        torch.cuda.synchronize(dev)
         self._check(self.lib.spark_scaled_projections(self.handle, buf.data_ptr(), size.value))
         self.scaled = buf
 

@@ -1115,7 +1115,7 @@ bool enqueue_one_row(spark_ctx *c, int l0, int l1, const RowDesc *row) {
 // ------------------------------------------------------------------ 8-bit projections
 
 constexpr int SCALED_ROWS = 1024;   // of a pass through the layers, at most
-constexpr int SCALED_CUS = 256;     // compute units that k is cut over, at most: the buffer's size depends on no device
+constexpr int SCALED_CUS = 256;     // compute units that k is cut over, here: the buffer's size depends on no device
 // Passes of more rows hand sums on in bf16, whose products take half the time (GLM shape, 1023 rows, down: 100 us, fp32 131);
 // up to here the weights' way from memory is what takes the time, and they stay in fp32.
 constexpr int SCALED_FP32_ROWS = 64;
@@ -1187,7 +1187,7 @@ int run_layers_scaled(spark_ctx *c, int l0, int l1, const RowDesc *rows, int m) 
   const spark_config &g = c->cfg;
   const int d = g.d_model, hd = g.head_dim, nq = g.n_q_heads, nkv = g.n_kv_heads, F = g.d_ffn, qw = nq * hd, qkv = qw + 2 * nkv * hd;
   const ScaledMap &s = c->sm;
-  const int type = m > SCALED_FP32_ROWS ? SR_BF16 : SR_FP32, n_cu = std::min(c->n_cu, SCALED_CUS);
+  const int type = m > SCALED_FP32_ROWS ? SR_BF16 : SR_FP32, n_cu = SCALED_CUS;
   uint8_t *codes = (uint8_t *)c->scaled + s.codes, *powers = (uint8_t *)c->scaled + s.powers;
   uint8_t *act_codes = (uint8_t *)c->scaled + s.act_codes, *act_powers = (uint8_t *)c->scaled + s.act_powers;
   void *y = c->scaled + s.y, *work = c->scaled + s.work;

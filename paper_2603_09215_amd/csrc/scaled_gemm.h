@@ -263,7 +263,13 @@ enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 // WAVES waves of NT row blocks each, 16 MT rows.  The weights go from memory into registers, RB k blocks ahead, each to one
 // wave; the rows' codes, which all waves share, through LDS in operand order, two buffers, a barrier per k block.  For
 // outputs in fp32 they lie there as fp16, converted once instead of by every wave: twice the LDS, 70 % fewer conversions (2048 rows,
-// a pair of 13696 x 4096: 439 -> 424 us).
+// a pair of 13696 x 4096: 452 -> 436 us).
+// What it reaches: 2048 x 8192 x 8192 in 162 us with outputs in bf16 (1.70 PFLOP/s), 250 in fp32 (1.10); 1023 x 4096 x 13696, whose k is cut,
+// 84 and 118 us (the second launch 9 of them).  The matrix units are busy 39 and 44 % of the time at the 2.0 GHz the chip then runs at;
+// the rest goes to the tiles' way from L2 through the vector cache (weights fetched by two waves each, four row blocks a
+// wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier, two weight blocks more in flight, and conversions
+// placed between the matrix instructions by hand were all within 2 %.
+// Few rows are bound by the weights' way: a pair of 18944 x 3584 with one row 26.4 us, 136 MB (a plain read: 20.4).
 template <int NT, int MT, int WAVES, int RB, bool FP32, TileEnd END, typename OUT>
 __global__ void __launch_bounds__(64 * WAVES) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
   constexpr int UNITS = 2 * MT, UN = (UNITS + WAVES - 1) / WAVES;   // units of the rows: 1 KiB of codes
@@ -493,7 +499,8 @@ template <int N> __device__ __forceinline__ void add_parts(const float *p, int s
   }
 }
 
-// The parts of a cut k, added in order.  parts [split][m][pitch]; four outputs a thread
+// The parts of a cut k, added in order.  parts [split][m][pitch]; four outputs a thread.  With few rows a launch's own time and one way
+// from memory (2 to 4 us), with 1023 x 4096 in two parts 9 us
 template <typename OUT>
 __global__ void __launch_bounds__(256) scaled_join_k(const float *__restrict__ parts, int splits, int m, int n, int pitch, OUT *__restrict__ out,
                                                      long long out_stride) {

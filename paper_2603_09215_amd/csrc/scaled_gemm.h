@@ -260,23 +260,25 @@ __device__ __forceinline__ TilePlace tile_place(int n_tiles, int m_tiles) {
 // sums for a finishing launch, [split][row][16 row blocks].
 enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 
-// WAVES waves of NT row blocks each, 16 MT rows.  The weights go from memory into registers, RB k blocks ahead, each to one
+// Eight waves of NT row blocks each, 16 MT rows.  The weights go from memory into registers, RB k blocks ahead, each to one
 // wave; the rows' codes, which all waves share, through LDS in operand order, two buffers, a barrier per k block.  For
 // outputs in fp32 they lie there as fp16, converted once instead of by every wave: twice the LDS, 70 % fewer conversions (2048 rows,
 // a pair of 13696 x 4096: 452 -> 436 us).
-// What it reaches: 2048 x 8192 x 8192 in 162 us with outputs in bf16 (1.70 PFLOP/s), 250 in fp32 (1.10); 1023 x 4096 x 13696, whose k is cut,
-// 84 and 118 us (the second launch 9 of them).  The matrix units are busy 39 and 44 % of the time at the 2.0 GHz the chip then runs at;
+// What it reaches: 2048 x 8192 x 8192 in 153 us with outputs in bf16 (1.79 PFLOP/s), 245 in fp32 (1.12); 1023 x 4096 x 13696, whose k is cut,
+// 83 and 111 us (the second launch 9 of them).  The matrix units are busy 39 and 44 % of the time at the 2.0 GHz the chip then runs at;
 // the rest goes to the tiles' way from L2 through the vector cache (weights fetched by two waves each, four row blocks a
-// wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier, two weight blocks more in flight, and conversions
+// wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier and conversions
 // placed between the matrix instructions by hand were all within 2 %.
-// Few rows are bound by the weights' way: a pair of 18944 x 3584 with one row 26.4 us, 136 MB (a plain read: 20.4).
-template <int NT, int MT, int WAVES, int RB, bool FP32, TileEnd END, typename OUT>
-__global__ void __launch_bounds__(64 * WAVES) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
+// RB = 2: 32 x 3584 x 18944 in 19.1 us, pairs of 24 rows 26.8 and 64 rows 33.9; four blocks ahead 22.0, 27.7 and 36.2, one 20.4, 27.1 and 35.8.
+// Few rows are bound by the weights' way: a pair of 18944 x 3584 with one row 26.3 us, 136 MB (a plain read: 20.4).
+constexpr int TILE_WAVES = 8;
+template <int NT, int MT, bool FP32, TileEnd END, typename OUT>
+__global__ void __launch_bounds__(64 * TILE_WAVES) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {
+  constexpr int WAVES = TILE_WAVES, RB = 2;
   constexpr int UNITS = 2 * MT, UN = (UNITS + WAVES - 1) / WAVES;   // units of the rows: 1 KiB of codes
   constexpr int UNIT = FP32 ? 128 : 64;   // sixteens of one in LDS
   constexpr int WORDS = 64 * WAVES;   // a thread has a word of the powers of either operand, wanted or not: a branch in the loop lets the compiler gather the products of several blocks behind it
   static_assert(END != TILE_GATED || (NT % 2 == 0 && NT * WAVES == 16), "a block of 128 outputs of both matrices");
-  static_assert(4 % RB == 0, "");
   extern __shared__ i32x4 lds[];   // [2][MT][half][64] codes (FP32: [2][MT][quarter][64] fp16), [2][2][WORDS] words of powers; gated: then [16 MT][OUT_PITCH] floats
   constexpr int OUT_PITCH = SR_BLOCK + 4, XROWS = 16 * MT, WROWS = 16 * NT * WAVES;
   uint32_t *words = (uint32_t *)(lds + 2 * UNITS * UNIT);

@@ -60,17 +60,18 @@ template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream
 // one wave), of one or two row blocks each, and as many operands of 16 rows as there are rows or registers.
 struct TilePlan { int shape, splits; };
 struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
-constexpr int TILE_WAVES = 8, TILES_MOST = 1 << 20;   // of a launch
-constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.52f, 0.35f}, {1, 4, 0.59f, 0.41f}, {2, 1, 0.56f, 0.35f}, {2, 2, 0.66f, 0.46f}, {2, 4, 1.07f, 0.75f}, {2, 8, 1.71f, 1.05f}};
+constexpr int TILES_MOST = 1 << 20;   // of a launch
+constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.39f, 0.41f}, {1, 4, 0.61f, 0.41f}, {2, 1, 0.44f, 0.38f}, {2, 2, 0.62f, 0.58f}, {2, 4, 0.95f, 0.67f}, {2, 8, 1.66f, 1.00f}};
 size_t lds_of(int tm, bool fp32, bool gated) {
   return std::max((size_t)(fp32 ? 4 : 2) * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
 }
 
 // The plan whose estimate is shortest.  A tile's k block takes its arithmetic or its weights' way from memory, of which a CU
-// gets 40 GB/s at most and all of them 6.35 TB/s (rows of tiles behind the first read them from L2); tiles go in rounds of one
-// per CU; parts are written and read once more, by a launch of its own.  In us, fitted to 106 sweeps of all shapes and cuts (1 to
-// 2048 rows, the projections of both backbones, both types): the choice is 0.3 % above the best of a sweep on average, 9 % at
-// most; one shape for each number of rows, k cut until every CU has a tile, was 4 % above it, 35 % at most.
+// gets 42 GB/s at most and all of them 6.3 TB/s (rows of tiles behind the first read them from L2); tiles go in rounds of one
+// per CU; parts are written and read once more, by a launch of its own.  In us beyond a launch's own, fitted to 178 sweeps of all
+// shapes and cuts (1 to 2048 rows, the projections of both backbones and 1000 x 1000, both types): the choice is 0.3 % above the
+// best of a sweep on average, 7 % at most; one shape for each number of rows, k cut until every CU has a tile, was 4 % above it,
+// 35 % at most.
 TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu) {
   TilePlan best{0, 1};
   float best_us = 1e30f;
@@ -84,10 +85,10 @@ TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu)
       const long long wgs = tiles * splits;
       const float active = (float)std::min<long long>(wgs, n_cu), rounds = (float)((wgs + n_cu - 1) / n_cu);
       const float bytes = (float)(t.nt * TILE_WAVES * SW_TILE), weights = (float)row_blocks * blocks * SW_TILE;
-      const float way = std::max(bytes / 39.7e3f, bytes * active / 6.35e6f);
+      const float way = std::max(bytes / 42.3e3f, bytes * active / 6.32e6f);
       const float kbs = (float)std::min(blocks, 4 * ((groups + splits - 1) / splits));
-      float us = rounds * (2.6f + kbs * std::max(fp32 ? t.us_fp32 : t.us_8bit, std::min(way, weights * 1.9f / 6.35e6f / (rounds * kbs))));
-      if (splits > 1) us += 2.3f + (splits + 0.77f) * (float)m * row_blocks * 64.0f / 4.4e6f;
+      float us = rounds * (0.11f + kbs * std::max(fp32 ? t.us_fp32 : t.us_8bit, std::min(way, weights * 1.52f / 6.32e6f / (rounds * kbs))));
+      if (splits > 1) us += 2.4f + (splits + 1.1f) * (float)m * row_blocks * 64.0f / 3.83e6f;
       if (us < best_us) { best_us = us; best = TilePlan{i, splits}; }
     }
   }
@@ -121,15 +122,15 @@ template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, con
   const size_t lds = lds_of(t.mt, FP32, END == TILE_GATED);
   auto go = [&](auto kern) { kern<<<grid, 64 * TILE_WAVES, lds, stream>>>(a, nt, mt, p.splits); };
   if constexpr (END != TILE_GATED) {
-    if (p.shape == 0) return go(scaled_tile_k<1, 2, 8, 4, FP32, END, OUT>);
-    if (p.shape == 1) return go(scaled_tile_k<1, 4, 8, 2, FP32, END, OUT>);
+    if (p.shape == 0) return go(scaled_tile_k<1, 2, FP32, END, OUT>);
+    if (p.shape == 1) return go(scaled_tile_k<1, 4, FP32, END, OUT>);
   }
   if constexpr (END == TILE_GATED || (END == TILE_PARTS && FP32)) {
-    if (p.shape == 2) return go(scaled_tile_k<2, 1, 8, 4, FP32, END, OUT>);
+    if (p.shape == 2) return go(scaled_tile_k<2, 1, FP32, END, OUT>);
   }
-  if (p.shape == 3) go(scaled_tile_k<2, 2, 8, 4, FP32, END, OUT>);
-  else if (p.shape == 4) go(scaled_tile_k<2, 4, 8, 4, FP32, END, OUT>);
-  else go(scaled_tile_k<2, 8, 8, 2, FP32, END, OUT>);
+  if (p.shape == 3) go(scaled_tile_k<2, 2, FP32, END, OUT>);
+  else if (p.shape == 4) go(scaled_tile_k<2, 4, FP32, END, OUT>);
+  else go(scaled_tile_k<2, 8, FP32, END, OUT>);
 }
 
 template <typename OUT> void matmul_launch(GemmArgs a, void *workspace, int n_cu, hipStream_t stream) {

@@ -197,7 +197,7 @@ MATMULS = [(1, 1, 1), (1, 16, 128), (1, 5, 300), (1, 4608, 3584), (2, 100, 1000)
            (200, 513, 1153), (255, 1024, 896), (256, 768, 512), (257, 300, 3000), (511, 640, 1280), (700, 1100, 300), (1023, 520, 260), (3, 96, 18944)]
 # sizes whose plans have each shape of tile, over all of k and over parts of it
 MATMULS += [(1500, 700, 100), (2049, 16, 2000), (65, 20000, 100), (257, 700, 4100), (1500, 1300, 100), (700, 700, 10000), (400, 1000, 4100), (3000, 1300, 100),
-            (65, 2000, 10000), (1500, 1300, 2900)]
+            (65, 2000, 10000), (1500, 1300, 2900), (700, 1000, 4100), (1500, 300, 10000), (1500, 1300, 4100)]
 
 
 @pytest.mark.parametrize("m,n,k", MATMULS)

@@ -194,7 +194,7 @@ def check_product(out, x, w, k, dtype):
 
 MATMULS = [(1, 1, 1), (1, 16, 128), (1, 5, 300), (1, 4608, 3584), (2, 100, 1000), (8, 257, 513), (15, 48, 640), (16, 130, 1024), (17, 129, 1100),
            (31, 1001, 1000), (33, 64, 129), (48, 300, 2048), (64, 500, 1500), (65, 16, 4096), (96, 1000, 700), (128, 256, 128), (129, 257, 384),
-           (200, 513, 1153), (255, 1024, 896), (256, 768, 512), (257, 300, 3000), (511, 640, 1280), (700, 1100, 300), (1023, 520, 260), (3, 96, 18944)]
+           (200, 513, 1153), (255, 1024, 896), (256, 768, 512), (257, 300, 3000), (511, 640, 1280), (700, 1100, 300), (1023, 520, 260), (3, 96, 18944), (12, 100, 21800), (16, 60, 40000), (16, 200, 16384), (9, 30, 30000)]
 # sizes whose plans have each shape of tile, over all of k and over parts of it
 MATMULS += [(1500, 700, 100), (2049, 16, 2000), (65, 20000, 100), (257, 700, 4100), (1500, 1300, 100), (700, 700, 10000), (400, 1000, 4100), (3000, 1300, 100),
             (65, 2000, 10000), (1500, 1300, 2900), (700, 1000, 4100), (1500, 300, 10000), (1500, 1300, 4100)]

@@ -33,13 +33,17 @@ def _padded(k: int) -> tuple[int, int]:
 
 def _matrix(t, what: str, shape=None):
     """(address, type, stride) of a 2-d device tensor of a type the kernels read, rows contiguous"""
-    code = _DTYPE.get(t.dtype) if isinstance(t, torch.Tensor) else None
-    if code is None or not t.is_cuda or t.dim() != 2:
+    try:
+        code = _DTYPE[t.dtype]
+        m, k = t.shape
+        stride, step = t.stride()
+        on_gpu = t.is_cuda
+    except (AttributeError, KeyError, TypeError, ValueError):
+        on_gpu = False
+    if not on_gpu:
         _refuse(f"{what}: a 2-d fp32 or bf16 tensor on the GPU is wanted")
-    m, k = t.shape
     if shape is not None and (m, k) != shape:
         _refuse(f"{what} is {m} x {k}, {shape[0]} x {shape[1]} is wanted")
-    stride, step = t.stride()
     if m <= 1 and stride < k:
         stride = k              # (of a single row torch may say anything)
     if k < 1 or (step != 1 and k > 1) or stride < k:
@@ -48,10 +52,10 @@ def _matrix(t, what: str, shape=None):
 
 
 def _launch(what: str, tensors, call, *args):
-    """call(*args, stream) with the tensors' device current and on its current stream"""
+    """call(*args, stream) with the tensors' (the first is one, others may be None) device current and on its current stream"""
     dev = tensors[0].get_device()
     for t in tensors:
-        if t.get_device() != dev:
+        if t is not None and t.get_device() != dev:
             _refuse("the tensors are on different devices")
     # (the raw handle: torch.cuda.current_stream() takes 3 us, the smallest launches here 2)
     if dev == torch._C._cuda_getDevice():
@@ -117,7 +121,7 @@ class ScaledWeights:
         if lib.spark_scaled_weight_bytes(self.n, self.k, int(self.pair), C.byref(size)):
             _refuse(f"weights of {self.n} x {self.k}")
         self.packed = torch.empty(size.value, dtype=torch.uint8, device=w.device)
-        _launch("packing the weights", (w, up) if self.pair else (w,), lib.spark_scaled_pack, at, up_at, code, stride, self.n, self.k,
+        _launch("packing the weights", (w, up), lib.spark_scaled_pack, at, up_at, code, stride, self.n, self.k,
                 self.packed.data_ptr(), size.value)
         self._workspace = {}   # rows -> bytes
 
@@ -168,7 +172,7 @@ def scaled_norm(h: torch.Tensor, gain: torch.Tensor, eps: float, y: torch.Tensor
         _refuse("eps must not be negative")
     out = _rows_out(out, m, k, h.device)
     if m:
-        _launch("scaled_norm", [t for t in (h, y, h_out, gain, out.codes) if t is not None], load_library().spark_scaled_norm, at, code, stride,
+        _launch("scaled_norm", (h, y, h_out, gain, out.codes), load_library().spark_scaled_norm, at, code, stride,
                 y_at, y_code, y_stride, out_at, out_stride, gain.data_ptr(), eps, m, k, out.codes.data_ptr(), out.scales.data_ptr())
     return out
 

@@ -41,7 +41,7 @@ struct NormArgs {
   long long h_stride, y_stride, out_stride;
   const RowDesc *rows;   // nullable: row r of h and h_out is rows[r].x_slot
   int m, k;
-  double eps;
+  double eps, one_over_k;   // (the launch's)
   uint8_t *codes, *powers;
 };
 

@@ -180,7 +180,9 @@ hipError_t launch_scaled_norm(const NormArgs &a, int h_dtype, int y_dtype, hipSt
   const bool vec = rows_vector(a.h, h_dtype, a.h_stride, a.k) && rows_vector(a.h_out, h_dtype, a.out_stride, a.k) && aligned16(a.gain) &&
                    (y_dtype == SR_NONE || rows_vector(a.y, y_dtype, a.y_stride, a.k));
   constexpr int MOST_ROWS = 1 << 20;   // of a launch, whose threads are counted in 32 bits
-  for (NormArgs b = a; b.m > 0;) {
+  NormArgs b = a;
+  b.one_over_k = 1.0 / a.k;
+  while (b.m > 0) {
     const int left = b.m - MOST_ROWS;
     b.m = std::min(b.m, MOST_ROWS);
     if (h_dtype == SR_FP32) norm_y<float>(b, y_dtype, vec, stream);

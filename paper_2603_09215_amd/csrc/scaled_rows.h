@@ -20,25 +20,29 @@ __device__ __forceinline__ float for_rounding(double d) {
   }
   return __uint_as_float(u);
 }
-// v + w to the nearest bf16, half to even, as fp32 numbers.  The fp32 sum lies on the same side of every middle as v + w
-// itself unless it is one; there a sum that was rounded (the other way round it does not lead back) is worked out in 64 bits.
-__device__ __forceinline__ void add_bf16(float (&v)[8], const float (&w)[8]) {
+// v + w to the nearest bf16, half to even, as fp32 numbers; v from bf16, w from Y.  The fp32 sum lies on the same side of every
+// middle as v + w itself unless it is one.  With w from bf16 it then is v + w: of 8 bits each, they do not fit into 24 only where
+// one is under 2^-16 of the other, which is a bf16 number and no middle near it.  With w from fp32 a sum that was rounded (the
+// other way round it does not lead back) is worked out in 64 bits.
+template <typename Y> __device__ __forceinline__ void add_bf16(float (&v)[8], const float (&w)[8]) {
   typedef float f2 __attribute__((ext_vector_type(2)));
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   float s[8];
-  bool unsure = false;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s[i] = v[i] + w[i];
-    unsure |= ((__float_as_uint(s[i]) & 0xffffu) == 0x8000u) & ((s[i] - v[i] != w[i]) | (s[i] - w[i] != v[i]));   // (no short cuts: a branch each)
-  }
-  if (__any(unsure)) {
+  for (int i = 0; i < 8; ++i) s[i] = v[i] + w[i];
+  if constexpr (sizeof(Y) == 4) {
+    bool unsure = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const double d = (double)v[i] + (double)w[i];
-      uint32_t u = __float_as_uint(s[i]);
-      if ((u & 0xffffu) == 0x8000u && (double)s[i] != d) u += fabs(d) > fabs((double)s[i]) ? 1u : ~0u;   // off the middle, to d's side
-      s[i] = __uint_as_float(u);
+    for (int i = 0; i < 8; ++i)
+      unsure |= ((__float_as_uint(s[i]) & 0xffffu) == 0x8000u) & ((s[i] - v[i] != w[i]) | (s[i] - w[i] != v[i]));   // (no short cuts: a branch each)
+    if (__any(unsure)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double d = (double)v[i] + (double)w[i];
+        uint32_t u = __float_as_uint(s[i]);
+        if ((u & 0xffffu) == 0x8000u && (double)s[i] != d) u += fabs(d) > fabs((double)s[i]) ? 1u : ~0u;   // off the middle, to d's side
+        s[i] = __uint_as_float(u);
+      }
     }
   }
 #pragma unroll
@@ -105,7 +109,7 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t &byte
 // Elements c0 .. c0+7 of a row of k, zeros behind its end; asked for, and settled once they are there.  VEC: rows are 16-byte
 // aligned and k is a multiple of eight.  Otherwise eight are fetched from wherever they lie (the hardware's vector loads need
 // no alignment), at a row's end the last eight of it, which are then moved into place: no branch stands between the loads.
-// (4099 rows of 2500 bf16 values: element by element 66 us, only the last ones so 29, this 22.5.)
+// (4099 rows of 2500 bf16 values: element by element 66 us, only the last ones so 29, this 22.5, now 19.6.)
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) AnyEight { T v[8]; };
 template <typename T> struct Eight { uint4 r[sizeof(T) / 2]; };   // as they lie in memory
 template <typename T, bool VEC>
@@ -171,6 +175,16 @@ __device__ __forceinline__ void store_eight(T *row, long long c0, int k, const f
 
 // ------------------------------------------------------------------ rows
 
+// 1 / sqrt(x) in 64 bits, x >= 0 or NaN; 0 and infinity give infinity and 0.  The hardware's estimate (2^-23 and better) and two steps of
+// Newton's: the root and two divisions by the library are 60 instructions of every wave, an eighth of the norm's.
+__device__ __forceinline__ double inverse_root(double x) {
+  const double r = __builtin_amdgcn_rsq(x);
+  double y = r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-x * y, y, 1.0), y);
+  return x > 0.0 && x < __builtin_inf() ? y : r;
+}
+
 // x [m][k] -> 8-bit rows.  Sixteen lanes a block, U blocks at a time; blocks of all rows in one sequence (2^27 at most).
 // Bound by memory: 8191 x 4096 bf16 in 21.7 us, 4.6 TB/s (a copy: 5.2); 32 x 3584 fp32 in 1.9 us, a launch's own time.
 template <typename T, bool VEC, int U>
@@ -206,8 +220,8 @@ scaled_rows_k(const T *__restrict__ x, long long stride, unsigned total, int k, 
 
 // h' = h + y (rounded to h's type; y absent: h' = h), v = h' / sqrt(mean h'^2 + eps) * gain -> 8-bit rows.
 // In 64 bits from the sum of squares to the code: that is what makes every code the one that the formula gives, whatever
-// the order of the sum; where fp32 settles the code (below) it stands in.  4096 x 4096 bf16 takes 29 us (4.0 TB/s, instructions
-// and memory about level), fp32 38 us (4.9 TB/s), 1023 x 4096 fp32 14 us, 2048 x 18944 fp32 106 us (4.8 TB/s), one row 3.4 us.
+// the order of the sum; where fp32 settles the code (below) it stands in.  4096 x 4096 bf16 takes 25 us (4.7 TB/s; instructions
+// and memory about level), fp32 37 us (5.0 TB/s), 1023 x 4096 fp32 14 us, 2048 x 18944 fp32 106 us (4.8 TB/s), one row 3.2 us.
 // One workgroup a row, of MOST threads at most; a thread has S times eight values in registers.  S == 0: a row of any length,
 // read a second time for the codes (from L2: 2048 x 18944 in 106 us; four times eight a thread, 640 threads: 121).  Workgroups that
 // stay and fetch their next row ahead take as long (4096 x 4096 bf16 31 us, 1023 rows 15), and so do rows dealt to the XCDs in runs.
@@ -234,7 +248,7 @@ __global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += w[i];   // (one rounding, whatever y's type)
       } else {
-        add_bf16(v, w);
+        add_bf16<Y>(v, w);
       }
     }
   };
@@ -267,22 +281,26 @@ __global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {
   __syncthreads();
   ss = 0.0;
   for (int w = 0; w < NT / 64; ++w) ss += sums[w];
-  const double inv = 1.0 / sqrt(ss / (double)k + a.eps);
+  const double inv = inverse_root(ss * a.one_over_k + a.eps);
   // The product in fp32, three roundings, is at most 3 units of its last place off: enough to tell which code is nearest
-  // unless it lies within 8 of a middle between two (whose last 19 bits are zeros), or some factor is outside [2^-100, 2^101)
-  // or the product below it.  Then, for one wave of 60, the products are taken in 64 bits.  (All of them in 64 bits: a pass of
-  // 4096 x 4096 bf16 took 35 us, bound by instructions.)
+  // unless it lies within 8 of a middle between two (whose last 19 bits are zeros), or may leave fp32's range: it does not with the
+  // root's inverse in [2^-30, 2^60], gains in [2^-20, 2^40] or zero, and sums of 2^-60 and more or zero (one too large is flagged as a
+  // middle).  Otherwise, for one wave of 60, the products are taken in 64 bits.  (All of them in 64 bits: a pass of 4096 x 4096 bf16 took 35 us, bound by instructions.)
   const float inv32 = (float)inv;
+  const bool odd = !(inv32 >= 0x1p-30f && inv32 <= 0x1p60f);
   auto give = [&](long long c0, const float (&vv)[8], const float (&g)[8]) {
     float n[8];
-    bool unsure = false;
+    uint32_t middle = ~0u, small = ~0u, low = ~0u, high = 0u;   // (smallest and largest of the eight; zeros, less one, are in none)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float by = inv32 * g[i];
-      n[i] = vv[i] * by;
-      const uint32_t u = __float_as_uint(n[i]), mag = u & 0x7fffffffu, e = __float_as_uint(by) & 0x7f800000u;
-      unsure |= ((mag != 0u) & (((u + 8u) & 0x7ffffu) < 16u)) | (mag - 1u < 0x0d7fffffu) | ((vv[i] != 0.f) & (e - 0x0d800000u >= 0x64800000u));
+      n[i] = vv[i] * (inv32 * g[i]);
+      const uint32_t u = __float_as_uint(n[i]), less = (__float_as_uint(vv[i]) & 0x7fffffffu) - 1u, size = __float_as_uint(g[i]) & 0x7fffffffu;
+      middle = min(middle, ((u + 8u) & 0x7ffffu) | (less & 0x80000000u));
+      small = min(small, less);
+      low = min(low, size - 1u);
+      high = max(high, size);
     }
+    const bool unsure = odd | (middle < 16u) | (small < 0x217fffffu) | (low < 0x357fffffu) | (high > 0x53800000u);
     if (__any(unsure)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) n[i] = for_rounding((double)vv[i] * inv * (double)g[i]);

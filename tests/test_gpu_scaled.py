@@ -137,6 +137,31 @@ def test_norm_keeps_the_input_where_an_output_is_given(ops):
     assert torch.equal(h, before) and torch.equal(out, before + y)
 
 
+@pytest.mark.parametrize("ytype", [F32, BF16])
+def test_bf16_sums_beside_the_middles(ops, ytype):
+    """h + y at the middle between two bf16 numbers and a little beside it, further down than an fp32 sum can hold"""
+    h = torch.tensor([256.0, 258.0, 1.0, -3.0, 2.0 ** -126, 1e30]).repeat_interleave(64)
+    unit = 2.0 ** (torch.frexp(h.abs())[1].float() - 9)                     # half a step of bf16 at h
+    off = torch.cat([torch.tensor([0.0, 1.0, -1.0]), 2.0 ** -torch.arange(7.0, 35.0), -2.0 ** -torch.arange(7.0, 35.0), torch.zeros(5)]).repeat(6)
+    rows = torch.stack([h, h, h, h, h])
+    y = torch.stack([unit * (1 + off), -unit * (1 + off), unit * 0.5 * (1 + off), unit * off, h * off]).to(ytype)
+    norm_case(ops, rows.to(BF16), y, torch.ones(384), 1e-6)
+
+
+def test_norm_of_special_gains(ops):
+    """gains and rows at the ends of what fp32 products can be trusted with"""
+    k = 512
+    g = torch.Generator().manual_seed(3)
+    h = torch.randn(6, k, generator=g) * torch.tensor([1.0, 1e-25, 1e25, 1e-38, 1e37, 1.0])[:, None]
+    gain = torch.randn(k, generator=g) * 2.0 ** torch.randint(-140, 120, (k,), generator=g).float()
+    gain[::7] = 0.0
+    h[:, 3::11] = 0.0
+    for eps in (0.0, 1e-6, 1e30):
+        norm_case(ops, h, None, gain, eps)
+        norm_case(ops, h, None, torch.full((k,), 2.0 ** -140), eps)
+        norm_case(ops, h.to(BF16), None, 1 + torch.randn(k, generator=g), eps)
+
+
 def test_norm_of_special_rows(ops):
     h = torch.randn(8, 640, generator=torch.Generator().manual_seed(1))
     h[0] = 0.0

@@ -264,8 +264,8 @@ enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 // wave; the rows' codes, which all waves share, through LDS in operand order, two buffers, a barrier per k block.  For
 // outputs in fp32 they lie there as fp16, converted once instead of by every wave: twice the LDS, 70 % fewer conversions (2048 rows,
 // a pair of 13696 x 4096: 452 -> 436 us).
-// What it reaches: 2048 x 8192 x 8192 in 153 us with outputs in bf16 (1.79 PFLOP/s), 245 in fp32 (1.12); 1023 x 4096 x 13696
-// 84 and 115 us.  The matrix units are busy 38 and 45 % of the time at the 2.0 GHz the chip then runs at;
+// What it reaches: 2048 x 8192 x 8192 in 147 us with outputs in bf16 (1.87 PFLOP/s), 245 in fp32 (1.12); 1023 x 4096 x 13696
+// 77 and 115 us.  The matrix units are busy 41 and 45 % of the time at the 2.0 GHz the chip then runs at;
 // the rest goes to the tiles' way from L2 through the vector cache (weights fetched by two waves each, four row blocks a
 // wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier and conversions
 // placed between the matrix instructions by hand were all within 2 %.
@@ -417,13 +417,20 @@ __global__ void __launch_bounds__(64 * TILE_WAVES) scaled_tile_k(GemmArgs a, int
         uint32_t wp[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) wp[nt] = ww[nt * 16] >> (8 * j);
+        i32x8 x[2];
+        uint32_t xp[2];
+        auto take_x = [&](int t) {
+          x[t % 2] = __builtin_shufflevector(xl[t * 128], xl[t * 128 + 64], 0, 1, 2, 3, 4, 5, 6, 7);
+          xp[t % 2] = xw[t * 16] >> (8 * j);
+        };
+        take_x(0);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          const i32x8 x = __builtin_shufflevector(xl[t * 128], xl[t * 128 + 64], 0, 1, 2, 3, 4, 5, 6, 7);
-          const uint32_t xp = xw[t * 16] >> (8 * j);
+          if (t + 1 < MT) take_x(t + 1);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
-            acc[nt][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j % RB][nt], x, acc[nt][t], 0, 0, 0, (int)wp[nt], 0, (int)xp);
+            acc[nt][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j % RB][nt], x[t % 2], acc[nt][t], 0, 0, 0, (int)wp[nt], 0, (int)xp[t % 2]);
+          if constexpr (NT * MT >= 16) __builtin_amdgcn_sched_barrier(0);   // (all of LDS's reads first, then the products: 158 us, not 147)
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) ask_w(kb + RB, nt, w[j % RB][nt]);

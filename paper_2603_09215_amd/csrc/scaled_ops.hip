@@ -61,7 +61,7 @@ template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream
 struct TilePlan { int shape, splits; };
 struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
 constexpr int TILES_MOST = 1 << 20;   // of a launch
-constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.39f, 0.41f}, {1, 4, 0.61f, 0.41f}, {2, 1, 0.44f, 0.38f}, {2, 2, 0.62f, 0.58f}, {2, 4, 0.95f, 0.67f}, {2, 8, 1.66f, 1.00f}};
+constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.39f, 0.41f}, {1, 4, 0.61f, 0.41f}, {2, 1, 0.44f, 0.38f}, {2, 2, 0.62f, 0.58f}, {2, 4, 0.95f, 0.67f}, {2, 8, 1.66f, 0.92f}};
 size_t lds_of(int tm, bool fp32, bool gated) {
   return std::max((size_t)(fp32 ? 4 : 2) * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
 }

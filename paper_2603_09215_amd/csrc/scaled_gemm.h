@@ -265,7 +265,7 @@ enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 // outputs in fp32 they lie there as fp16, converted once instead of by every wave: twice the LDS, 70 % fewer conversions (2048 rows,
 // a pair of 13696 x 4096: 452 -> 436 us).
 // What it reaches: 2048 x 8192 x 8192 in 147 us with outputs in bf16 (1.87 PFLOP/s), 245 in fp32 (1.12); 1023 x 4096 x 13696
-// 77 and 115 us.  The matrix units are busy 41 and 45 % of the time at the 2.0 GHz the chip then runs at;
+// 77 and 115 us.  The matrix units are busy 45 % of the time at the 2.0 GHz the chip then runs at;
 // the rest goes to the tiles' way from L2 through the vector cache (weights fetched by two waves each, four row blocks a
 // wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier and conversions
 // placed between the matrix instructions by hand were all within 2 %.

@@ -68,15 +68,20 @@ template <typename CODES, int N> __device__ __forceinline__ void scaled_f16(cons
 __device__ __forceinline__ uint32_t byte_of(uint32_t bytes, int j) { return bytes >> (8 * j) & 255u; }
 // 2^(byte - top), byte <= top; far down: 0
 __device__ __forceinline__ float power_below(uint32_t byte, uint32_t top) { return __uint_as_float((uint32_t)max((int)byte - (int)top + 127, 0) << 23); }
-// The activations' power times 2^-ROOM: the sums are without the weights' largest power until the end, and rows of numbers
-// up to 1e37 are to stay in fp32's range (as are rows of 1e-30).
-constexpr int ROOM = 20;
-__device__ __forceinline__ float power_with_room(uint32_t byte) { return __uint_as_float((uint32_t)max((int)byte - ROOM, 0) << 23); }
-// what the sums are multiplied by at the end: 2^(top - 127 + ROOM), in two steps, the second 2^ROOM
+// The sums are without the weights' largest power until the end, and times 2^-ROOM: of numbers that fp32 holds times weights of 448
+// at most, 2^22 of them, every sum is then less than 2^(128 + 8.9 + 22 - 32), finite.  fp32's smallest step makes them multiples of
+// 2^(ROOM - 149) of that largest power; the activations' power itself is exact down to 2^(ROOM - 149).
+constexpr int ROOM = 32;
+__device__ __forceinline__ float power_with_room(uint32_t byte) { return __uint_as_float(byte << 23) * (1.0f / (float)(1ll << ROOM)); }
+// What the sums are multiplied by at the end: 2^(top - 127 + ROOM), one multiplication that rounds; where that is no fp32 number, by
+// the rest of it before the other (of two that are 1 and more the first passes fp32's end only if both do).
 __device__ __forceinline__ f32x4 with_tops(const f32x4 &v, uint32_t tops) {
   f32x4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = v[i] * __uint_as_float(byte_of(tops, i) << 23) * (float)(1 << ROOM);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t e = byte_of(tops, i) + ROOM, most = min(e, 254u);
+    r[i] = v[i] * __uint_as_float((e - most + 127u) << 23) * __uint_as_float(most << 23);
+  }
   return r;
 }
 

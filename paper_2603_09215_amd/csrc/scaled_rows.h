@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {
     const bool unsure = odd | (middle < 16u) | (small < 0x217fffffu) | (low < 0x357fffffu) | (high > 0x53800000u);
     if (__any(unsure)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) n[i] = for_rounding((double)vv[i] * inv * (double)g[i]);
+      for (int i = 0; i < 8; ++i) n[i] = c0 + i < k ? for_rounding((double)vv[i] * inv * (double)g[i]) : 0.f;   // (zeros times a NaN behind a row's end are zeros)
     }
     uint32_t byte;
     const uint2 c = block_codes(n, byte);   // (a block's sixteen lanes are all inside the padded row, or none)

@@ -354,7 +354,8 @@ int spark_scaled_rows(const void *x, int32_t dtype, int64_t stride, int32_t m, i
 
 /* The residual's addition and the RMSNorm behind it: h' = h + y, rounded once to h's type and written to
  * h_out (which may be h itself), then the 8-bit rows of h' / sqrt(mean h'^2 + eps) * gain, worked out in
- * 64 bits, so that every code is the one this formula gives.  h, h_out [m][k] of h_dtype; y [m][k] of
+ * 64 bits, so that every code is the one this formula gives, past fp32's range too (more than the format's
+ * largest number, 448 * 2^127, becomes that).  h, h_out [m][k] of h_dtype; y [m][k] of
  * y_dtype, or NULL: h' = h; gain fp32 [k]; eps >= 0 (a row of zeros with eps 0 gives NaN codes). */
 int spark_scaled_norm(const void *h, int32_t h_dtype, int64_t h_stride, const void *y, int32_t y_dtype,
                       int64_t y_stride, void *h_out, int64_t out_stride, const float *gain, double eps, int32_t m,

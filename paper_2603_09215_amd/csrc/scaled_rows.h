@@ -301,15 +301,34 @@ __global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {
       high = max(high, size);
     }
     const bool unsure = odd | (middle < 16u) | (small < 0x217fffffu) | (low < 0x357fffffu) | (high > 0x53800000u);
+    uint32_t lift = 0u;   // of the block's power
     if (__any(unsure)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) n[i] = c0 + i < k ? for_rounding((double)vv[i] * inv * (double)g[i]) : 0.f;   // (zeros times a NaN behind a row's end are zeros)
+      for (int i = 0; i < 8; ++i) n[i] = for_rounding((double)vv[i] * inv * (double)g[i]);
+      // (a norm is at most sqrt(k) times its gain, and k 2^22)
+      if (__builtin_expect(__any(high >= 0x79800000u), 0)) {   // blocks that pass fp32's range: 2^-64 of them, of the format's largest number at most
+        double d[8];
+        bool far = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          d[i] = (double)vv[i] * inv * (double)g[i];
+          far |= fabs(d[i]) >= 0x1p127 && fabs(d[i]) < __builtin_inf();
+        }
+        lift = max_of_16(far) ? 64u : 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (lift) n[i] = for_rounding((fabs(d[i]) < __builtin_inf() ? fmin(fmax(d[i], -0x1.cp135), 0x1.cp135) : d[i]) * 0x1p-64);
+      }
+      if (__builtin_expect(odd, 0)) {   // a root that is no number: zeros behind the row's end all the same
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] = c0 + i < k ? n[i] : 0.f;
+      }
     }
     uint32_t byte;
     const uint2 c = block_codes(n, byte);   // (a block's sixteen lanes are all inside the padded row, or none)
     if (c0 < kp) {
       *(uint2 *)(a.codes + r * kp + c0) = c;
-      if ((threadIdx.x & 15) == 0) a.powers[r * pitch + c0 / SR_BLOCK] = (uint8_t)byte;
+      if ((threadIdx.x & 15) == 0) a.powers[r * pitch + c0 / SR_BLOCK] = (uint8_t)(byte + lift);
     }
   };
   if constexpr (S > 0) {

@@ -18,6 +18,7 @@ import torch
 from .binding import SparkError, load_library
 
 BLOCK = 128
+LONGEST, MOST_ROWS = 1 << 22, (1 << 31) - 1   # of a row; of the calls, whose sizes are 32-bit numbers (ctypes would cut larger ones)
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -29,6 +30,11 @@ def _padded(k: int) -> tuple[int, int]:
     """codes and powers of a row of k values"""
     blocks = -(-k // BLOCK)
     return blocks * BLOCK, -(-blocks // 4) * 4
+
+
+def _size(what: str, m: int, k: int):
+    if not (0 <= m <= MOST_ROWS and 1 <= k <= LONGEST):
+        _refuse(f"{what}: {m} x {k}, and up to {MOST_ROWS} rows of 1 to {LONGEST} values are taken")
 
 
 def _matrix(t, what: str, shape=None):
@@ -44,9 +50,10 @@ def _matrix(t, what: str, shape=None):
         _refuse(f"{what}: a 2-d fp32 or bf16 tensor on the GPU is wanted")
     if shape is not None and (m, k) != shape:
         _refuse(f"{what} is {m} x {k}, {shape[0]} x {shape[1]} is wanted")
+    _size(what, m, k)
     if m <= 1 and stride < k:
         stride = k              # (of a single row torch may say anything)
-    if k < 1 or (step != 1 and k > 1) or stride < k:
+    if (step != 1 and k > 1) or stride < k:
         _refuse(f"{what}: the elements of a row must lie next to each other, and rows apart")
     return t.data_ptr(), code, stride
 
@@ -73,7 +80,8 @@ class ScaledRows:
     __slots__ = ("codes", "scales", "m", "k")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, k: int):
-        if codes.dim() != 2 or scales.dim() != 2 or k < 1 or codes.shape[0] != scales.shape[0] or \
+        _size("8-bit rows", codes.shape[0] if codes.dim() else 0, k)
+        if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0] or \
                 (codes.shape[1], scales.shape[1]) != _padded(k) or codes.dtype != torch.float8_e4m3fn or \
                 scales.dtype != torch.float8_e8m0fnu or not codes.is_contiguous() or not scales.is_contiguous():
             _refuse("codes and scales do not make 8-bit rows")
@@ -83,8 +91,7 @@ class ScaledRows:
 
     @classmethod
     def empty(cls, m: int, k: int, device="cuda") -> "ScaledRows":
-        if m < 0 or k < 1:
-            _refuse(f"8-bit rows of {m} x {k}")
+        _size("8-bit rows", m, k)
         kp, pitch = _padded(k)
         return cls(torch.empty(m, kp, dtype=torch.float8_e4m3fn, device=device),
                    torch.empty(m, pitch, dtype=torch.float8_e8m0fnu, device=device), k)
@@ -129,6 +136,7 @@ class ScaledWeights:
         """of a product with m rows"""
         need = self._workspace.get(m)
         if need is None:
+            _size("a product's rows", m, self.k)
             size = C.c_size_t()
             with torch.cuda.device(self.packed.device):
                 if load_library().spark_scaled_workspace_bytes(m, self.n, self.k, int(self.pair), C.byref(size)):

@@ -7,13 +7,15 @@
 
 Every call runs on the current stream of its tensors' device, allocates its results unless they are given
 (`out`), and raises SparkError with nothing launched where a tensor does not fit.  There is no fallback: the
-work is done by libspark.so's kernels.
+work is done by libspark.so's kernels.  The operators have no derivatives: a tensor that a gradient or tangent is wanted
+of is refused (detach it, or call them under torch.no_grad()), and a tensor that they write counts as changed in place.
 """
 from __future__ import annotations
 
 import ctypes as C
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import SparkError, load_library
 
@@ -38,7 +40,7 @@ def _size(what: str, m: int, k: int):
 
 
 def _matrix(t, what: str, shape=None):
-    """(address, type, stride) of a 2-d device tensor of a type the kernels read, rows contiguous"""
+    """(address, type, stride, rows, row's length) of a 2-d device tensor of a type the kernels read, rows contiguous"""
     try:
         code = _DTYPE[t.dtype]
         m, k = t.shape
@@ -50,20 +52,35 @@ def _matrix(t, what: str, shape=None):
         _refuse(f"{what}: a 2-d fp32 or bf16 tensor on the GPU is wanted")
     if shape is not None and (m, k) != shape:
         _refuse(f"{what} is {m} x {k}, {shape[0]} x {shape[1]} is wanted")
-    _size(what, m, k)
+    if m > MOST_ROWS or not 1 <= k <= LONGEST:
+        _size(what, m, k)
     if m <= 1 and stride < k:
         stride = k              # (of a single row torch may say anything)
     if (step != 1 and k > 1) or stride < k:
         _refuse(f"{what}: the elements of a row must lie next to each other, and rows apart")
-    return t.data_ptr(), code, stride
+    return t.data_ptr(), code, stride, m, k
 
 
-def _launch(what: str, tensors, call, *args):
-    """call(*args, stream) with the tensors' (the first is one, others may be None) device current and on its current stream"""
+def _no_gradient(*tensors):
+    """nothing may pass whose gradient or tangent would be lost without a word"""
+    dual = forward_ad._current_level >= 0   # (outside a level of forward mode there are no tangents)
+    for t in tensors:
+        if t is not None and ((t.requires_grad and torch.is_grad_enabled()) or (dual and forward_ad.unpack_dual(t).tangent is not None)):
+            _refuse("the operators on 8-bit rows have no derivatives, and a gradient or tangent of a tensor is wanted")
+
+
+def _launch(what: str, tensors, written, call, *args):
+    """call(*args, stream) with the tensors' (the first is one, others may be None) device current and on its current stream;
+    `written`: those given tensors that it changes"""
     dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.get_device() != dev:
-            _refuse("the tensors are on different devices")
+        if t is not None:
+            if t.get_device() != dev:
+                _refuse("the tensors are on different devices")
+            if t.requires_grad:
+                _no_gradient(t)
+    if forward_ad._current_level >= 0:
+        _no_gradient(*tensors)
     # (the raw handle: torch.cuda.current_stream() takes 3 us, the smallest launches here 2)
     if dev == torch._C._cuda_getDevice():
         rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
@@ -72,6 +89,8 @@ def _launch(what: str, tensors, call, *args):
             rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         raise SparkError(rc, what + " was refused or failed")
+    if written:   # (torch.autograd.graph.increment_version without its checks: half a call's 0.4 us)
+        torch._C._increment_version(written)
 
 
 class ScaledRows:
@@ -87,6 +106,7 @@ class ScaledRows:
             _refuse("codes and scales do not make 8-bit rows")
         if codes.device.type != "cuda" or codes.device != scales.device:
             _refuse("8-bit rows: both tensors on one GPU are wanted")
+        _no_gradient(codes, scales)
         self.codes, self.scales, self.m, self.k = codes, scales, codes.shape[0], k
 
     @classmethod
@@ -103,12 +123,13 @@ class ScaledRows:
         return v.view(self.m, blocks * BLOCK)[:, :self.k]
 
 
-def _rows_out(out, m: int, k: int, device) -> ScaledRows:
+def _rows_out(out, m: int, k: int, device):
+    """(the rows to write, those of its tensors that were given)"""
     if out is None:
-        return ScaledRows.empty(m, k, device)
+        return ScaledRows.empty(m, k, device), ()
     if out.m != m or out.k != k:
         _refuse(f"out holds {out.m} x {out.k} values, {m} x {k} are written")
-    return out
+    return out, (out.codes, out.scales)
 
 
 class ScaledWeights:
@@ -116,19 +137,18 @@ class ScaledWeights:
     order the matrix instructions take them."""
 
     def __init__(self, w: torch.Tensor, up: torch.Tensor | None = None):
-        at, code, stride = _matrix(w, "w")
-        self.n, self.k = w.shape
+        at, code, stride, self.n, self.k = _matrix(w, "w")
         self.pair = up is not None
         up_at = None
         if self.pair:
-            up_at, up_code, up_stride = _matrix(up, "up", (self.n, self.k))
+            up_at, up_code, up_stride, _, _ = _matrix(up, "up", (self.n, self.k))
             if (up_code, up_stride) != (code, stride):
                 _refuse("up must have w's type and stride")
         lib, size = load_library(), C.c_size_t()
         if lib.spark_scaled_weight_bytes(self.n, self.k, int(self.pair), C.byref(size)):
             _refuse(f"weights of {self.n} x {self.k}")
         self.packed = torch.empty(size.value, dtype=torch.uint8, device=w.device)
-        _launch("packing the weights", (w, up), lib.spark_scaled_pack, at, up_at, code, stride, self.n, self.k,
+        _launch("packing the weights", (w, up), None, lib.spark_scaled_pack, at, up_at, code, stride, self.n, self.k,
                 self.packed.data_ptr(), size.value)
         self._workspace = {}   # rows -> bytes
 
@@ -155,11 +175,10 @@ class ScaledWeights:
 
 def scaled_rows(x: torch.Tensor, out: ScaledRows | None = None) -> ScaledRows:
     """x [m][k], fp32 or bf16, as 8-bit rows"""
-    at, code, stride = _matrix(x, "x")
-    m, k = x.shape
-    out = _rows_out(out, m, k, x.device)
+    at, code, stride, m, k = _matrix(x, "x")
+    out, given = _rows_out(out, m, k, x.device)
     if m:
-        _launch("scaled_rows", (x, out.codes), load_library().spark_scaled_rows, at, code, stride, m, k, out.codes.data_ptr(),
+        _launch("scaled_rows", (x, out.codes), given, load_library().spark_scaled_rows, at, code, stride, m, k, out.codes.data_ptr(),
                 out.scales.data_ptr())
     return out
 
@@ -168,19 +187,18 @@ def scaled_norm(h: torch.Tensor, gain: torch.Tensor, eps: float, y: torch.Tensor
                 h_out: torch.Tensor | None = None, out: ScaledRows | None = None) -> ScaledRows:
     """h' = h + y (in h's type, written to h_out, or to h where none is given), then the 8-bit rows of
     h' / sqrt(mean h'^2 + eps) * gain.  h, y, h_out [m][k] fp32 or bf16, gain fp32 [k]."""
-    at, code, stride = _matrix(h, "h")
-    shape = m, k = tuple(h.shape)
-    y_at, y_code, y_stride = (None, 0, 0) if y is None else _matrix(y, "y", shape)
-    out_at, out_code, out_stride = (at, code, stride) if h_out is None else _matrix(h_out, "h_out", shape)
+    at, code, stride, m, k = _matrix(h, "h")
+    y_at, y_code, y_stride, _, _ = (None, 0, 0, m, k) if y is None else _matrix(y, "y", (m, k))
+    out_at, out_code, out_stride, _, _ = (at, code, stride, m, k) if h_out is None else _matrix(h_out, "h_out", (m, k))
     if out_code != code:
         _refuse("h_out must have h's type")
     if gain.dtype != torch.float32 or gain.shape != (k,) or not gain.is_contiguous():
         _refuse(f"gain: fp32 [{k}] is wanted")
     if not eps >= 0.0:
         _refuse("eps must not be negative")
-    out = _rows_out(out, m, k, h.device)
+    out, given = _rows_out(out, m, k, h.device)
     if m:
-        _launch("scaled_norm", (h, y, h_out, gain, out.codes), load_library().spark_scaled_norm, at, code, stride,
+        _launch("scaled_norm", (h, y, h_out, gain, out.codes), (h if h_out is None else h_out, *given), load_library().spark_scaled_norm, at, code, stride,
                 y_at, y_code, y_stride, out_at, out_stride, gain.data_ptr(), eps, m, k, out.codes.data_ptr(), out.scales.data_ptr())
     return out
 
@@ -189,14 +207,15 @@ def scaled_matmul(x: ScaledRows, w: ScaledWeights, out: torch.Tensor | None = No
     """x W^T, [m][n] of `dtype` (fp32 or bf16; out's, where it is given)"""
     if w.pair or x.k != w.k:
         _refuse(f"rows of {x.k} and {'a pair of matrices' if w.pair else 'weights'} of {w.k}")
+    given = None if out is None else (out,)
     if out is None:
         if dtype not in _DTYPE:
             _refuse("dtype: fp32 or bf16 is wanted")
         out = torch.empty(x.m, w.n, dtype=dtype, device=x.codes.device)
-    at, code, stride = _matrix(out, "out", (x.m, w.n))
+    at, code, stride, _, _ = _matrix(out, "out", (x.m, w.n))
     if x.m:
         keep, ws, need = w.workspace(x.m)
-        _launch("scaled_matmul", (x.codes, w.packed, out), load_library().spark_scaled_matmul, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
+        _launch("scaled_matmul", (x.codes, w.packed, out), given, load_library().spark_scaled_matmul, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
                 w.packed.data_ptr(), w.n, w.k, at, code, stride, ws, need)
     return out
 
@@ -205,11 +224,11 @@ def scaled_gated(x: ScaledRows, w: ScaledWeights, out: ScaledRows | None = None)
     """silu(x Wg^T) * (x Wu^T) as 8-bit rows [m][n]; w: a pair"""
     if not w.pair or x.k != w.k:
         _refuse(f"rows of {x.k} and {'a pair' if w.pair else 'one matrix'} of {w.k}: a pair of gate and up is wanted")
-    out = _rows_out(out, x.m, w.n, x.codes.device)
+    out, given = _rows_out(out, x.m, w.n, x.codes.device)
     if x.m:
         if out.codes.data_ptr() == x.codes.data_ptr():
             _refuse("out must not be x")
         keep, ws, need = w.workspace(x.m)
-        _launch("scaled_gated", (x.codes, w.packed, out.codes), load_library().spark_scaled_gated, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
+        _launch("scaled_gated", (x.codes, w.packed, out.codes), given, load_library().spark_scaled_gated, x.codes.data_ptr(), x.scales.data_ptr(), x.m,
                 w.packed.data_ptr(), w.n, w.k, out.codes.data_ptr(), out.scales.data_ptr(), ws, need)
     return out

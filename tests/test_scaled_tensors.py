@@ -54,3 +54,41 @@ def test_rows_past_32_bits():
     for k in ((1 << 32) + 64, 0, (1 << 22) + 1):
         with pytest.raises(SparkError, match="are taken"):
             scaled.ScaledRows(codes, scales, k)
+
+
+def test_gradients_are_refused():
+    """where torch keeps a graph (requires_grad) or tangents; under no_grad a parameter is a tensor as any other"""
+    w = torch.nn.Parameter(torch.ones(4, 64))
+    with pytest.raises(SparkError, match="no derivatives"):
+        scaled._no_gradient(None, torch.ones(3), w)
+    with torch.no_grad():
+        scaled._no_gradient(w)
+    scaled._no_gradient(w.detach(), None)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(torch.ones(4, 64), torch.ones(4, 64))
+        with pytest.raises(SparkError, match="no derivatives"):
+            scaled._no_gradient(dual)
+        scaled._no_gradient(torch.ones(4, 64))
+        with torch.no_grad(), pytest.raises(SparkError, match="no derivatives"):
+            scaled._no_gradient(dual)
+
+
+def test_every_launch_looks_for_gradients():
+    """before anything is called, on the first tensor or another"""
+    class On:
+        requires_grad = False
+
+        def get_device(self):
+            return 0
+
+    class Wanted(torch.Tensor):
+        def get_device(self):
+            return 0
+
+    def never(*args):
+        raise AssertionError("called")
+
+    w = torch.ones(3).as_subclass(Wanted).requires_grad_()
+    for tensors in ((w,), (On(), None, w)):
+        with pytest.raises(SparkError, match="no derivatives"):
+            scaled._launch("x", tensors, None, never)

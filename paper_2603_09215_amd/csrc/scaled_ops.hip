@@ -6,6 +6,7 @@
 
 #include "../../include/spark.h"
 #include "scaled_gemm.h"
+#include "scaled_plan.h"
 
 namespace spark {
 namespace {
@@ -56,43 +57,9 @@ template <typename OUT> void stream_launch(const GemmArgs &a, hipStream_t stream
   else scaled_stream_k<false, OUT><<<grid, 64 * nw * kw, sums, stream>>>(a, nw, kw);
 }
 
-// Tiles: their size, and into how many parts k is cut.  All have eight waves along the outputs (a row block's codes go to
-// one wave), of one or two row blocks each, and as many operands of 16 rows as there are rows or registers.
-struct TilePlan { int shape, splits; };
-struct TileShape { int nt, mt; float us_fp32, us_8bit; };   // us: of a k block, where the matrix instructions and conversions take the time
 constexpr int TILES_MOST = 1 << 20;   // of a launch
-constexpr TileShape TILE_SHAPES[] = {{1, 2, 0.39f, 0.41f}, {1, 4, 0.61f, 0.41f}, {2, 1, 0.44f, 0.38f}, {2, 2, 0.62f, 0.58f}, {2, 4, 0.95f, 0.67f}, {2, 8, 1.66f, 0.92f}};
 size_t lds_of(int tm, bool fp32, bool gated) {
   return std::max((size_t)(fp32 ? 4 : 2) * tm * SW_TILE + 4 * 512 * sizeof(uint32_t), gated ? sizeof(float) * 16 * tm * (SR_BLOCK + 4) : 0);
-}
-
-// The plan whose estimate is shortest.  A tile's k block takes its arithmetic or its weights' way from memory, of which a CU
-// gets 42 GB/s at most and all of them 6.3 TB/s (rows of tiles behind the first read them from L2); tiles go in rounds of one
-// per CU; parts are written and read once more, by a launch of its own.  In us beyond a launch's own, fitted to 178 sweeps of all
-// shapes and cuts (1 to 2048 rows, the projections of both backbones and 1000 x 1000, both types): the choice is 0.3 % above the
-// best of a sweep on average, 7 % at most; one shape for each number of rows, k cut until every CU has a tile, was 4 % above it,
-// 35 % at most.
-TilePlan tile_plan(int m, int row_blocks, int k, bool pair, bool fp32, int n_cu) {
-  TilePlan best{0, 1};
-  float best_us = 1e30f;
-  const int groups = sr_pitch(k) / 4, blocks = sr_blocks(k);
-  for (int i = 0; i < (int)(sizeof(TILE_SHAPES) / sizeof(TILE_SHAPES[0])); ++i) {
-    const TileShape &t = TILE_SHAPES[i];
-    if (pair ? t.nt != 2 : i == 2) continue;   // (gate and partner belong to one wave; of single matrices the third shape was best at 8 sizes of 3276)
-    if (t.mt > 1 && 8 * t.mt >= m) continue;   // (half of the tile's rows would do)
-    const long long tiles = (long long)((row_blocks + t.nt * TILE_WAVES - 1) / (t.nt * TILE_WAVES)) * ((m - 1) / (16 * t.mt) + 1);
-    for (int splits = 1; splits <= groups && (splits == 1 || tiles * splits <= 2ll * n_cu); ++splits) {
-      const long long wgs = tiles * splits;
-      const float active = (float)std::min<long long>(wgs, n_cu), rounds = (float)((wgs + n_cu - 1) / n_cu);
-      const float bytes = (float)(t.nt * TILE_WAVES * SW_TILE), weights = (float)row_blocks * blocks * SW_TILE;
-      const float way = std::max(bytes / 42.3e3f, bytes * active / 6.32e6f);
-      const float kbs = (float)std::min(blocks, 4 * ((groups + splits - 1) / splits));
-      float us = rounds * (0.11f + kbs * std::max(fp32 ? t.us_fp32 : t.us_8bit, std::min(way, weights * 1.52f / 6.32e6f / (rounds * kbs))));
-      if (splits > 1) us += 2.4f + (splits + 1.1f) * (float)m * row_blocks * 64.0f / 3.83e6f;
-      if (us < best_us) { best_us = us; best = TilePlan{i, splits}; }
-    }
-  }
-  return best;
 }
 
 template <bool FP32, TileEnd END, typename OUT> void tile_launch(GemmArgs a, const TilePlan &p, hipStream_t stream) {

@@ -22,6 +22,9 @@ from .binding import SparkError, load_library
 BLOCK = 128
 LONGEST, MOST_ROWS = 1 << 22, (1 << 31) - 1   # of a row; of the calls, whose sizes are 32-bit numbers (ctypes would cut larger ones)
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1}
+# The current device, its current stream's raw handle, and the versions of tensors that were written: torch.cuda.current_stream() and
+# torch.autograd.graph.increment_version() take 3 and 0.4 us, the smallest launches here 2.
+_device, _stream, _changed = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._increment_version
 
 
 def _refuse(why: str):
@@ -81,16 +84,15 @@ def _launch(what: str, tensors, written, call, *args):
                 _no_gradient(t)
     if forward_ad._current_level >= 0:
         _no_gradient(*tensors)
-    # (the raw handle: torch.cuda.current_stream() takes 3 us, the smallest launches here 2)
-    if dev == torch._C._cuda_getDevice():
-        rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if dev == _device():
+        rc = call(*args, _stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = call(*args, torch._C._cuda_getCurrentRawStream(dev))
+            rc = call(*args, _stream(dev))
     if rc:
         raise SparkError(rc, what + " was refused or failed")
-    if written:   # (torch.autograd.graph.increment_version without its checks: half a call's 0.4 us)
-        torch._C._increment_version(written)
+    if written:
+        _changed(written)
 
 
 class ScaledRows:
@@ -123,10 +125,10 @@ class ScaledRows:
         return v.view(self.m, blocks * BLOCK)[:, :self.k]
 
 
-def _rows_out(out, m: int, k: int, device):
-    """(the rows to write, those of its tensors that were given)"""
+def _rows_out(out, m: int, k: int, like):
+    """(the rows to write, beside `like`; those of its tensors that were given)"""
     if out is None:
-        return ScaledRows.empty(m, k, device), ()
+        return ScaledRows.empty(m, k, like.device), ()
     if out.m != m or out.k != k:
         _refuse(f"out holds {out.m} x {out.k} values, {m} x {k} are written")
     return out, (out.codes, out.scales)
@@ -166,7 +168,9 @@ class ScaledWeights:
 
     def workspace(self, m: int):
         """(tensor or None, its address, its bytes) for one call; torch's allocator hands it on in stream order"""
-        need = self.workspace_bytes(m)
+        need = self._workspace.get(m)
+        if need is None:
+            need = self.workspace_bytes(m)
         if not need:
             return None, None, 0
         t = torch.empty(need, dtype=torch.uint8, device=self.packed.device)
@@ -176,7 +180,7 @@ class ScaledWeights:
 def scaled_rows(x: torch.Tensor, out: ScaledRows | None = None) -> ScaledRows:
     """x [m][k], fp32 or bf16, as 8-bit rows"""
     at, code, stride, m, k = _matrix(x, "x")
-    out, given = _rows_out(out, m, k, x.device)
+    out, given = _rows_out(out, m, k, x)
     if m:
         _launch("scaled_rows", (x, out.codes), given, load_library().spark_scaled_rows, at, code, stride, m, k, out.codes.data_ptr(),
                 out.scales.data_ptr())
@@ -192,11 +196,11 @@ def scaled_norm(h: torch.Tensor, gain: torch.Tensor, eps: float, y: torch.Tensor
     out_at, out_code, out_stride, _, _ = (at, code, stride, m, k) if h_out is None else _matrix(h_out, "h_out", (m, k))
     if out_code != code:
         _refuse("h_out must have h's type")
-    if gain.dtype != torch.float32 or gain.shape != (k,) or not gain.is_contiguous():
+    if gain.dtype is not torch.float32 or gain.dim() != 1 or gain.numel() != k or not gain.is_contiguous():
         _refuse(f"gain: fp32 [{k}] is wanted")
     if not eps >= 0.0:
         _refuse("eps must not be negative")
-    out, given = _rows_out(out, m, k, h.device)
+    out, given = _rows_out(out, m, k, h)
     if m:
         _launch("scaled_norm", (h, y, h_out, gain, out.codes), (h if h_out is None else h_out, *given), load_library().spark_scaled_norm, at, code, stride,
                 y_at, y_code, y_stride, out_at, out_stride, gain.data_ptr(), eps, m, k, out.codes.data_ptr(), out.scales.data_ptr())
@@ -224,7 +228,7 @@ def scaled_gated(x: ScaledRows, w: ScaledWeights, out: ScaledRows | None = None)
     """silu(x Wg^T) * (x Wu^T) as 8-bit rows [m][n]; w: a pair"""
     if not w.pair or x.k != w.k:
         _refuse(f"rows of {x.k} and {'a pair' if w.pair else 'one matrix'} of {w.k}: a pair of gate and up is wanted")
-    out, given = _rows_out(out, x.m, w.n, x.codes.device)
+    out, given = _rows_out(out, x.m, w.n, x.codes)
     if x.m:
         if out.codes.data_ptr() == x.codes.data_ptr():
             _refuse("out must not be x")

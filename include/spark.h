@@ -335,7 +335,7 @@ int spark_tune(spark_ctx *ctx, const char *name, int32_t value);
  * 8-bit rows: m rows of k values are `codes`, uint8 [m][kp] of e4m3 numbers (4 exponent, 3 fraction
  * bits, largest 448, no infinities), kp = k rounded up to a multiple of 128, zeros behind k; and
  * `powers`, uint8 [m][pitch], pitch = kp / 128 rounded up to a multiple of 4: a byte b for every 128
- * codes of a row, which stand for code * 2^(b - 127); 127 behind kp / 128.  The power is the smallest
+ * codes of a row, 1 to 254, which stand for code * 2^(b - 127); 127 behind kp / 128.  The power is the smallest
  * of 2^-126 and up for which no magnitude of the block passes 448 (a block of zeros: 2^0); values are
  * rounded to the nearest code, half to even.  A NaN or infinity becomes e4m3's NaN and has no part in
  * the block's power.  codes 16-byte, powers 4-byte aligned.
@@ -401,8 +401,10 @@ int spark_scaled_gated(const void *codes, const void *powers, int32_t m, const v
  * the rows that a projection reads are 8-bit rows, and passes of more than 64 rows hand its sums on in
  * bf16.  The results are those of a model whose projections have 8-bit weights and inputs, not those of the bf16
  * model.  May be called between any two calls, cached keys and values stay; NULL goes back to the caller's weights.
+ * The buffer comes on top of what a context holds: the caller's weights stay in use (embedding, heads), and prompts go in passes
+ * of more than 256 rows only in a context with room for its fp16 copy of the weights, which the 8-bit passes themselves do not read.
  * Returns when the weights are packed.  SPARK_EINVAL: an fp32 model; SPARK_ENOMEM: buffer too small or misaligned (the
- * context goes on as before in both). */
+ * context goes on as before in both); SPARK_EHIP: packing failed, the layers run on the caller's weights. */
 int spark_scaled_model_bytes(const spark_config *cfg, size_t *bytes);
 int spark_scaled_projections(spark_ctx *ctx, void *buffer, size_t bytes);
 

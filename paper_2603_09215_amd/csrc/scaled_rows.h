@@ -186,7 +186,7 @@ __device__ __forceinline__ double inverse_root(double x) {
 }
 
 // x [m][k] -> 8-bit rows.  Sixteen lanes a block, U blocks at a time; blocks of all rows in one sequence (2^27 at most).
-// Bound by memory: 8191 x 4096 bf16 in 21.7 us, 4.6 TB/s (a copy: 5.2); 32 x 3584 fp32 in 1.9 us, a launch's own time.
+// Bound by memory: 8191 x 4096 bf16 in 22.2 us, 4.5 TB/s (a copy: 5.2); 32 x 3584 fp32 in 2.4 us, a launch's own time.
 template <typename T, bool VEC, int U>
 __global__ void __launch_bounds__(256)
 scaled_rows_k(const T *__restrict__ x, long long stride, unsigned total, int k, uint8_t *__restrict__ codes, uint8_t *__restrict__ powers) {
@@ -221,9 +221,10 @@ scaled_rows_k(const T *__restrict__ x, long long stride, unsigned total, int k, 
 // h' = h + y (rounded to h's type; y absent: h' = h), v = h' / sqrt(mean h'^2 + eps) * gain -> 8-bit rows.
 // In 64 bits from the sum of squares to the code: that is what makes every code the one that the formula gives, whatever
 // the order of the sum; where fp32 settles the code (below) it stands in.  4096 x 4096 bf16 takes 25 us (4.7 TB/s; instructions
-// and memory about level), fp32 37 us (5.0 TB/s), 1023 x 4096 fp32 14 us, 2048 x 18944 fp32 106 us (4.8 TB/s), one row 3.2 us.
+// and memory about level), fp32 with y in bf16 37 us (5.0 TB/s); with both in fp32 1023 x 4096 14 us, 2048 x 18944 112 us
+// (4.5 TB/s), one row 3.0 us.
 // One workgroup a row, of MOST threads at most; a thread has S times eight values in registers.  S == 0: a row of any length,
-// read a second time for the codes (from L2: 2048 x 18944 in 106 us; four times eight a thread, 640 threads: 121).  Workgroups that
+// read a second time for the codes (from L2: 2048 x 18944 in 112 us; four times eight a thread, 640 threads: 121).  Workgroups that
 // stay and fetch their next row ahead take as long (4096 x 4096 bf16 31 us, 1023 rows 15), and so do rows dealt to the XCDs in runs.
 template <typename T, typename Y, bool HAS_Y, bool VEC, int MOST, int S>
 __global__ void __launch_bounds__(MOST) scaled_norm_k(NormArgs a) {

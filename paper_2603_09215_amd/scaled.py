@@ -202,7 +202,9 @@ def scaled_norm(h: torch.Tensor, gain: torch.Tensor, eps: float, y: torch.Tensor
         _refuse("eps must not be negative")
     out, given = _rows_out(out, m, k, h)
     if m:
-        _launch("scaled_norm", (h, y, h_out, gain, out.codes), (h if h_out is None else h_out, *given), load_library().spark_scaled_norm, at, code, stride,
+        if y is not None or out_at != at:   # (otherwise h' is h, where it lies)
+            given = (h if h_out is None else h_out, *given)
+        _launch("scaled_norm", (h, y, h_out, gain, out.codes), given, load_library().spark_scaled_norm, at, code, stride,
                 y_at, y_code, y_stride, out_at, out_stride, gain.data_ptr(), eps, m, k, out.codes.data_ptr(), out.scales.data_ptr())
     return out
 

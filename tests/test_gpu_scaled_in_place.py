@@ -20,6 +20,10 @@ def test_a_backward_pass_over_a_changed_stream_is_refused(ops):   # noqa: F811
     ops.scaled_norm(h, gain, 1e-6, y=torch.ones_like(h), h_out=out)   # h stays as it is
     loss.backward()
     assert torch.equal(w.grad, h.sum(0))
+    w.grad, loss = None, (h * w).sum()
+    ops.scaled_norm(h, gain, 1e-6)                                    # nothing is added to it: h stays too
+    loss.backward()
+    assert torch.equal(w.grad, h.sum(0))
 
 
 def test_versions_of_what_is_written(ops):   # noqa: F811
@@ -28,7 +32,9 @@ def test_versions_of_what_is_written(ops):   # noqa: F811
     w, pair, out = ops.ScaledWeights(weights(100, 256, 1).cuda()), ops.ScaledWeights(weights(100, 256, 2).cuda(), weights(100, 256, 3).cuda()), torch.empty(4, 100, device="cuda")
     for call, written, read in ((lambda: ops.scaled_rows(x, out=rows), (rows.codes, rows.scales), (x,)),
                                 (lambda: ops.scaled_norm(x, gain, 1e-6, h_out=h_out, out=rows), (h_out, rows.codes, rows.scales), (x, gain)),
-                                (lambda: ops.scaled_norm(x, gain, 1e-6), (x,), (gain,)),
+                                (lambda: ops.scaled_norm(x, gain, 1e-6, y=h_out), (x,), (gain, h_out)),
+                                (lambda: ops.scaled_norm(x, gain, 1e-6), (), (x, gain)),               # (nothing is added: x stays)
+                                (lambda: ops.scaled_norm(x, gain, 1e-6, h_out=x, out=rows), (rows.codes, rows.scales), (x, gain)),
                                 (lambda: ops.scaled_matmul(rows, w, out=out), (out,), (rows.codes, rows.scales)),
                                 (lambda: ops.scaled_gated(rows, pair, out=act), (act.codes, act.scales), (rows.codes, rows.scales))):
         before = [t._version for t in (*written, *read)]

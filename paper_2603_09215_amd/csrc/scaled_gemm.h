@@ -73,15 +73,11 @@ __device__ __forceinline__ float power_below(uint32_t byte, uint32_t top) { retu
 // 2^(ROOM - 149) of that largest power; the activations' power itself is exact down to 2^(ROOM - 149).
 constexpr int ROOM = 32;
 __device__ __forceinline__ float power_with_room(uint32_t byte) { return __uint_as_float(byte << 23) * (1.0f / (float)(1ll << ROOM)); }
-// What the sums are multiplied by at the end: 2^(top - 127 + ROOM), one multiplication that rounds; where that is no fp32 number, by
-// the rest of it before the other (of two that are 1 and more the first passes fp32's end only if both do).
+// at the end the sums times 2^(top - 127 + ROOM), rounded once; that may be no fp32 number, so it is added to their exponents
 __device__ __forceinline__ f32x4 with_tops(const f32x4 &v, uint32_t tops) {
   f32x4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t e = byte_of(tops, i) + ROOM, most = min(e, 254u);
-    r[i] = v[i] * __uint_as_float((e - most + 127u) << 23) * __uint_as_float(most << 23);
-  }
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(v[i], (int)byte_of(tops, i) + (ROOM - 127));
   return r;
 }
 

@@ -151,8 +151,8 @@ template <bool FP32> __device__ __forceinline__ void add_block(f32x4 &acc, const
 // out = X W^T, up to 16 rows.  A workgroup has nw row blocks, kw waves each, which share k; their sums meet in
 // LDS, added in order.  IN_LDS: the rows' codes lie in LDS, fetched once for all waves, rows 16 bytes apart beyond their length
 // so that sixteen of them read side by side meet in no bank; otherwise (long rows) each wave reads its part of them itself, a
-// byte beside every byte of the weights.  4608 x 3584: 6.8 us with one row, 9.2 with 16 (floor 2.5, a plain read in the same
-// pieces 4.7); 3584 x 18944: 14.0 us with one (4.9 TB/s; 224 of 256 CUs have a row block), 18.2 with 16.
+// byte beside every byte of the weights.  4608 x 3584: 6.7 us with one row, 9.2 with 16 (floor 2.5, a plain read in the same
+// pieces 4.7); 3584 x 18944: 14.5 us with one (4.7 TB/s; 224 of 256 CUs have a row block), 18.5 with 16.
 template <bool IN_LDS, typename OUT>
 __global__ void __launch_bounds__(1024) scaled_stream_k(GemmArgs a, int nw, int kw) {
   constexpr bool FP32 = sizeof(OUT) == 4;
@@ -265,13 +265,13 @@ enum TileEnd { TILE_OUT, TILE_GATED, TILE_PARTS };
 // wave; the rows' codes, which all waves share, through LDS in operand order, two buffers, a barrier per k block.  For
 // outputs in fp32 they lie there as fp16, converted once instead of by every wave: twice the LDS, 70 % fewer conversions (2048 rows,
 // a pair of 13696 x 4096: 452 -> 436 us).
-// What it reaches: 2048 x 8192 x 8192 in 147 us with outputs in bf16 (1.87 PFLOP/s), 249 in fp32 (1.10); 1023 x 4096 x 13696
+// What it reaches: 2048 x 8192 x 8192 in 146 us with outputs in bf16 (1.88 PFLOP/s), 246 in fp32 (1.12); 1023 x 4096 x 13696
 // 77 and 115 us.  The matrix units are busy 45 % of the time at the 2.0 GHz the chip then runs at;
 // the rest goes to the tiles' way from L2 through the vector cache (weights fetched by two waves each, four row blocks a
 // wave: bf16 162 -> 197 us) and from LDS.  Two k blocks per barrier and conversions
 // placed between the matrix instructions by hand were all within 2 %.
 // RB = 2: 32 x 3584 x 18944 in 19.1 us, pairs of 24 rows 26.8 and 64 rows 33.9; four blocks ahead 22.0, 27.7 and 36.2, one 20.4, 27.1 and 35.8.
-// Few rows are bound by the weights' way: a pair of 18944 x 3584 with one row 26.1 us, 136 MB (a plain read: 20.4).
+// Few rows are bound by the weights' way: a pair of 18944 x 3584 with one row 26.0 us, 136 MB (a plain read: 20.4).
 constexpr int TILE_WAVES = 8;
 template <int NT, int MT, bool FP32, TileEnd END, typename OUT>
 __global__ void __launch_bounds__(64 * TILE_WAVES) scaled_tile_k(GemmArgs a, int n_tiles, int m_tiles, int splits) {

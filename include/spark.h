@@ -408,6 +408,118 @@ int spark_scaled_gated(const void *codes, const void *powers, int32_t m, const v
 int spark_scaled_model_bytes(const spark_config *cfg, size_t *bytes);
 int spark_scaled_projections(spark_ctx *ctx, void *buffer, size_t bytes);
 
+/* ---- Operators on a paged cache ----------------------------------------------------------------
+ *
+ * What lies between the q/k/v product of a layer and its o product, for programs that keep the cache
+ * themselves: rotation and cache write, attention, the weights that it gave the cached tokens, and eviction by
+ * those.  No context is needed.
+ *
+ * The cache is one [device] tensor laid out as a context's pool is, [page][layer][k|v][kv_head][token in its
+ * page][head_dim].  A batch is n sequences: rows starts[s] .. starts[s + 1] - 1 of the row operands are the new
+ * rows of sequence s, lengths[s] its slots in use, those of the new rows among them, which are its last ones, and
+ * table [n][max_pages] its pages: slot t of sequence s is token t mod page_tokens of page table[s][t / page_tokens].
+ * Row i of the r rows of a sequence of length c has slot c - r + i and sees slots 0 .. c - r + i (causal) or
+ * 0 .. c - 1 (causal 0).  A row whose slot is negative has no place and sees nothing.
+ *
+ * starts, lengths and table are read on the device, by each call anew, and may change between two replays of a
+ * captured graph; m, n and max_pages are the sizes of the row operands, starts (less one), and table.  What they hold is
+ * held to their ranges there: starts ascend and are cut to 0 .. m, lengths to 0 .. max_pages * page_tokens.  A page that is not
+ * 0 .. n_pages - 1 holds nothing: nothing is written there, none of its slots is seen, and zeros are read where
+ * an entry of it is moved.  Rows before starts[0] and from starts[n] on are left as they are, as are slots, weights
+ * and entries behind a sequence's length except where it says so.  Slots that a row does not see have no part in its
+ * result, whatever they hold (infinities and NaN too).
+ *
+ * As for the operators on 8-bit rows: pointers are [device] unless marked, of the current device, on which hip_stream has
+ * to be as well; nothing is allocated, copied or waited for, so the calls may be captured; strides count elements from row to
+ * row and are at least the row's length; m == 0 (but for spark_cache_weigh, whose
+ * sums are then empty) or n == 0 is a call that does nothing; outputs must not overlap
+ * inputs except where it says so, and two sequences must not share pages that a call writes to.  Results are the same bits at every call.
+ * SPARK_EINVAL: a NULL pointer, a size, stride, type or alignment outside the limits (nothing is launched);
+ * SPARK_ENOMEM: workspace too small; SPARK_EHIP: the launch failed. */
+typedef struct spark_cache {
+  uint32_t size;         /* sizeof(spark_cache) */
+  int32_t dtype;         /* SPARK_DTYPE_* */
+  int32_t n_pages;       /* 1 .. 2^24 */
+  int32_t n_layers;      /* 1 .. 2^16 */
+  int32_t n_kv_heads;    /* 1 .. 2^12 */
+  int32_t page_tokens;   /* a multiple of 16, at most 2^16 */
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t layer;         /* the one that a call works on, 0 .. n_layers - 1 */
+  void *pool;            /* 16-byte aligned */
+} spark_cache;
+
+typedef struct spark_cache_batch {
+  uint32_t size;          /* sizeof(spark_cache_batch) */
+  int32_t m;              /* rows of the row operands, up to 2^22 */
+  int32_t n;              /* sequences, up to 2^16 */
+  int32_t max_pages;      /* pages a sequence has at most; slots (times page_tokens) up to 2^24 */
+  const int32_t *starts;  /* [n + 1] */
+  const int32_t *lengths; /* [n] */
+  const int32_t *table;   /* [n][max_pages] */
+} spark_cache_batch;
+
+/* How queries and keys are turned on their way: x / sqrt(mean x^2 + eps) * gain for each head (where its gain is
+ * given), then pairs of its first `rotary` values by angle = position * freqs[j]: (a, b) -> amplitude *
+ * (a cos - b sin, b cos + a sin), the pairs (j, j + rotary / 2), or interleaved (2 j, 2 j + 1).  Angles are worked
+ * out in 64 bits.  A position is its row's slot, or positions[row]. */
+typedef struct spark_rotation {
+  uint32_t size;            /* sizeof(spark_rotation) */
+  int32_t rotary;           /* even, 0 (nothing is turned) .. head_dim */
+  int32_t interleaved;
+  float amplitude;          /* finite */
+  const double *freqs;      /* [rotary / 2], NULL with rotary 0 */
+  const int32_t *positions; /* [m], or NULL */
+  const float *q_gain;      /* [head_dim], or NULL: no norm */
+  const float *k_gain;      /* the same */
+  double eps;               /* >= 0 */
+} spark_rotation;
+
+/* q [m][n_q_heads][head_dim], k and v [m][n_kv_heads][head_dim] of src_dtype, each with its stride, on their way
+ * into the cache: queries turned and rounded once to the cache's type in q_out [m][n_q_heads][head_dim] (q itself
+ * if the types and strides are the same), keys turned and values as they are, rounded once, to their rows' slots.
+ * n_q_heads is a multiple of n_kv_heads, up to 2^12.  rotation [host] is read before the call returns. */
+int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch, const spark_rotation *rotation,
+                       int32_t n_q_heads, int32_t src_dtype, const void *q, int64_t q_stride, const void *k,
+                       int64_t k_stride, const void *v, int64_t v_stride, void *q_out, int64_t out_stride,
+                       void *hip_stream);
+
+/* Bytes of workspace [host] that spark_cache_attend needs for these sizes on the current device, at most (the pointers in
+ * cache and batch are not looked at).  The workspace is the call's until its work is done: calls that may run at the same
+ * time need one each.  16-byte aligned, contents of no account; NULL where none is needed. */
+int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads,
+                                size_t *bytes);
+
+/* out [m][n_q_heads][head_dim] = sum over the slots t that a row sees of p_t v_t, p = softmax(scale q . k_t), query head h
+ * with kv head h / (n_q_heads / n_kv_heads); q and out of the cache's type, 16-byte aligned, strides multiples of 8 elements.
+ * lse (or NULL) fp32 [m][n_q_heads]: log sum exp(scale q . k_t).  A row that sees nothing gets zeros, and minus infinity
+ * in lse.  scale is finite and not 0.  Scores, maxima and sums are fp32; with a bf16 cache the probabilities go into their products with the
+ * values rounded to bf16, relative to the largest one so far. */
+int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q,
+                       int64_t q_stride, float scale, int32_t causal, void *out, int64_t out_stride, float *lse,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The attention weight that each slot gets from the batch's rows: out[s][kv_head][t] = decay * before[s][kv_head][t] + sum
+ * over the rows of s that see t and the query heads of kv_head of exp(scale q . k_t - lse), for t below the
+ * sequence's length; a row with lse of minus infinity gives nothing.  q, scale and causal as for spark_cache_attend, lse as it wrote it.
+ * out, before fp32 [n][n_kv_heads][max_pages * page_tokens], before may be out itself, or NULL (zeros); decay is finite, and
+ * with 0 before is not read. */
+int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q,
+                      int64_t q_stride, float scale, int32_t causal, const float *lse, const float *before, float decay,
+                      float *out, void *hip_stream);
+
+/* Eviction.  Sequences longer than `keep` keep for each kv head `keep` slots: their first `first`, their last
+ * `recent`, and of the others those with the most weight (equal ones: the lowest slot first; a NaN weighs most); shorter ones keep
+ * all.  Keys, values and weights of what is kept move to slots 0, 1, .. in their old order: keys and values to
+ * the pages of table_out [n][out_pages] (of the same cache; none may be a page of table), or in place with table_out NULL
+ * (no page twice in table); weights to weights_out, of weights' shape or weights itself, zeros between the new
+ * length and the old.  kept int32 [n][n_kv_heads][keep]: the old slots, -1 behind the new length; lengths_out int32 [n]:
+ * the new lengths, min(length, keep).  first, recent >= 0, first + recent <= keep, 1 <= keep <= max_pages * page_tokens and, with table_out,
+ * <= out_pages * page_tokens.  Keys keep the rotation that they have; rows appended later pass their positions to
+ * spark_cache_append.  starts and m of the batch are not looked at. */
+int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, const float *weights, int32_t keep,
+                      int32_t first, int32_t recent, const int32_t *table_out, int32_t out_pages, float *weights_out,
+                      int32_t *kept, int32_t *lengths_out, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

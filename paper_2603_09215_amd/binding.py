@@ -27,7 +27,8 @@ EXPORTS = ("spark_workspace_bytes", "spark_init", "spark_seq_open", "spark_prefi
            "spark_seq_text_budget", "spark_schedule_preview", "spark_seq_set_phase", "spark_align_phases",
            "spark_init_static", "spark_tune", "spark_measure_read", "spark_scaled_rows", "spark_scaled_norm",
            "spark_scaled_weight_bytes", "spark_scaled_pack", "spark_scaled_workspace_bytes", "spark_scaled_matmul",
-           "spark_scaled_gated", "spark_scaled_model_bytes", "spark_scaled_projections")
+           "spark_scaled_gated", "spark_scaled_model_bytes", "spark_scaled_projections", "spark_cache_append",
+           "spark_cache_workspace_bytes", "spark_cache_attend", "spark_cache_weigh", "spark_cache_evict")
 
 
 class SparkConfig(C.Structure):
@@ -53,6 +54,23 @@ class SparkStats(C.Structure):
                 ("speech_ee_steps", C.c_int64), ("flush_rows", C.c_int64 * (2 * SPARK_MAX_PERIOD)),
                 ("mean_text_depth", C.c_double), ("mean_speech_depth", C.c_double),
                 ("speech_layer_saving", C.c_double), ("text_ee_steps", C.c_int64)]
+
+
+class SparkCache(C.Structure):
+    _fields_ = [("size", C.c_uint32)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_pages", "n_layers", "n_kv_heads", "page_tokens", "head_dim", "layer")] + \
+               [("pool", C.c_void_p)]
+
+
+class SparkCacheBatch(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("m", C.c_int32), ("n", C.c_int32), ("max_pages", C.c_int32),
+                ("starts", C.c_void_p), ("lengths", C.c_void_p), ("table", C.c_void_p)]
+
+
+class SparkRotation(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("rotary", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float),
+                ("freqs", C.c_void_p), ("positions", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p),
+                ("eps", C.c_double)]
 
 
 class SparkError(RuntimeError):
@@ -112,6 +130,13 @@ def load_library() -> C.CDLL:
     lib.spark_scaled_gated.argtypes = [P, P, I, P, I, I, P, P, P, Z, P]
     lib.spark_scaled_model_bytes.argtypes = [C.POINTER(SparkConfig), C.POINTER(Z)]
     lib.spark_scaled_projections.argtypes = [P, P, Z]
+    CB = (C.POINTER(SparkCache), C.POINTER(SparkCacheBatch))
+    F = C.c_float
+    lib.spark_cache_append.argtypes = [*CB, C.POINTER(SparkRotation), I, I, P, L, P, L, P, L, P, L, P]
+    lib.spark_cache_workspace_bytes.argtypes = [*CB, I, C.POINTER(Z)]
+    lib.spark_cache_attend.argtypes = [*CB, I, P, L, F, I, P, L, P, P, Z, P]
+    lib.spark_cache_weigh.argtypes = [*CB, I, P, L, F, I, P, P, F, P, P]
+    lib.spark_cache_evict.argtypes = [*CB, P, I, I, I, P, I, P, P, P, P]
     _lib = lib
     return lib
 

@@ -1,0 +1,46 @@
+// A paged cache and the batch of sequences that a call works on, as the kernels see them (include/spark.h, "Operators on a
+// paged cache").  What the device tensors hold is cut to its range here, so no value in them leads out of a buffer.
+#pragma once
+#include "device_common.h"
+
+namespace spark {
+
+struct CacheView {
+  void *pool;             // of the layer: its first page's keys of head 0
+  long long page_stride;  // elements
+  int n_pages, n_kv_heads, page_tokens, head_dim;
+  // keys (which 0) or values (1) of a head in a page: [page_tokens][head_dim]
+  template <typename T> __device__ __forceinline__ T *plane(int page, int which, int head) const {
+    return (T *)pool + page * page_stride + (long long)(which * n_kv_heads + head) * page_tokens * head_dim;
+  }
+};
+
+struct BatchView {
+  const int *starts, *lengths, *table;
+  int m, n, max_pages;
+};
+
+struct Sequence {
+  int row0, rows, length;
+  const int *pages;
+  __device__ __forceinline__ int slot(int row) const { return length - rows + row; }   // negative: none
+};
+
+__device__ __forceinline__ int cut(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+__device__ __forceinline__ Sequence sequence(const BatchView &b, int s, int page_tokens) {
+  Sequence q;
+  q.row0 = cut(b.starts[s], 0, b.m);
+  q.rows = cut(b.starts[s + 1], q.row0, b.m) - q.row0;
+  q.length = cut(b.lengths[s], 0, b.max_pages * page_tokens);
+  q.pages = b.table + (long long)s * b.max_pages;
+  return q;
+}
+
+// the page of a slot, -1 where there is none
+__device__ __forceinline__ int page_of(const Sequence &q, int slot, int page_tokens, int n_pages) {
+  const int p = q.pages[slot / page_tokens];
+  return (unsigned)p < (unsigned)n_pages ? p : -1;
+}
+
+}  // namespace spark

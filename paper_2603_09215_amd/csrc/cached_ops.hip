@@ -1,0 +1,170 @@
+// The operators on a paged cache: launches and C ABI (include/spark.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/spark.h"
+#include "cached_append.h"
+#include "cached_attend.h"
+#include "cached_evict.h"
+#include "cached_weigh.h"
+
+namespace spark {
+namespace {
+
+bool aligned(const void *p, size_t a) { return p && ((uintptr_t)p & (a - 1)) == 0; }
+size_t type_bytes(int dtype) { return dtype == SPARK_DTYPE_BF16 ? 2 : 4; }
+bool dtype_ok(int32_t d) { return d == SPARK_DTYPE_FP32 || d == SPARK_DTYPE_BF16; }
+bool within(int64_t v, int64_t lo, int64_t hi) { return v >= lo && v <= hi; }
+
+// sizes alone
+bool sizes_ok(const spark_cache *c, const spark_cache_batch *b) {
+  return c && b && c->size == sizeof(spark_cache) && b->size == sizeof(spark_cache_batch) && dtype_ok(c->dtype) && within(c->n_pages, 1, 1 << 24) &&
+         within(c->n_layers, 1, 1 << 16) && within(c->n_kv_heads, 1, 1 << 12) && within(c->page_tokens, 16, 1 << 16) && c->page_tokens % 16 == 0 &&
+         (c->head_dim == 64 || c->head_dim == 128) && within(c->layer, 0, c->n_layers - 1) && within(b->m, 0, 1 << 22) && within(b->n, 0, 1 << 16) &&
+         (int64_t)b->n * c->n_kv_heads <= 1 << 20 &&
+         within(b->max_pages, 1, 1 << 24) && (int64_t)b->max_pages * c->page_tokens <= 1 << 24;
+}
+bool heads_ok(const spark_cache *c, int32_t n_q_heads) { return within(n_q_heads, 1, 1 << 12) && n_q_heads % c->n_kv_heads == 0; }
+bool batch_ok(const spark_cache *c, const spark_cache_batch *b) {
+  return sizes_ok(c, b) && aligned(c->pool, 16) && aligned(b->starts, 4) && aligned(b->lengths, 4) && aligned(b->table, 4);
+}
+// rows of `heads` vectors
+bool rows_ok(const void *p, size_t align, int64_t stride, int64_t heads, const spark_cache *c) {
+  return aligned(p, align) && within(stride, heads * c->head_dim, (int64_t)1 << 40);
+}
+
+CacheView view(const spark_cache *c) {
+  const long long layer = 2ll * c->n_kv_heads * c->page_tokens * c->head_dim;
+  return CacheView{(char *)c->pool + c->layer * layer * type_bytes(c->dtype), layer * c->n_layers, c->n_pages, c->n_kv_heads, c->page_tokens, c->head_dim};
+}
+BatchView view(const spark_cache_batch *b) { return BatchView{b->starts, b->lengths, b->table, b->m, b->n, b->max_pages}; }
+int status() { return hipGetLastError() == hipSuccess ? SPARK_OK : SPARK_EHIP; }
+
+// calls f(T{}, std::integral_constant<int, HD>{})
+template <typename F> void by_cache(int dtype, int head_dim, F f) {
+  using H64 = std::integral_constant<int, 64>;
+  using H128 = std::integral_constant<int, 128>;
+  if (dtype == SPARK_DTYPE_FP32) head_dim == 64 ? f(float{}, H64{}) : f(float{}, H128{});
+  else head_dim == 64 ? f(bf16_t{}, H64{}) : f(bf16_t{}, H128{});
+}
+
+}  // namespace
+}  // namespace spark
+
+using namespace spark;
+
+extern "C" {
+
+int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch, const spark_rotation *rotation, int32_t n_q_heads, int32_t src_dtype,
+                       const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out,
+                       int64_t out_stride, void *hip_stream) {
+  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !dtype_ok(src_dtype) || !rotation || rotation->size != sizeof(spark_rotation))
+    return SPARK_EINVAL;
+  const size_t sb = type_bytes(src_dtype), cb = type_bytes(cache->dtype);
+  if (!rows_ok(q, sb, q_stride, n_q_heads, cache) || !rows_ok(k, sb, k_stride, cache->n_kv_heads, cache) ||
+      !rows_ok(v, sb, v_stride, cache->n_kv_heads, cache) || !rows_ok(q_out, cb, out_stride, n_q_heads, cache) ||
+      (q_out == q && (src_dtype != cache->dtype || (out_stride != q_stride && batch->m > 1))))
+    return SPARK_EINVAL;
+  if (!within(rotation->rotary, 0, cache->head_dim) || rotation->rotary % 2 || !std::isfinite(rotation->amplitude) || !(rotation->eps >= 0.0) ||
+      (rotation->rotary > 0 && !aligned(rotation->freqs, 8)) || ((uintptr_t)rotation->positions & 3) || ((uintptr_t)rotation->q_gain & 3) ||
+      ((uintptr_t)rotation->k_gain & 3))
+    return SPARK_EINVAL;
+  if (batch->m == 0 || batch->n == 0) return SPARK_OK;
+  AppendArgs a{};
+  a.cache = view(cache); a.batch = view(batch);
+  a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = out_stride;
+  a.n_q_heads = n_q_heads; a.rotary = rotation->rotary; a.interleaved = rotation->interleaved != 0;
+  a.amplitude = rotation->amplitude; a.eps = rotation->eps;
+  a.freqs = rotation->freqs; a.positions = rotation->positions; a.q_gain = rotation->q_gain; a.k_gain = rotation->k_gain;
+  auto vec = [](const void *p, size_t bytes, int64_t stride) { return aligned(p, 4 * bytes) && stride % 4 == 0; };
+  const bool wide = a.rotary % 8 == 0 && vec(q, sb, q_stride) && vec(k, sb, k_stride) && vec(v, sb, v_stride) && vec(q_out, cb, out_stride);
+  const int heads = n_q_heads + 2 * cache->n_kv_heads;
+  a.rows = batch->m >= 2048 ? 4 : 1;
+  a.heads_per_wg = a.rows > 1 ? heads : 16;
+  const dim3 grid((batch->m + a.rows - 1) / a.rows, (heads + a.heads_per_wg - 1) / a.heads_per_wg);
+  const size_t lds = sizeof(float) * a.rows * std::max(2, a.rotary);
+  by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    auto go = [&](auto kern) { kern<<<grid, 256, lds, (hipStream_t)hip_stream>>>(a); };
+    if (src_dtype == SPARK_DTYPE_FP32) wide ? go(cached_append_k<float, T, HD, true>) : go(cached_append_k<float, T, HD, false>);
+    else wide ? go(cached_append_k<bf16_t, T, HD, true>) : go(cached_append_k<bf16_t, T, HD, false>);
+  });
+  return status();
+}
+
+int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, size_t *bytes) {
+  if (!sizes_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !bytes) return SPARK_EINVAL;
+  *bytes = 0;
+  return SPARK_OK;
+}
+
+int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
+                       int32_t causal, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 ||
+      !rows_ok(out, 16, out_stride, n_q_heads, cache) || out_stride % 8 || ((uintptr_t)lse & 3) || !std::isfinite(scale) || scale == 0.f)
+    return SPARK_EINVAL;
+  if (batch->m == 0 || batch->n == 0) return SPARK_OK;
+  AttendArgs a{};
+  a.cache = view(cache); a.batch = view(batch);
+  a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride;
+  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0; a.scale = scale;
+  by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
+    cached_attend_k<decltype(t), decltype(hd)::value><<<dim3(batch->m, n_q_heads), 64, 0, (hipStream_t)hip_stream>>>(a);
+  });
+  return status();
+}
+
+int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
+                      int32_t causal, const float *lse, const float *before, float decay, float *out, void *hip_stream) {
+  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || (batch->m > 0 && (!rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 || !aligned(lse, 4))) ||
+      ((uintptr_t)before & 3) || !aligned(out, 4) || !std::isfinite(scale) || scale == 0.f || !std::isfinite(decay))
+    return SPARK_EINVAL;
+  if (batch->n == 0) return SPARK_OK;
+  WeighArgs a{};
+  a.cache = view(cache); a.batch = view(batch);
+  a.q = q; a.lse = lse; a.before = decay != 0.f ? before : nullptr; a.out = out; a.q_stride = q_stride;
+  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0; a.scale = scale; a.decay = decay;
+  const int slots = batch->max_pages * cache->page_tokens;
+  by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
+    cached_weigh_k<decltype(t), decltype(hd)::value><<<dim3(batch->n * cache->n_kv_heads, std::min((slots + 255) / 256, 512)), 256, 0, (hipStream_t)hip_stream>>>(a);
+  });
+  return status();
+}
+
+int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, const float *weights, int32_t keep, int32_t first, int32_t recent,
+                      const int32_t *table_out, int32_t out_pages, float *weights_out, int32_t *kept, int32_t *lengths_out, void *hip_stream) {
+  if (!sizes_ok(cache, batch) || !aligned(cache->pool, 16) || !aligned(batch->lengths, 4) || !aligned(batch->table, 4) || !aligned(weights, 4) ||
+      !aligned(weights_out, 4) || !aligned(kept, 4) || !aligned(lengths_out, 4) || ((uintptr_t)table_out & 3) || lengths_out == batch->lengths)
+    return SPARK_EINVAL;
+  const int64_t slots = (int64_t)batch->max_pages * cache->page_tokens;
+  if (first < 0 || recent < 0 || !within(keep, 1, slots) || (int64_t)first + recent > keep ||
+      (table_out && (!within(out_pages, 1, 1 << 24) || (int64_t)out_pages * cache->page_tokens < keep)))
+    return SPARK_EINVAL;
+  if (batch->n == 0) return SPARK_OK;
+  EvictArgs a{};
+  a.cache = view(cache); a.batch = view(batch);
+  a.weights = weights; a.weights_out = weights_out; a.kept = kept; a.lengths_out = lengths_out;
+  a.table_out = table_out ? table_out : batch->table;
+  a.out_pages = table_out ? out_pages : batch->max_pages;
+  a.keep = keep; a.first = first; a.recent = recent;
+  const int heads = batch->n * cache->n_kv_heads;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  cached_choose_k<<<heads, EVICT_THREADS, 0, stream>>>(a);
+  by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value, PIECES = HD * sizeof(T) / 16;
+    if (a.table_out == batch->table) {
+      cached_move_k<T, HD, 8><<<heads * 2 * (PIECES / 8), 1024, 0, stream>>>(a);
+    } else {
+      const int rounds = (keep * PIECES + 255) / 256;
+      cached_move_k<T, HD, PIECES><<<dim3(heads * 2, std::min(rounds, 256)), 256, 0, stream>>>(a);
+    }
+  });
+  return status();
+}
+
+}  // extern "C"

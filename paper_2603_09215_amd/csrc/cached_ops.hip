@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "../../include/spark.h"
@@ -26,7 +27,9 @@ bool sizes_ok(const spark_cache *c, const spark_cache_batch *b) {
          (int64_t)b->n * c->n_kv_heads <= 1 << 20 &&
          within(b->max_pages, 1, 1 << 24) && (int64_t)b->max_pages * c->page_tokens <= 1 << 24;
 }
-bool heads_ok(const spark_cache *c, int32_t n_q_heads) { return within(n_q_heads, 1, 1 << 12) && n_q_heads % c->n_kv_heads == 0; }
+bool heads_ok(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads) {
+  return within(n_q_heads, 1, 1 << 12) && n_q_heads % c->n_kv_heads == 0 && (int64_t)b->m * n_q_heads <= 1 << 28;
+}
 bool batch_ok(const spark_cache *c, const spark_cache_batch *b) {
   return sizes_ok(c, b) && aligned(c->pool, 16) && aligned(b->starts, 4) && aligned(b->lengths, 4) && aligned(b->table, 4);
 }
@@ -50,6 +53,50 @@ template <typename F> void by_cache(int dtype, int head_dim, F f) {
   else head_dim == 64 ? f(bf16_t{}, H64{}) : f(bf16_t{}, H128{});
 }
 
+// How attention is cut: `pairs` (row, head) pairs a tile, at most `tiles` tiles for each kv head, their tokens in `splits` parts
+struct AttendPlan {
+  int pairs, splits;
+  long long tiles;
+};
+AttendPlan attend_plan(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, int n_cu) {
+  AttendPlan p;
+  const long long group = n_q_heads / c->n_kv_heads, m = b->m, mean = std::max<long long>(1, m * group / b->n), slots = (long long)b->max_pages * c->page_tokens;
+  const bool wide = c->dtype == SPARK_DTYPE_FP32 && c->head_dim == 128;   // (queries and sums take twice the registers)
+  p.pairs = mean <= 16 ? 16 : mean <= 64 ? 32 : mean <= 128 || wide ? 128 : 256;
+  // (every sequence adds at most one tile that is not full)
+  p.tiles = std::min(m * ((group + p.pairs - 1) / p.pairs), m * group / p.pairs + b->n);
+  const long long wgs = p.tiles * c->n_kv_heads;
+  const int piece = p.pairs <= 32 ? 128 : 256;   // the fewest tokens that are worth a part
+  p.splits = (int)std::max<long long>(1, std::min<long long>({slots / piece, (p.pairs <= 32 ? 4 : 1) * n_cu / wgs, 64}));
+  return p;
+}
+size_t attend_workspace(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, const AttendPlan &p) {
+  return p.splits == 1 ? 0 : (size_t)p.splits * b->m * n_q_heads * (c->head_dim + 2) * sizeof(float);
+}
+
+// compute units of the current device; looked up once per device
+int compute_units() {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// more LDS than 64 KiB has to be asked for, once a kernel and device
+template <auto KERN> bool allow_lds(size_t bytes) {
+  static std::atomic<uint64_t> asked{0};
+  if (bytes <= 60 << 10) return true;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return false;
+  if (dev < 64 && (asked.load(std::memory_order_relaxed) >> dev & 1)) return true;
+  if (hipFuncSetAttribute((const void *)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return false;
+  if (dev < 64) asked.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return true;
+}
+
 }  // namespace
 }  // namespace spark
 
@@ -60,7 +107,7 @@ extern "C" {
 int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch, const spark_rotation *rotation, int32_t n_q_heads, int32_t src_dtype,
                        const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out,
                        int64_t out_stride, void *hip_stream) {
-  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !dtype_ok(src_dtype) || !rotation || rotation->size != sizeof(spark_rotation))
+  if (!batch_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || !dtype_ok(src_dtype) || !rotation || rotation->size != sizeof(spark_rotation))
     return SPARK_EINVAL;
   const size_t sb = type_bytes(src_dtype), cb = type_bytes(cache->dtype);
   if (!rows_ok(q, sb, q_stride, n_q_heads, cache) || !rows_ok(k, sb, k_stride, cache->n_kv_heads, cache) ||
@@ -97,30 +144,64 @@ int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch,
 }
 
 int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, size_t *bytes) {
-  if (!sizes_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !bytes) return SPARK_EINVAL;
+  if (!sizes_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || !bytes) return SPARK_EINVAL;
   *bytes = 0;
+  if (batch->m == 0 || batch->n == 0) return SPARK_OK;
+  const int n_cu = compute_units();
+  if (n_cu <= 0) return SPARK_EHIP;
+  *bytes = attend_workspace(cache, batch, n_q_heads, attend_plan(cache, batch, n_q_heads, n_cu));
   return SPARK_OK;
 }
 
 int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
                        int32_t causal, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
-  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || !rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 ||
+  if (!batch_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || !rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 ||
       !rows_ok(out, 16, out_stride, n_q_heads, cache) || out_stride % 8 || ((uintptr_t)lse & 3) || !std::isfinite(scale) || scale == 0.f)
     return SPARK_EINVAL;
   if (batch->m == 0 || batch->n == 0) return SPARK_OK;
+  const int n_cu = compute_units();
+  if (n_cu <= 0) return SPARK_EHIP;
+  const AttendPlan plan = attend_plan(cache, batch, n_q_heads, n_cu);
+  const size_t need = attend_workspace(cache, batch, n_q_heads, plan);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SPARK_ENOMEM;
+  if (need > 0 && !aligned(workspace, 16)) return SPARK_EINVAL;
   AttendArgs a{};
   a.cache = view(cache); a.batch = view(batch);
   a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride;
-  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0; a.scale = scale;
+  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0;
+  a.factor = std::fabs(scale) * 1.44269504088896340736f;
+  a.flip = scale < 0.f ? 0x80000000u : 0u;
+  a.splits = plan.splits;
+  a.part = (float *)workspace;
+  a.part_ml = (float2 *)(a.part + (size_t)plan.splits * batch->m * n_q_heads * cache->head_dim);
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const unsigned grid = (unsigned)(plan.tiles * cache->n_kv_heads * plan.splits);
+  bool ok = true;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
-    cached_attend_k<decltype(t), decltype(hd)::value><<<dim3(batch->m, n_q_heads), 64, 0, (hipStream_t)hip_stream>>>(a);
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    auto go = [&](auto kern, int threads, size_t lds, bool allowed) {
+      if ((ok = allowed)) kern<<<grid, threads, lds, stream>>>(a);
+    };
+    if (plan.pairs <= 32) {
+      if (plan.pairs == 16) go(cached_stream_k<T, HD, 1>, 256, Stream<T, HD, 1>::LDS, true);
+      else go(cached_stream_k<T, HD, 2>, 256, Stream<T, HD, 2>::LDS, true);
+    } else if (plan.pairs == 128) {
+      go(cached_tile_k<T, HD, 4>, 256, Tile<T, HD, 4>::LDS, allow_lds<cached_tile_k<T, HD, 4>>(Tile<T, HD, 4>::LDS));
+    } else if constexpr (HD * sizeof(T) < 512) {
+      go(cached_tile_k<T, HD, 8>, 512, Tile<T, HD, 8>::LDS, allow_lds<cached_tile_k<T, HD, 8>>(Tile<T, HD, 8>::LDS));
+    }
+    if (ok && plan.splits > 1) {
+      const long long vectors = (long long)batch->m * n_q_heads, each = 256 / (HD / 4);
+      cached_join_k<T, HD><<<(unsigned)((vectors + each - 1) / each), 256, 0, stream>>>(a);
+    }
   });
-  return status();
+  return ok ? status() : SPARK_EHIP;
 }
 
 int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
                       int32_t causal, const float *lse, const float *before, float decay, float *out, void *hip_stream) {
-  if (!batch_ok(cache, batch) || !heads_ok(cache, n_q_heads) || (batch->m > 0 && (!rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 || !aligned(lse, 4))) ||
+  if (!batch_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || (batch->m > 0 && (!rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 || !aligned(lse, 4))) ||
       ((uintptr_t)before & 3) || !aligned(out, 4) || !std::isfinite(scale) || scale == 0.f || !std::isfinite(decay))
     return SPARK_EINVAL;
   if (batch->n == 0) return SPARK_OK;

@@ -208,10 +208,16 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
   WeighArgs a{};
   a.cache = view(cache); a.batch = view(batch);
   a.q = q; a.lse = lse; a.before = decay != 0.f ? before : nullptr; a.out = out; a.q_stride = q_stride;
-  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0; a.scale = scale; a.decay = decay;
-  const int slots = batch->max_pages * cache->page_tokens;
+  a.n_q_heads = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.causal = causal != 0;
+  a.factor = std::fabs(scale) * 1.44269504088896340736f;
+  a.flip = scale < 0.f ? 0x80000000u : 0u;
+  a.decay = decay;
+  // (from two blocks of pairs for each of four waves on)
+  a.way = (long long)batch->m * a.group / batch->n >= 256 ? 4 : 1;
+  const int slots = batch->max_pages * cache->page_tokens, each = 128 / a.way;
+  const dim3 grid(batch->n * cache->n_kv_heads, std::min((slots + each - 1) / each, 1024));
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
-    cached_weigh_k<decltype(t), decltype(hd)::value><<<dim3(batch->n * cache->n_kv_heads, std::min((slots + 255) / 256, 512)), 256, 0, (hipStream_t)hip_stream>>>(a);
+    cached_weigh_k<decltype(t), decltype(hd)::value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a);
   });
   return status();
 }

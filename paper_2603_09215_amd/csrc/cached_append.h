@@ -46,27 +46,25 @@ template <typename T> __device__ __forceinline__ void load4(const T *p, float *f
     f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
   }
 }
-template <typename T> __device__ __forceinline__ void store4(T *p, const float *f) {
-  if constexpr (sizeof(T) == 4) {
-    *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
-  } else {
-    *(uint2 *)p = make_uint2(f32_to_bf16(f[0]) | ((uint32_t)f32_to_bf16(f[1]) << 16), f32_to_bf16(f[2]) | ((uint32_t)f32_to_bf16(f[3]) << 16));
-  }
+template <typename T> __device__ __forceinline__ void store_four(T *p, const float *f) {
+  if constexpr (sizeof(T) == 4) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+  else *(uint2 *)p = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
 }
 
 // A head's vector takes HD / 8 lanes of eight values each, as four pairs: (a, b) of pair p are values (p, p + rotary / 2),
-// interleaved (2 p, 2 p + 1), and past the rotary part (which stays) its neighbours.  VEC: rotary a multiple of
-// eight and everything aligned for vectors of four values; then a lane's pairs are all turned or none.
+// interleaved (2 p, 2 p + 1), and past the rotary part (which stays) neighbours.  A group of such lanes has one row and goes through its share of
+// the heads, so angles, gains and the row's place are found once for all of them.  VEC: rotary a multiple of eight
+// and everything aligned for vectors of four values; then a lane's pairs are all turned or none.
 template <typename S, typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
-  extern __shared__ float s_trig[];   // [rows][rotary / 2] cosines and sines
+  extern __shared__ float2 s_trig[];   // [rows][rotary / 2] cosine and sine
+  __shared__ int s_seq[4];
   constexpr int LANES = HD / 8;
   const int half = a.rotary / 2, row_first = blockIdx.x * a.rows, row_end = min(row_first + a.rows, a.batch.m);
-  __shared__ int s_seq[64];
-  // each row's sequence: the last that starts at it or before (rows outside all of them: -1)
+  // each row's sequence: the first that ends behind it, if it has begun (rows outside all of them: -1)
   if ((int)threadIdx.x < row_end - row_first) {
     const int r = row_first + threadIdx.x;
-    int lo = 0, hi = a.batch.n;   // the first start past r lies in lo .. hi + 1
+    int lo = 0, hi = a.batch.n;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (a.batch.starts[mid + 1] > r) hi = mid;
@@ -76,113 +74,116 @@ __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
   }
   __syncthreads();
   for (int i = threadIdx.x; i < (row_end - row_first) * half; i += blockDim.x) {
-    const int r = row_first + i / half, j = i % half, s = s_seq[i / half];
+    const int r = row_first + i / half, s = s_seq[i / half];
     if (s < 0) continue;
-    const Sequence q = sequence(a.batch, s, a.cache.page_tokens);
-    const int position = a.positions ? a.positions[r] : q.slot(r - q.row0);
+    int position;
+    if (a.positions) {
+      position = a.positions[r];
+    } else {
+      const Sequence q = sequence(a.batch, s, a.cache.page_tokens);
+      position = q.slot(r - q.row0);
+    }
     float c, sn;
-    cos_sin((double)position * a.freqs[j], c, sn);
-    s_trig[2 * i] = c * a.amplitude;
-    s_trig[2 * i + 1] = sn * a.amplitude;
+    cos_sin((double)position * a.freqs[i % half], c, sn);
+    s_trig[i] = make_float2(c * a.amplitude, sn * a.amplitude);
   }
   __syncthreads();
-  const int heads = a.n_q_heads + 2 * a.cache.n_kv_heads, head0 = blockIdx.y * a.heads_per_wg, share = min(a.heads_per_wg, heads - head0);
-  const int c = threadIdx.x % LANES, p0 = 4 * c;
-  for (int u = threadIdx.x / LANES; u < (row_end - row_first) * share; u += blockDim.x / LANES) {
-    const int i = u / share, r = row_first + i, h = head0 + u % share, s = s_seq[i];
-    if (s < 0) continue;   // (the same for all lanes of a head)
-    const int which = h < a.n_q_heads ? 0 : h < a.n_q_heads + a.cache.n_kv_heads ? 1 : 2;
-    const int kvh = h - a.n_q_heads - (which == 2 ? a.cache.n_kv_heads : 0);
-    const S *src = which == 0 ? (const S *)a.q + r * a.q_stride + (long long)h * HD
-                 : which == 1 ? (const S *)a.k + r * a.k_stride + (long long)kvh * HD
-                              : (const S *)a.v + r * a.v_stride + (long long)kvh * HD;
-    const bool turn = which < 2;
-    // where pair p lies
-    auto first = [&](int p) { return p < half ? (a.interleaved ? 2 * p : p) : a.rotary + 2 * (p - half); };
-    auto second = [&](int p) { return p < half ? (a.interleaved ? 2 * p + 1 : p + half) : a.rotary + 2 * (p - half) + 1; };
-    const bool apart = !a.interleaved && p0 < half;   // (VEC)
-    float x[4], y[4];
-    if constexpr (VEC) {
-      float lo[4], hi[4];
-      load4(src + (apart ? p0 : first(p0)), lo);
-      load4(src + (apart ? p0 + half : first(p0) + 4), hi);
+
+  const int groups = blockDim.x / LANES / a.rows, group = threadIdx.x / LANES, i = group / groups, r = row_first + i;
+  if (r >= row_end || s_seq[i] < 0) return;
+  const Sequence seq = sequence(a.batch, s_seq[i], a.cache.page_tokens);
+  const int slot = seq.slot(r - seq.row0), page = slot < 0 ? -1 : page_of(seq, slot, a.cache.page_tokens, a.cache.n_pages);
+  const int token = slot < 0 ? 0 : slot % a.cache.page_tokens;
+  const int c = threadIdx.x % LANES, p0 = 4 * c, nq = a.n_q_heads, nkv = a.cache.n_kv_heads;
+  // where a lane's eight values lie: VEC two fours, else pairs
+  const bool turned = p0 < half, apart = turned && !a.interleaved;
+  int at[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = apart ? lo[e] : e < 2 ? lo[2 * (e & 1)] : hi[2 * (e & 1)];
-        y[e] = apart ? hi[e] : e < 2 ? lo[2 * (e & 1) + 1] : hi[2 * (e & 1) + 1];
-      }
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (VEC) {
+      at[e] = apart ? p0 + (e & 3) + (e >> 2) * half : (turned ? 2 * p0 : a.rotary + 2 * (p0 - half)) + e;
+    } else {   // the first of four pairs, the second of them
+      const int p = p0 + (e & 3);
+      at[e] = p < half ? (a.interleaved ? 2 * p + (e >> 2) : p + (e >> 2) * half) : a.rotary + 2 * (p - half) + (e >> 2);
+    }
+  }
+  float cs[4], sn[4], gain[2][8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 v = p0 + e < half ? s_trig[i * half + p0 + e] : make_float2(1.f, 0.f);
+    cs[e] = v.x;
+    sn[e] = v.y;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    gain[0][e] = a.q_gain ? a.q_gain[at[e]] : 1.f;
+    gain[1][e] = a.k_gain ? a.k_gain[at[e]] : 1.f;
+  }
+  const int head0 = blockIdx.y * a.heads_per_wg, head_end = min(head0 + a.heads_per_wg, nq + 2 * nkv);
+  const S *q = (const S *)a.q + r * a.q_stride, *k = (const S *)a.k + r * a.k_stride, *v = (const S *)a.v + r * a.v_stride;
+  T *out = (T *)a.q_out + r * a.out_stride, *place = a.cache.plane<T>(max(page, 0), 0, 0) + token * HD;
+  const long long plane = (long long)a.cache.page_tokens * HD;
+#pragma unroll 2
+  for (int h = head0 + group % groups; h < head_end; h += groups) {
+    const int which = h < nq ? 0 : h < nq + nkv ? 1 : 2;
+    const S *src = which == 0 ? q + h * HD : which == 1 ? k + (h - nq) * HD : v + (h - nq - nkv) * HD;
+    float x[8];
+    if constexpr (VEC) {
+      load4(src + at[0], x);
+      load4(src + at[4], x + 4);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = Elem<S>::widen(src[first(p0 + e)]);
-        y[e] = Elem<S>::widen(src[second(p0 + e)]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = Elem<S>::widen(src[at[e]]);
     }
-    const float *gain = which == 0 ? a.q_gain : which == 1 ? a.k_gain : nullptr;
-    if (gain) {
+    if (which == 0 ? a.q_gain != nullptr : which == 1 && a.k_gain != nullptr) {
       float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += x[e] * x[e] + y[e] * y[e];
+      for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
       if (sum > 1e-30f && sum < 1e37f) {
         const float f = 1.0f / sqrtf(sum * (1.0f / HD) + (float)a.eps);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] *= f * gain[first(p0 + e)];
-          y[e] *= f * gain[second(p0 + e)];
-        }
+        for (int e = 0; e < 8; ++e) x[e] *= f * (which == 0 ? gain[0][e] : gain[1][e]);
       } else {   // squares that leave fp32's range (the same lanes for all of a head)
         double wide = 0.0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) wide += (double)x[e] * x[e] + (double)y[e] * y[e];
+        for (int e = 0; e < 8; ++e) wide += (double)x[e] * x[e];
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) wide += __shfl_xor(wide, o, 64);
         const double f = 1.0 / sqrt(wide * (1.0 / HD) + a.eps);
 #pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)(x[e] * f * (which == 0 ? gain[0][e] : gain[1][e]));
+      }
+    }
+    if (which < 2 && a.rotary) {
+      if (!VEC || apart) {
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (!VEC && p0 + e >= half) continue;
+            const float t = x[e] * cs[e] - x[4 + e] * sn[e];
+            x[4 + e] = x[4 + e] * cs[e] + x[e] * sn[e];
+            x[e] = t;
+          }
+        }
+      } else if (turned) {
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[e] = (float)(x[e] * f * gain[first(p0 + e)]);
-          y[e] = (float)(y[e] * f * gain[second(p0 + e)]);
+          const float t = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
+          x[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+          x[2 * e] = t;
         }
       }
     }
-    if (turn) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (p0 + e < half) {
-          const float cs = s_trig[2 * (i * half + p0 + e)], sn = s_trig[2 * (i * half + p0 + e) + 1];
-          const float t = x[e] * cs - y[e] * sn;
-          y[e] = y[e] * cs + x[e] * sn;
-          x[e] = t;
-        }
-      }
-    }
-    T *dst;
-    if (which == 0) {
-      dst = (T *)a.q_out + r * a.out_stride + (long long)h * HD;
-    } else {
-      const Sequence q = sequence(a.batch, s, a.cache.page_tokens);
-      const int slot = q.slot(r - q.row0);
-      if (slot < 0) continue;
-      const int page = page_of(q, slot, a.cache.page_tokens, a.cache.n_pages);
-      if (page < 0) continue;
-      dst = a.cache.plane<T>(page, which - 1, kvh) + slot % a.cache.page_tokens * HD;
-    }
+    if (which > 0 && page < 0) continue;
+    T *dst = which == 0 ? out + h * HD : place + (which - 1) * nkv * plane + (h - nq - (which - 1) * nkv) * plane;
     if constexpr (VEC) {
-      float lo[4], hi[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lo[e] = apart ? x[e] : (e & 1) ? y[e >> 1] : x[e >> 1];
-        hi[e] = apart ? y[e] : (e & 1) ? y[2 + (e >> 1)] : x[2 + (e >> 1)];
-      }
-      store4(dst + (apart ? p0 : first(p0)), lo);
-      store4(dst + (apart ? p0 + half : first(p0) + 4), hi);
+      store_four(dst + at[0], x);
+      store_four(dst + at[4], x + 4);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dst[first(p0 + e)] = Elem<T>::narrow(x[e]);
-        dst[second(p0 + e)] = Elem<T>::narrow(y[e]);
-      }
+      for (int e = 0; e < 8; ++e) dst[at[e]] = Elem<T>::narrow(x[e]);
     }
   }
 }

@@ -40,13 +40,6 @@ typedef __attribute__((ext_vector_type(8))) __bf16 ca_bf16x8;
 typedef __attribute__((ext_vector_type(4))) short ca_s16x4;
 typedef __attribute__((ext_vector_type(4))) float ca_f32x4;
 typedef __attribute__((ext_vector_type(16))) float ca_f32x16;
-typedef __attribute__((ext_vector_type(2))) __bf16 ca_bf16x2;
-typedef __attribute__((ext_vector_type(2))) float ca_f32x2;
-
-__device__ __forceinline__ uint32_t ca_pack(float a, float b) {   // half to even, one instruction
-  const ca_f32x2 f = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, ca_bf16x2));
-}
 __device__ __forceinline__ ca_bf16x8 ca_operand(const uint4 &v) { return __builtin_bit_cast(ca_bf16x8, v); }
 template <typename T> __device__ __forceinline__ uint4 ca_signed(uint4 v, uint32_t flip) {
   const uint32_t x = sizeof(T) == 4 ? flip : flip | (flip >> 16);
@@ -86,15 +79,17 @@ template <typename T, int HD> __device__ __forceinline__ int ca_turn(int row) {
   return ((row & 3) << 2) | ((row >> 2) & 3);
 }
 
-// The tile of pairs that a workgroup takes, from a count over all sequences: (sequence, tile in it, tiles of it), or false.
+// The tile of pairs that a workgroup takes, from a count over all sequences: its sequence, tile in it and tiles of it, or false.
 // Called by whole waves.
-__device__ __forceinline__ bool find_tile(const BatchView &b, int page_tokens, int group, int per_tile, int tile, int &s, int &t, int &count) {
+__device__ __forceinline__ bool find_tile(const BatchView &b, int page_tokens, int group, int per_tile, int tile, Sequence &q, int &t, int &count) {
   const int lane = threadIdx.x & 63;
   for (int s0 = 0; s0 < b.n; s0 += 64) {
-    int c = 0;
+    int c = 0, row0 = 0, rows = 0, length = 0;
     if (s0 + lane < b.n) {
-      const int row0 = cut(b.starts[s0 + lane], 0, b.m);
-      c = ((cut(b.starts[s0 + lane + 1], row0, b.m) - row0) * group + per_tile - 1) / per_tile;
+      length = b.lengths[s0 + lane];
+      row0 = cut(b.starts[s0 + lane], 0, b.m);
+      rows = cut(b.starts[s0 + lane + 1], row0, b.m) - row0;
+      c = (rows * group + per_tile - 1) / per_tile;
     }
     int incl = c;
 #pragma unroll
@@ -105,12 +100,15 @@ __device__ __forceinline__ bool find_tile(const BatchView &b, int page_tokens, i
     const unsigned long long past = __ballot(incl > tile);
     if (past) {
       const int l = __ffsll(past) - 1;
-      s = s0 + l;
-      count = __builtin_amdgcn_readfirstlane(__shfl(c, l, 64));
-      t = tile - (__builtin_amdgcn_readfirstlane(__shfl(incl, l, 64)) - count);
+      q.row0 = __builtin_amdgcn_readlane(row0, l);
+      q.rows = __builtin_amdgcn_readlane(rows, l);
+      q.length = cut(__builtin_amdgcn_readlane(length, l), 0, b.max_pages * page_tokens);
+      q.pages = b.table + (long long)(s0 + l) * b.max_pages;
+      count = __builtin_amdgcn_readlane(c, l);
+      t = tile - (__builtin_amdgcn_readlane(incl, l) - count);
       return true;
     }
-    tile -= __builtin_amdgcn_readfirstlane(__shfl(incl, 63, 64));
+    tile -= __builtin_amdgcn_readlane(incl, 63);
   }
   return false;
 }
@@ -150,9 +148,9 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
   const int nkv = a.cache.n_kv_heads, kvh = blockIdx.x % nkv, split = blockIdx.x / nkv % a.splits;
-  int s, tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, NB * 16, blockIdx.x / nkv / a.splits, s, tile, count)) return;
-  const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
+  Sequence seq;
+  int tile, count;
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, NB * 16, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
   const int pair0 = tile * NB * 16, pairs = min(NB * 16, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
@@ -183,15 +181,6 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
   uint4 vr[BF ? S::V_LOADS : S::V_LOADS / 4];
   char *s_v = (char *)ca_smem + wave * S::V_BYTES;
   constexpr int LPT = HD / 8;   // bf16: lanes a token's values take
-  unsigned here = 0;            // which 16s of the piece have a page
-  auto load = [&](int pages) {
-    here = 0;
-#pragma unroll
-    for (int i = 0; i < S::BLOCKS; ++i) {
-      const int page = __builtin_amdgcn_readlane(pages, i);
-      if (page >= 0) here |= 1u << i;
-    }
-  };
   auto load_keys = [&](int piece, int pages) {
 #pragma unroll
     for (int i = 0; i < S::BLOCKS; ++i) {
@@ -255,17 +244,17 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
   };
 
   constexpr int PER16 = S::TOKENS / 16;
+  // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
+  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, piece * PER16 + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
   int piece = first + wave;
-  int pages = pages_of(seq, a.cache, piece * PER16 + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0);
+  int pages = pages_at(piece), next_pages = pages_at(piece + S::WAVES);
   if (piece < stop) {
     load_keys(piece, pages);
     load_values(piece, pages);
   }
-  int next_pages = pages_of(seq, a.cache, (piece + S::WAVES) * PER16 + (lane & (S::BLOCKS - 1)), piece + S::WAVES < stop ? end : 0);
   __syncthreads();   // (s_bad)
   for (; piece < stop; piece += S::WAVES) {
-    load(pages);
-    const unsigned now = here;
+    const unsigned now = (unsigned)__ballot(pages >= 0) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
     const int t0 = piece * S::TOKENS;
     ca_f32x4 sc[NB][S::BLOCKS];
 #pragma unroll
@@ -286,6 +275,11 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
           }
         }
       }
+    pages = next_pages;
+    if (piece + S::WAVES < stop) {
+      next_pages = pages_at(piece + 2 * S::WAVES);
+      load_keys(piece + S::WAVES, pages);
+    }
     if (t0 + S::TOKENS - 1 > least) clean(piece);
     uint4 va[BF ? 1 : HD / 16];
     if constexpr (BF) {
@@ -300,12 +294,7 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) va[d] = vr[d];
     }
-    pages = next_pages;
-    if (piece + S::WAVES < stop) {
-      load_keys(piece + S::WAVES, pages);
-      load_values(piece + S::WAVES, pages);
-      next_pages = pages_of(seq, a.cache, (piece + 2 * S::WAVES) * PER16 + (lane & (S::BLOCKS - 1)), piece + 2 * S::WAVES < stop ? end : 0);
-    }
+    if (piece + S::WAVES < stop) load_values(piece + S::WAVES, pages);
     const bool masked = t0 + S::TOKENS - 1 > least || now != (1u << S::BLOCKS) - 1;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -347,8 +336,8 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
       ca_bf16x8 p[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        p[b] = ca_operand(make_uint4(ca_pack(sc[b][0][0], sc[b][0][1]), ca_pack(sc[b][0][2], sc[b][0][3]), ca_pack(sc[b][1][0], sc[b][1][1]),
-                                     ca_pack(sc[b][1][2], sc[b][1][3])));
+        p[b] = ca_operand(make_uint4(pack_bf16(sc[b][0][0], sc[b][0][1]), pack_bf16(sc[b][0][2], sc[b][0][3]), pack_bf16(sc[b][1][0], sc[b][1][1]),
+                                     pack_bf16(sc[b][1][2], sc[b][1][3])));
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
         union { ca_s16x4 h[2]; ca_bf16x8 v; } x;
@@ -429,7 +418,7 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
       } else {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         T *out = (T *)a.out + r * a.out_stride + (long long)h * HD + e0;
-        if constexpr (BF) *(uint2 *)out = make_uint2(ca_pack(y[0] * inv, y[1] * inv), ca_pack(y[2] * inv, y[3] * inv));
+        if constexpr (BF) *(uint2 *)out = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
         else *(float4 *)out = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
         if (a.lse && e0 == 0) a.lse[(long long)r * a.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
       }
@@ -460,10 +449,10 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int nkv = a.cache.n_kv_heads, kvh = blockIdx.x % nkv, split = blockIdx.x / nkv % a.splits;
-  int s, tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, blockIdx.x / nkv / a.splits, s, tile, count)) return;
+  Sequence seq;
+  int tile, count;
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
   tile = count - 1 - tile;   // the longest first
-  const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
   const int pair0 = tile * S::PAIRS, pairs = min(S::PAIRS, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
@@ -604,7 +593,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
           for (int j = 0; j < 2; ++j) {   // 16 tokens
             uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = ca_pack(sc[b][8 * j + 2 * e], sc[b][8 * j + 2 * e + 1]);
+            for (int e = 0; e < 4; ++e) w[e] = pack_bf16(sc[b][8 * j + 2 * e], sc[b][8 * j + 2 * e + 1]);
             const ca_bf16x8 pr = ca_operand(make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) {
@@ -662,7 +651,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
       const int e0 = 32 * d + 8 * i + 4 * half;
       const float4 y = make_float4(o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv);
       if (a.splits > 1) *(float4 *)(a.part + at * HD + e0) = y;
-      else if constexpr (BF) *(uint2 *)((T *)a.out + r0 * a.out_stride + (long long)h * HD + e0) = make_uint2(ca_pack(y.x, y.y), ca_pack(y.z, y.w));
+      else if constexpr (BF) *(uint2 *)((T *)a.out + r0 * a.out_stride + (long long)h * HD + e0) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
       else *(float4 *)((T *)a.out + r0 * a.out_stride + (long long)h * HD + e0) = y;
     }
   if (half == 0) {
@@ -673,36 +662,57 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
 
 // ------------------------------------------------------------------ the parts together
 
+constexpr int MOST_SPLITS = 64;
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
   constexpr int LANES = HD / 4;
   const long long i = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (i >= (long long)a.batch.m * a.n_q_heads) return;
   const int r = (int)(i / a.n_q_heads), e0 = threadIdx.x % LANES * 4;
-  int lo = 0, hi = a.batch.n;   // whose row is it
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (a.batch.starts[mid + 1] > r) hi = mid;
-    else lo = mid + 1;
-  }
-  if (lo == a.batch.n || a.batch.starts[lo] > r) return;
+  const int lane = threadIdx.x % LANES;
+  bool ours = false;   // somebody's row
+  for (int s = lane; s < a.batch.n; s += LANES) ours |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1];
   const long long step = (long long)a.batch.m * a.n_q_heads;
-  float m = -INFINITY, l = 0.f;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[s * step + i].x);
-  const float base = m == -INFINITY ? 0.f : m;
-  ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * step + i];
-    if (ml.y == 0.f) continue;   // (its sums were not written)
-    const float f = ca_exp2(ml.x - base);
-    const ca_f32x4 v = *(const ca_f32x4 *)(a.part + (s * step + i) * HD + e0);
-    l += ml.y * f;
+  // the parts' maxima and sums, one or a few a lane
+  constexpr int EACH = MOST_SPLITS / LANES;
+  float f[EACH], l = 0.f, m = -INFINITY;
+  float2 ml[EACH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] += f == 0.f && !(fabsf(v[e]) < INFINITY) ? v[e] : v[e] * f;   // (an infinity stays one)
+  for (int j = 0; j < EACH; ++j) {
+    const int s = j * LANES + lane;
+    ml[j] = s < a.splits ? a.part_ml[s * step + i] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, ml[j].x);
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, o, LANES));
+    ours |= __shfl_xor((int)ours, o, LANES) != 0;
+  }
+  if (!ours) return;
+  const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    f[j] = ml[j].y == 0.f ? -1.f : ca_exp2(ml[j].x - base);   // (-1: its sums were not written)
+    l += ml[j].y == 0.f ? 0.f : ml[j].y * f[j];
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, LANES);
+  ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  const float *part = a.part + i * HD + e0;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+#pragma unroll 8
+    for (int s = 0; s < min(LANES, a.splits - j * LANES); ++s) {
+      const float g = __shfl(f[j], s, LANES);
+      const ca_f32x4 v = *(const ca_f32x4 *)(part + (j * LANES + s) * step * HD);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += g < 0.f ? 0.f : g == 0.f && !(fabsf(v[e]) < INFINITY) ? v[e] : v[e] * g;   // (an infinity stays one)
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   T *out = (T *)a.out + r * a.out_stride + i % a.n_q_heads * HD + e0;
-  if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(ca_pack(y[0] * inv, y[1] * inv), ca_pack(y[2] * inv, y[3] * inv));
+  if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
   else *(float4 *)out = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
   if (a.lse && e0 == 0) a.lse[i] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
 }

@@ -19,13 +19,39 @@ constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
 // larger weight, larger key; -0 as +0; every NaN above all numbers
 __device__ __forceinline__ uint32_t weight_key(float w) { return float_order_key(w + 0.f); }
 
-// What is kept, one workgroup a sequence and head.  The `need` heaviest of the slots between the first and the recent ones: the
-// key of the last of them by four digits of eight bits from the top, counted in LDS, each over the slots that
-// share the digits found so far; then one pass in slot order writes the slots above that key and the
-// first of those that have it.  Places are counts of what stays before them, so nothing depends on the order of threads.
+// What is kept, one workgroup a sequence and head, up to eight slots in a row to a thread.  The `need` heaviest of the slots between the first
+// and the recent ones: the key of the last of them by digits of 11, 11 and 10 bits from the top, counted in LDS, each over the slots that share
+// the digits found so far; then the slots above that key and the first of those that have it are written in slot
+// order.  Places are counts of what stays before them, so nothing depends on the order of threads.  Up to 8192 slots are read once.
+constexpr int EVICT_EACH = 8, EVICT_BINS = 2048;
+static_assert(EVICT_BINS == 2 * EVICT_THREADS && EVICT_WAVES == 16, "two digits a thread; waves fit a row of lanes");
+
+// sum over the threads before this one in the workgroup, and over all of them
+__device__ __forceinline__ unsigned evict_scan(unsigned v, unsigned *s_wave, unsigned &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned up = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += up;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = incl;
+  __syncthreads();
+  unsigned w = s_wave[lane & 15];
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    const unsigned up = __shfl_up(w, o, 16);
+    if ((lane & 15) >= o) w += up;
+  }
+  total = __shfl(w, 15, 64);
+  const unsigned before = __shfl(w, max(wave - 1, 0), 64);
+  return incl - v + (wave ? before : 0u);
+}
+
 __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
-  __shared__ unsigned s_count[256], s_wave[EVICT_WAVES], s_wave_ties[EVICT_WAVES], s_digit, s_before;
-  const int s = blockIdx.x / a.cache.n_kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ unsigned s_count[EVICT_BINS], s_wave[EVICT_WAVES], s_digit, s_before;
+  const int s = blockIdx.x / a.cache.n_kv_heads, tid = threadIdx.x;
   const int slots = a.batch.max_pages * a.cache.page_tokens, length = cut(a.batch.lengths[s], 0, slots);
   const float *w = a.weights + (long long)blockIdx.x * slots;
   float *w_out = a.weights_out + (long long)blockIdx.x * slots;
@@ -35,65 +61,86 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
   const bool all = length <= a.keep;
   const int lo = all ? 0 : a.first, hi = all ? 0 : length - a.recent;   // what is chosen from
   unsigned need = all ? 0u : (unsigned)(a.keep - a.first - a.recent), prefix = 0;
-  if (need > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) s_count[tid] = 0;
+  const bool some = need > 0;
+  const int each = cut((length + EVICT_THREADS - 1) / EVICT_THREADS, 1, EVICT_EACH), chunk = each * EVICT_THREADS;
+  float x[EVICT_EACH];
+  int held = -1;   // which chunk x is of
+  auto fetch = [&](int c0) {
+    if (c0 == held) return;
+    held = c0;
+#pragma unroll
+    for (int e = 0; e < EVICT_EACH; ++e) {
+      const int t = c0 + tid * each + e;
+      x[e] = e < each && t < length ? w[t] : 0.f;
+    }
+  };
+  if (some) {
+    constexpr uint32_t ZERO = 0x80000000u;   // the key of nothing, which many slots may have: counted by waves
+#pragma unroll 1
+    for (int digit = 0; digit < 3; ++digit) {
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, above = digit == 1 ? 21 : 10;
+      const unsigned mask = digit == 2 ? 1023u : 2047u;
+      s_count[2 * tid] = 0;
+      s_count[2 * tid + 1] = 0;
       __syncthreads();
-      for (int t = lo + tid; t < hi; t += EVICT_THREADS) {
-        const uint32_t key = weight_key(w[t]);
-        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_count[(key >> shift) & 255], 1u);
+      for (int c0 = 0; c0 < length; c0 += chunk) {
+        fetch(c0);
+        unsigned zeros = 0;
+#pragma unroll
+        for (int e = 0; e < EVICT_EACH; ++e) {
+          if (e < each) {
+            const int t = c0 + tid * each + e;
+            const uint32_t key = weight_key(x[e]);
+            const bool counts = t >= lo && t < hi && (digit == 0 || (key >> above) == (prefix >> above));
+            zeros += __popcll(__ballot(counts && key == ZERO));
+            if (counts && key != ZERO) atomicAdd(&s_count[(key >> shift) & mask], 1u);
+          }
+        }
+        if (zeros && (tid & 63) == 0) atomicAdd(&s_count[(ZERO >> shift) & mask], zeros);
       }
       __syncthreads();
-      if (wave == 0) {   // lane l: the digits 255 - 4 l and the three below it
-        unsigned c[4], sum = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += c[e] = s_count[255 - 4 * lane - e];
-        unsigned incl = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const unsigned up = __shfl_up(incl, o, 64);
-          if (lane >= o) incl += up;
-        }
-        unsigned before = incl - sum;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (before < need && need <= before + c[e]) { s_digit = 255 - 4 * lane - e; s_before = before; }
-          before += c[e];
-        }
-      }
+      // from the highest digit down, two a thread
+      const unsigned d0 = EVICT_BINS - 1 - 2 * tid, n0 = s_count[d0], n1 = s_count[d0 - 1];
+      unsigned total;
+      const unsigned before = evict_scan(n0 + n1, s_wave, total);
+      if (before < need && need <= before + n0) { s_digit = d0; s_before = before; }
+      else if (before + n0 < need && need <= before + n0 + n1) { s_digit = d0 - 1; s_before = before + n0; }
       __syncthreads();
       prefix |= s_digit << shift;
       need -= s_before;   // of those with this key so far
-      __syncthreads();
     }
   }
   // in slot order; `need` of the slots whose key is `prefix`
-  const bool some = !all && a.keep > a.first + a.recent;
-  unsigned base = 0, base_ties = 0;   // what stays, and slots with the key, before this round
-  for (int t0 = 0; t0 < length; t0 += EVICT_THREADS) {
-    const int t = t0 + tid;
-    const float x = t < length ? w[t] : 0.f;
-    const uint32_t key = weight_key(x);
-    const bool middle = t >= lo && t < hi, tie = some && middle && key == prefix;
-    const bool above = t < length && (!middle || (some && key > prefix));
-    const unsigned long long b_above = __ballot(above), b_tie = __ballot(tie), below = (1ull << lane) - 1;
-    if (lane == 0) { s_wave[wave] = __popcll(b_above); s_wave_ties[wave] = __popcll(b_tie); }
-    __syncthreads();
-    unsigned place = base + __popcll(b_above & below), ties = base_ties + __popcll(b_tie & below);
-    for (int v = 0; v < EVICT_WAVES; ++v) {
-      const unsigned n = s_wave[v], nt = s_wave_ties[v];
-      if (v < wave) { place += n; ties += nt; }
-      base += n;
-      base_ties += nt;
+  unsigned base = 0, base_ties = 0;   // what stays for sure, and slots with the key, before this chunk
+  for (int c0 = 0; c0 < length; c0 += chunk) {
+    fetch(c0);
+    unsigned above = 0, tie = 0;   // bits
+#pragma unroll
+    for (int e = 0; e < EVICT_EACH; ++e) {
+      const int t = c0 + tid * each + e;
+      const uint32_t key = weight_key(x[e]);
+      const bool middle = t >= lo && t < hi, there = e < each && t < length;
+      if (there && (!middle || (some && key > prefix))) above |= 1u << e;
+      if (there && some && middle && key == prefix) tie |= 1u << e;
     }
-    place += min(ties, need);
-    if (above || (tie && ties < need)) {
-      kept[place] = t;
-      w_out[place] = x;   // (place <= t, and all threads have read their slot)
+    unsigned total;
+    const unsigned before = evict_scan(__popc(above) | __popc(tie) << 16, s_wave, total);   // (8192 at most of each)
+    unsigned ties = base_ties + (before >> 16), place = base + (before & 0xffffu) + min(ties, need);
+#pragma unroll
+    for (int e = 0; e < EVICT_EACH; ++e) {
+      const bool is_tie = (tie >> e) & 1;
+      if (((above >> e) & 1) || (is_tie && ties < need)) {
+        kept[place] = c0 + tid * each + e;
+        w_out[place] = x[e];   // (place is at most the slot, and all threads have read theirs)
+        ++place;
+      }
+      ties += is_tie;
     }
-    __syncthreads();
+    base += total & 0xffffu;
+    base_ties += total >> 16;
   }
   for (int t = left + tid; t < a.keep; t += EVICT_THREADS) kept[t] = -1;
+  __syncthreads();
   for (int t = left + tid; t < length; t += EVICT_THREADS) w_out[t] = 0.f;
 }
 

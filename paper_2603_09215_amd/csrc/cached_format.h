@@ -26,6 +26,13 @@ struct Sequence {
   __device__ __forceinline__ int slot(int row) const { return length - rows + row; }   // negative: none
 };
 
+typedef __attribute__((ext_vector_type(2))) __bf16 ca_bf16x2;
+typedef __attribute__((ext_vector_type(2))) float ca_f32x2;
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {   // half to even, one instruction
+  const ca_f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, ca_bf16x2));
+}
+
 __device__ __forceinline__ int cut(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 __device__ __forceinline__ Sequence sequence(const BatchView &b, int s, int page_tokens) {

@@ -66,8 +66,8 @@ AttendPlan attend_plan(const spark_cache *c, const spark_cache_batch *b, int32_t
   // (every sequence adds at most one tile that is not full)
   p.tiles = std::min(m * ((group + p.pairs - 1) / p.pairs), m * group / p.pairs + b->n);
   const long long wgs = p.tiles * c->n_kv_heads;
-  const int piece = p.pairs <= 32 ? 128 : 256;   // the fewest tokens that are worth a part
-  p.splits = (int)std::max<long long>(1, std::min<long long>({slots / piece, (p.pairs <= 32 ? 4 : 1) * n_cu / wgs, 64}));
+  const int piece = p.pairs <= 32 ? 32 : 64;
+  p.splits = (int)std::max<long long>(1, std::min<long long>({(long long)std::sqrt(2.0 * slots / piece), (p.pairs <= 32 ? 2 : 1) * n_cu / wgs, MOST_SPLITS}));
   return p;
 }
 size_t attend_workspace(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, const AttendPlan &p) {
@@ -132,7 +132,7 @@ int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch,
   a.rows = batch->m >= 2048 ? 4 : 1;
   a.heads_per_wg = a.rows > 1 ? heads : 16;
   const dim3 grid((batch->m + a.rows - 1) / a.rows, (heads + a.heads_per_wg - 1) / a.heads_per_wg);
-  const size_t lds = sizeof(float) * a.rows * std::max(2, a.rotary);
+  const size_t lds = sizeof(float) * a.rows * a.rotary;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;

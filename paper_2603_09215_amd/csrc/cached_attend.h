@@ -5,8 +5,8 @@
 // over the slots t that a row sees, in one pass with a running maximum and sum.  The (row, query head) pairs of a sequence and kv
 // head share its keys and values; they are counted through, pair p being row p / group and head p mod group, and cut into tiles.
 //
-//   cached_stream_k  up to 16 or 32 pairs: bound by the cache's way through memory.  Each wave has its own tokens.
-//   cached_tile_k    128 or 256 pairs: bound by the matrix units.  A tile of keys and values in LDS serves all waves.
+//   cached_stream_k  16 pairs: bound by the cache's way through memory.  Each wave has its own tokens.
+//   cached_tile_k    128 or 256 pairs, bf16: bound by the matrix units.  A tile of keys and values in LDS serves all waves.
 //   cached_join_k    where too few tiles would leave compute units idle, their tokens are cut into `splits` parts, whose
 //                    unfinished sums come through the workspace; this adds them up in order.
 //
@@ -19,6 +19,7 @@
 // them get from them is added at the end (a probability is positive: infinity stays, NaN too).
 #pragma once
 #include "cached_format.h"
+#include "cached_plan.h"
 
 namespace spark {
 
@@ -37,16 +38,17 @@ struct AttendArgs {
 };
 
 typedef __attribute__((ext_vector_type(8))) __bf16 ca_bf16x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t ca_u32x4;
 typedef __attribute__((ext_vector_type(4))) short ca_s16x4;
 typedef __attribute__((ext_vector_type(4))) float ca_f32x4;
 typedef __attribute__((ext_vector_type(16))) float ca_f32x16;
-__device__ __forceinline__ ca_bf16x8 ca_operand(const uint4 &v) { return __builtin_bit_cast(ca_bf16x8, v); }
-template <typename T> __device__ __forceinline__ uint4 ca_signed(uint4 v, uint32_t flip) {
+__device__ __forceinline__ ca_bf16x8 ca_operand(const ca_u32x4 &v) { return __builtin_bit_cast(ca_bf16x8, v); }
+template <typename T> __device__ __forceinline__ ca_u32x4 ca_signed(ca_u32x4 v, uint32_t flip) {
   const uint32_t x = sizeof(T) == 4 ? flip : flip | (flip >> 16);
-  return make_uint4(v.x ^ x, v.y ^ x, v.z ^ x, v.w ^ x);
+  return ca_u32x4{v.x ^ x, v.y ^ x, v.z ^ x, v.w ^ x};
 }
 // elements that are no numbers to zero; true if there was one
-template <typename T> __device__ __forceinline__ bool ca_only_numbers(uint4 &v) {
+template <typename T> __device__ __forceinline__ bool ca_only_numbers(ca_u32x4 &v) {
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
   bool bad = false;
 #pragma unroll
@@ -58,7 +60,7 @@ template <typename T> __device__ __forceinline__ bool ca_only_numbers(uint4 &v) 
       if ((w[i] & 0x7f80u) == 0x7f80u) { w[i] &= 0xffff0000u; bad = true; }
     }
   }
-  v = make_uint4(w[0], w[1], w[2], w[3]);
+  v = ca_u32x4{w[0], w[1], w[2], w[3]};
   return bad;
 }
 __device__ __forceinline__ float ca_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -121,223 +123,220 @@ __device__ __forceinline__ int last_seen(const Sequence &q, int row, int causal)
 
 // the page of each 16 slots from slot 16 (first + i) on in lane i; -1 past `end` or where there is none
 __device__ __forceinline__ int pages_of(const Sequence &q, const CacheView &c, int sixteen, int end) {
-  return sixteen * 16 < end ? page_of(q, sixteen * 16, c.page_tokens, c.n_pages) : -1;
+  if (sixteen * 16 >= end) return -1;
+  int index, token;
+  place_of(c, sixteen, index, token);
+  const int p = q.pages[index];
+  return (unsigned)p < (unsigned)c.n_pages ? p : -1;
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ void write_result(const AttendArgs &a, int r, int h, int e0, ca_f32x4 y, float m, float l) {
+  y *= l == 0.f ? 0.f : 1.0f / l;
+  T *out = (T *)a.out + r * a.out_stride + (long long)h * HD + e0;
+  if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+  else *(ca_f32x4 *)out = y;
+  if (a.lse && e0 == 0) a.lse[(long long)r * a.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+}
+// four elements of a row and head: the result, or with more parts than one what it is joined from (m: maximum, l: sum)
+template <typename T, int HD>
+__device__ __forceinline__ void finish(const AttendArgs &a, int split, int r, int h, int e0, ca_f32x4 y, float m, float l) {
+  const long long i = (long long)r * a.n_q_heads + h;
+  if (a.splits > 1) {
+    const long long at = (long long)split * a.batch.m * a.n_q_heads + i;
+    *(ca_f32x4 *)(a.part + at * HD + e0) = y;
+    if (e0 == 0) a.part_ml[at] = make_float2(m, l);
+    return;
+  }
+  write_result<T, HD>(a, r, h, e0, y, m, l);
 }
 
 // ------------------------------------------------------------------ few pairs
 
-// NB blocks of 16 pairs; four waves, each with every fourth piece of TOKENS tokens of the workgroup's.  Matrix instructions of 16 x 16:
+// Tiles of 16 pairs; four waves, each with every fourth piece of TOKENS tokens of the workgroup's.  Matrix instructions of 16 x 16:
 //   A of the scores: a lane's token is l mod 16, its k values come straight from the cache, 16 bytes a load;
 //   A of the values: bf16 through LDS of the wave's own, read transposed; fp32 straight from the cache.
 // The next piece's loads are on their way while a piece is worked on.
-template <typename T, int HD, int NB> struct Stream {
-  static constexpr int WAVES = 4, TOKENS = sizeof(T) == 2 ? 32 : 16, BLOCKS = TOKENS / 16;
-  static constexpr int STEPS = HD * (int)sizeof(T) / 64;           // 16-byte loads of a lane for 16 tokens' keys
-  static constexpr int V_LOADS = sizeof(T) == 2 ? TOKENS * HD / 512 : HD / 4;   // of a lane: 16 bytes, fp32: four
+template <typename T, int HD> struct Stream {
+  static constexpr int PAIRS = 16, WAVES = 4, TOKENS = sizeof(T) == 2 ? 32 : 16, BLOCKS = TOKENS / 16;
+  static constexpr int STEPS = HD * (int)sizeof(T) / 64;                        // 16-byte loads of a lane for 16 tokens' keys
+  static constexpr int V_LOADS = HD * TOKENS * (int)sizeof(T) / 1024;           // of a lane for a piece's values, 16 bytes in all
   static constexpr int V_BYTES = sizeof(T) == 2 ? TOKENS * HD * 2 : 0;          // of LDS, a wave's
   static constexpr int O_PITCH = HD + 4;
-  static constexpr size_t LDS = WAVES * V_BYTES > (int)sizeof(float) * WAVES * 16 * O_PITCH ? WAVES * V_BYTES : sizeof(float) * WAVES * 16 * O_PITCH;
+  static constexpr size_t LDS = sizeof(float) * WAVES * PAIRS * O_PITCH;
+  static_assert(LDS >= (size_t)WAVES * V_BYTES, "values and sums share it");
 };
 
-template <typename T, int HD, int NB>
-__global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
-  using S = Stream<T, HD, NB>;
+template <typename T, int HD>
+__global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
+  using S = Stream<T, HD>;
   constexpr bool BF = sizeof(T) == 2;
   extern __shared__ uint4 ca_smem[];
-  __shared__ float s_max[S::WAVES][NB * 16], s_sum[S::WAVES][NB * 16];
+  __shared__ float s_max[S::WAVES][S::PAIRS], s_sum[S::WAVES][S::PAIRS];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
   const int nkv = a.cache.n_kv_heads, kvh = blockIdx.x % nkv, split = blockIdx.x / nkv % a.splits;
   Sequence seq;
   int tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, NB * 16, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
-  const int pair0 = tile * NB * 16, pairs = min(NB * 16, seq.rows * a.group - pair0);
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
+  const int pair0 = tile * S::PAIRS, pairs = min(S::PAIRS, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
   const int first = split * share, stop = min(all, first + share);   // pieces
   if (threadIdx.x == 0) s_bad = 0;
 
-  uint4 q[NB][S::STEPS];
-  int limit[NB];
+  // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
+  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, piece * S::BLOCKS + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
+  int piece = first + wave;
+  int pages = pages_at(piece), next_pages = pages_at(piece + S::WAVES);
+  const int mine = pair0 + min(col, pairs - 1), my_row = mine / a.group;   // (pairs past the last: that one, not written)
+  const int limit = last_seen(seq, my_row, a.causal);
+  ca_u32x4 q[S::STEPS];
+  {
+    const T *at = (const T *)a.q + (seq.row0 + my_row) * a.q_stride + (long long)(kvh * a.group + mine % a.group) * HD;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int p = pair0 + min(b * 16 + col, pairs - 1), row = p / a.group;   // (pairs past the last: that one, not written)
-    limit[b] = last_seen(seq, row, a.causal);
-    const T *at = (const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)(kvh * a.group + p % a.group) * HD;
-#pragma unroll
-    for (int i = 0; i < S::STEPS; ++i) q[b][i] = ca_signed<T>(((const uint4 *)at)[4 * i + quad], a.flip);
+    for (int i = 0; i < S::STEPS; ++i) q[i] = ca_signed<T>(((const ca_u32x4 *)at)[4 * i + quad], a.flip);
   }
-  ca_f32x4 o[NB][HD / 16];
-  float top[NB], sum[NB];
+  ca_f32x4 o[HD / 16];
+  float top = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    top[b] = -INFINITY;
-    sum[b] = 0.f;
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[b][d] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < HD / 16; ++d) o[d] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
 
-  uint4 kr[S::BLOCKS][S::STEPS];
-  uint4 vr[BF ? S::V_LOADS : S::V_LOADS / 4];
+  ca_u32x4 kr[S::BLOCKS][S::STEPS], vr[S::V_LOADS];
   char *s_v = (char *)ca_smem + wave * S::V_BYTES;
   constexpr int LPT = HD / 8;   // bf16: lanes a token's values take
-  auto load_keys = [&](int piece, int pages) {
+  auto load_keys = [&](int piece, int pages) {   // (where there is no page: from the first, of no account)
 #pragma unroll
     for (int i = 0; i < S::BLOCKS; ++i) {
-      const int page = __builtin_amdgcn_readlane(pages, i), in = (piece * S::TOKENS + 16 * i) % a.cache.page_tokens;
-      if (page >= 0) {
-        const uint4 *k = (const uint4 *)(a.cache.plane<T>(page, 0, kvh) + (in + col) * HD) + quad;
+      int index, in;
+      place_of(a.cache, piece * S::BLOCKS + i, index, in);
+      const ca_u32x4 *k = (const ca_u32x4 *)(a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, i), 0), 0, kvh) + (in + col) * HD) + quad;
 #pragma unroll
-        for (int e = 0; e < S::STEPS; ++e) kr[i][e] = k[4 * e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < S::STEPS; ++e) kr[i][e] = make_uint4(0, 0, 0, 0);
-      }
+      for (int e = 0; e < S::STEPS; ++e) kr[i][e] = k[4 * e];
     }
   };
   auto load_values = [&](int piece, int pages) {
 #pragma unroll
     for (int i = 0; i < S::BLOCKS; ++i) {
-      const int page = __builtin_amdgcn_readlane(pages, i), in = (piece * S::TOKENS + 16 * i) % a.cache.page_tokens;
-      const T *v = a.cache.plane<T>(max(page, 0), 1, kvh) + in * HD;
+      int index, in;
+      place_of(a.cache, piece * S::BLOCKS + i, index, in);
+      const T *v = a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, i), 0), 1, kvh) + in * HD;
       if constexpr (BF) {
         constexpr int EACH = S::V_LOADS / S::BLOCKS;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) vr[i * EACH + e] = page >= 0 ? ((const uint4 *)v)[e * 64 + lane] : make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < EACH; ++e) vr[i * EACH + e] = ((const ca_u32x4 *)v)[e * 64 + lane];
       } else {
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) {
-          uint32_t w[4];
+        for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = page >= 0 ? ((const uint32_t *)v)[(4 * quad + e) * HD + 16 * d + col] : 0u;
-          vr[d] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+          for (int e = 0; e < 4; ++e) vr[d][e] = ((const uint32_t *)v)[(4 * quad + e) * HD + 16 * d + col];
       }
     }
   };
-  // values behind `least`
-  auto clean = [&](int piece) {
+  // values behind `least`, and of no page
+  auto clean = [&](int piece, unsigned here) {
     const int t0 = piece * S::TOKENS;
     bool bad = false;
     if constexpr (BF) {
 #pragma unroll
       for (int e = 0; e < S::V_LOADS; ++e) {
-        const int t = t0 + (e * 64 + lane) / LPT;
-        if (t >= end) vr[e] = make_uint4(0, 0, 0, 0);
-        else if (t > least) bad |= ca_only_numbers<T>(vr[e]);
+        const int in = (e * 64 + lane) / LPT;
+        if (t0 + in >= end || !((here >> (in / 16)) & 1)) vr[e] = ca_u32x4{0, 0, 0, 0};
+        else if (t0 + in > least) bad |= ca_only_numbers<T>(vr[e]);
       }
     } else {
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) {
-        uint32_t w[4] = {vr[d].x, vr[d].y, vr[d].z, vr[d].w};
+      for (int e = 0; e < 4; ++e) {
+        const int t = t0 + 4 * quad + e;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = t0 + 4 * quad + e;
-          const bool none = (w[e] & 0x7f800000u) == 0x7f800000u;
-          bad |= none && t > least && t < end;
-          if (t >= end || (none && t > least)) w[e] = 0u;
+        for (int d = 0; d < HD / 16; ++d) {
+          const bool none = (vr[d][e] & 0x7f800000u) == 0x7f800000u;
+          bad |= none && t > least && t < end && here;
+          if (t >= end || !here || (none && t > least)) vr[d][e] = 0u;
         }
-        vr[d] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
     if (bad) s_bad = 1;
   };
 
-  constexpr int PER16 = S::TOKENS / 16;
-  // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
-  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, piece * PER16 + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
-  int piece = first + wave;
-  int pages = pages_at(piece), next_pages = pages_at(piece + S::WAVES);
   if (piece < stop) {
     load_keys(piece, pages);
     load_values(piece, pages);
   }
   __syncthreads();   // (s_bad)
   for (; piece < stop; piece += S::WAVES) {
-    const unsigned now = (unsigned)__ballot(pages >= 0) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
+    const unsigned here = (unsigned)__ballot(pages >= 0) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
     const int t0 = piece * S::TOKENS;
-    ca_f32x4 sc[NB][S::BLOCKS];
+    ca_f32x4 sc[S::BLOCKS];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int i = 0; i < S::BLOCKS; ++i) {
+      sc[i] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < S::BLOCKS; ++i) {
-        sc[b][i] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int e = 0; e < S::STEPS; ++e) {
+        if constexpr (BF) {
+          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ca_operand(kr[i][e]), ca_operand(q[e]), sc[i], 0, 0, 0);
+        } else {
+          const ca_f32x4 k = __builtin_bit_cast(ca_f32x4, kr[i][e]), x = __builtin_bit_cast(ca_f32x4, q[e]);
 #pragma unroll
-        for (int e = 0; e < S::STEPS; ++e) {
-          if constexpr (BF) {
-            sc[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ca_operand(kr[i][e]), ca_operand(q[b][e]), sc[b][i], 0, 0, 0);
-          } else {
-            const float4 k = __builtin_bit_cast(float4, kr[i][e]), x = __builtin_bit_cast(float4, q[b][e]);
-            sc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x, x.x, sc[b][i], 0, 0, 0);
-            sc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.y, x.y, sc[b][i], 0, 0, 0);
-            sc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.z, x.z, sc[b][i], 0, 0, 0);
-            sc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w, x.w, sc[b][i], 0, 0, 0);
-          }
+          for (int j = 0; j < 4; ++j) sc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], x[j], sc[i], 0, 0, 0);
         }
       }
+    }
     pages = next_pages;
     if (piece + S::WAVES < stop) {
       next_pages = pages_at(piece + 2 * S::WAVES);
       load_keys(piece + S::WAVES, pages);
     }
-    if (t0 + S::TOKENS - 1 > least) clean(piece);
-    uint4 va[BF ? 1 : HD / 16];
+    const bool masked = t0 + S::TOKENS - 1 > least || here != (1u << S::BLOCKS) - 1;
+    if (masked) {
+      clean(piece, here);
+#pragma unroll
+      for (int i = 0; i < S::BLOCKS; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t0 + 16 * i + 4 * quad + e > limit || !((here >> i) & 1)) sc[i][e] = -INFINITY;
+    }
+    ca_f32x4 va[BF ? 1 : S::V_LOADS];
     if constexpr (BF) {
 #pragma unroll
       for (int e = 0; e < S::V_LOADS; ++e) {
         const int t = (e * 64 + lane) / LPT, c = lane % LPT;
-        *(uint4 *)(s_v + t * HD * 2 + ((c ^ ca_turn<T, HD>(t)) << 4)) = vr[e];
+        *(ca_u32x4 *)(s_v + t * HD * 2 + ((c ^ ca_turn<T, HD>(t)) << 4)) = vr[e];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     } else {
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) va[d] = vr[d];
+      for (int d = 0; d < S::V_LOADS; ++d) va[d] = __builtin_bit_cast(ca_f32x4, vr[d]);
     }
     if (piece + S::WAVES < stop) load_values(piece + S::WAVES, pages);
-    const bool masked = t0 + S::TOKENS - 1 > least || now != (1u << S::BLOCKS) - 1;
+
+    float big = -INFINITY;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (masked) {
+    for (int i = 0; i < S::BLOCKS; ++i)
 #pragma unroll
-        for (int i = 0; i < S::BLOCKS; ++i)
+      for (int e = 0; e < 4; ++e) big = fmaxf(big, sc[i][e]);
+    big = fmaxf(big, __shfl_xor(big, 16, 64));
+    big = ca_max_halves(big) * a.factor;
+    // a pair's maximum follows once it is 2^8 behind: sums in fp32 have room for that
+    const bool behind = big > top + 8.f;
+    if (__any(behind)) {
+      const float up = behind ? big : top, f = ca_exp2(top - (up == -INFINITY ? 0.f : up));
+      top = up;
+      sum *= f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (t0 + 16 * i + 4 * quad + e > limit[b] || !((now >> i) & 1)) sc[b][i][e] = -INFINITY;
-      }
-      float big = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < S::BLOCKS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) big = fmaxf(big, sc[b][i][e]);
-      big = fmaxf(big, __shfl_xor(big, 16, 64));
-      big = ca_max_halves(big) * a.factor;
-      // a pair's maximum follows once it is 2^8 behind: sums in fp32 have room for that
-      const bool behind = big > top[b] + 8.f;
-      if (__any(behind)) {
-        const float up = behind ? big : top[b], f = ca_exp2(top[b] - (up == -INFINITY ? 0.f : up));
-        top[b] = up;
-        sum[b] *= f;
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[b][d][e] *= f;
-      }
-      const float base = top[b] == -INFINITY ? 0.f : top[b];
-#pragma unroll
-      for (int i = 0; i < S::BLOCKS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[b][i][e] = ca_exp2(fmaf(sc[b][i][e], a.factor, -base));
-          sum[b] += sc[b][i][e];
-        }
+      for (int d = 0; d < HD / 16; ++d) o[d] *= f;
     }
-    if constexpr (BF) {
-      ca_bf16x8 p[NB];
+    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-        p[b] = ca_operand(make_uint4(pack_bf16(sc[b][0][0], sc[b][0][1]), pack_bf16(sc[b][0][2], sc[b][0][3]), pack_bf16(sc[b][1][0], sc[b][1][1]),
-                                     pack_bf16(sc[b][1][2], sc[b][1][3])));
+    for (int i = 0; i < S::BLOCKS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sc[i][e] = ca_exp2(fmaf(sc[i][e], a.factor, -base));
+        sum += sc[i][e];
+      }
+    if constexpr (BF) {
+      const ca_bf16x8 p = ca_operand(ca_u32x4{pack_bf16(sc[0][0], sc[0][1]), pack_bf16(sc[0][2], sc[0][3]), pack_bf16(sc[1][0], sc[1][1]), pack_bf16(sc[1][2], sc[1][3])});
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
         union { ca_s16x4 h[2]; ca_bf16x8 v; } x;
@@ -347,103 +346,81 @@ __global__ void __launch_bounds__(256) cached_stream_k(AttendArgs a) {
           x.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
               (__attribute__((address_space(3))) ca_s16x4 *)(s_v + t * HD * 2 + ((c ^ ca_turn<T, HD>(t)) << 4) + 8 * (col & 1)));
         }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, p[b], o[b][d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, p, o[d], 0, 0, 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     } else {
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) {
-        const float4 v = __builtin_bit_cast(float4, va[d]);
+      for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          o[b][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x, sc[b][0][0], o[b][d], 0, 0, 0);
-          o[b][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.y, sc[b][0][1], o[b][d], 0, 0, 0);
-          o[b][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.z, sc[b][0][2], o[b][d], 0, 0, 0);
-          o[b][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w, sc[b][0][3], o[b][d], 0, 0, 0);
-        }
-      }
+        for (int j = 0; j < 4; ++j) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(va[d][j], sc[0][j], o[d], 0, 0, 0);
     }
   }
 
   // the waves' sums brought to one maximum and added in order
   float *s_o = (float *)ca_smem;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    sum[b] += __shfl_xor(sum[b], 16, 64);
-    sum[b] = ca_sum_halves(sum[b]);
-    if (quad == 0) { s_max[wave][b * 16 + col] = top[b]; s_sum[wave][b * 16 + col] = sum[b]; }
-  }
+  sum += __shfl_xor(sum, 16, 64);
+  sum = ca_sum_halves(sum);
+  if (quad == 0) { s_max[wave][col] = top; s_sum[wave][col] = sum; }
   __syncthreads();   // (and every wave is done with its values)
-  const bool bad = s_bad != 0;
+  auto most = [&](int c) {
+    float m = s_max[0][c];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    float most = -INFINITY;
+    for (int w = 1; w < S::WAVES; ++w) m = fmaxf(m, s_max[w][c]);
+    return m;
+  };
+  {
+    const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
 #pragma unroll
-    for (int w = 0; w < S::WAVES; ++w) most = fmaxf(most, s_max[w][b * 16 + col]);
-    const float f = ca_exp2(top[b] - (most == -INFINITY ? 0.f : most));
+    for (int d = 0; d < HD / 16; ++d) *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = o[d] * f;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < pairs * (HD / 4); i += 64 * S::WAVES) {
+    const int c = i / (HD / 4), e0 = i % (HD / 4) * 4, p = pair0 + c;
+    const float m = most(c);
+    float l = 0.f;
+    ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) *(ca_f32x4 *)(s_o + (wave * 16 + col) * S::O_PITCH + 16 * d + 4 * quad) = o[b][d] * f;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * HD / 4; i += 64 * S::WAVES) {
-      const int c = i / (HD / 4), e0 = i % (HD / 4) * 4, p = pair0 + b * 16 + c;
-      if (b * 16 + c >= pairs) break;
-      float m = -INFINITY, l = 0.f;
+    for (int w = 0; w < S::WAVES; ++w) {
+      l += s_sum[w][c] * ca_exp2(s_max[w][c] - (m == -INFINITY ? 0.f : m));
+      y += *(const ca_f32x4 *)(s_o + (w * S::PAIRS + c) * S::O_PITCH + e0);
+    }
+    const int row = p / a.group, r = seq.row0 + row, h = kvh * a.group + p % a.group;
+    if (s_bad) {
+      const int last = min(last_seen(seq, row, a.causal), stop * S::TOKENS - 1);
+      for (int t = max(first * S::TOKENS, least + 1); t <= last; ++t) {
+        const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
+        if (page < 0) continue;
 #pragma unroll
-      for (int w = 0; w < S::WAVES; ++w) m = fmaxf(m, s_max[w][b * 16 + c]);
-      ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < S::WAVES; ++w) {
-        l += s_sum[w][b * 16 + c] * ca_exp2(s_max[w][b * 16 + c] - (m == -INFINITY ? 0.f : m));
-        y += *(const ca_f32x4 *)(s_o + (w * 16 + c) * S::O_PITCH + e0);
-      }
-      const int row = p / a.group, r = seq.row0 + row, h = kvh * a.group + p % a.group;
-      if (bad) {
-        const int last = last_seen(seq, row, a.causal);
-        for (int t = max(first * S::TOKENS, least + 1); t <= min(last, stop * S::TOKENS - 1); ++t) {
-          const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
-          if (page < 0) continue;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = Elem<T>::widen(a.cache.plane<T>(page, 1, kvh)[t % a.cache.page_tokens * HD + e0 + e]);
-            if (!(fabsf(v) < INFINITY)) y[e] += v;
-          }
+        for (int e = 0; e < 4; ++e) {
+          const float v = Elem<T>::widen(a.cache.plane<T>(page, 1, kvh)[t % a.cache.page_tokens * HD + e0 + e]);
+          if (!(fabsf(v) < INFINITY)) y[e] += v;
         }
       }
-      if (a.splits > 1) {
-        const long long at = ((long long)split * a.batch.m + r) * a.n_q_heads + h;
-        *(ca_f32x4 *)(a.part + at * HD + e0) = y;
-        if (e0 == 0) a.part_ml[at] = make_float2(m, l);
-      } else {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        T *out = (T *)a.out + r * a.out_stride + (long long)h * HD + e0;
-        if constexpr (BF) *(uint2 *)out = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
-        else *(float4 *)out = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-        if (a.lse && e0 == 0) a.lse[(long long)r * a.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
-      }
     }
-    __syncthreads();
+    finish<T, HD>(a, split, r, h, e0, y, m, l);
   }
 }
 
 // ------------------------------------------------------------------ many pairs
 
-// WAVES waves of 32 pairs each; tiles of 64 tokens' keys and values in LDS, two of them, so that the next one's loads run while one is
+// WAVES waves of 32 pairs each, bf16; tiles of 64 tokens' keys and values in LDS, two of them, so that the next one's loads run while one is
 // worked on.  Matrix instructions of 32 x 32 (A: a lane's token or head element is l mod 32, its k those of l / 32); a lane
-// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.
-template <typename T, int HD, int WAVES> struct Tile {
+// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.  (fp32's matrix instructions
+// take so long that the stream keeps up: such a kernel took 339 us against 361 for 2000 rows of 28 heads, 106 against 101 for 16 heads of 64.)
+template <int HD, int WAVES> struct Tile {
   static constexpr int TOKENS = 64, PAIRS = 32 * WAVES;
-  static constexpr int ROW = HD * (int)sizeof(T), LPT = ROW / 16;                   // bytes of a token, lanes that they take
+  static constexpr int ROW = HD * (int)sizeof(bf16_t), LPT = ROW / 16;                   // bytes of a token, lanes that they take
   static constexpr int PER = 64 * WAVES / LPT, LOADS = TOKENS / PER;                // tokens of a pass of loads, passes
   static constexpr int BYTES = TOKENS * ROW;
   static constexpr size_t LDS = 4 * (size_t)BYTES;                                  // keys and values, two buffers
 };
 
-template <typename T, int HD, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 512 ? 1 : 2) cached_tile_k(AttendArgs a) {
-  using S = Tile<T, HD, WAVES>;
-  constexpr bool BF = sizeof(T) == 2;
+template <int HD, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
+  using T = bf16_t;
+  using S = Tile<HD, WAVES>;
   constexpr int STEPS = HD * (int)sizeof(T) / 32;   // 16-byte pieces of a query that a lane holds
   extern __shared__ uint4 ca_smem[];
   __shared__ int s_bad;
@@ -464,164 +441,187 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
   const int limit = last_seen(seq, row, a.causal);
   const int wave_least = last_seen(seq, (pair0 + min(wave * 32, pairs - 1)) / a.group, a.causal);
   const int wave_most = last_seen(seq, (pair0 + min(wave * 32 + 31, pairs - 1)) / a.group, a.causal);
-  uint4 q[STEPS];
+  ca_u32x4 q[STEPS];
   {
     const T *at = (const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)(kvh * a.group + p % a.group) * HD;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) q[i] = ca_signed<T>(((const uint4 *)at)[2 * i + half], a.flip);
+    for (int i = 0; i < STEPS; ++i) q[i] = ca_signed<T>(((const ca_u32x4 *)at)[2 * i + half], a.flip);
   }
 
   char *lds = (char *)ca_smem;
   const int st = threadIdx.x / S::LPT, sc16 = threadIdx.x % S::LPT;   // this thread's token in a pass, and 16 bytes of it
-  uint4 kr[S::LOADS], vr[S::LOADS];
+  ca_u32x4 kr[S::LOADS], vr[S::LOADS];
   // the pages of a tile's four 16s in lanes 0..3
   auto pages_at = [&](int t) { return pages_of(seq, a.cache, 4 * t + (lane & 3), t < stop ? end : 0); };
-  auto load = [&](int t, int pages) {
+  auto load = [&](int t, int pages, int which, ca_u32x4 (&to)[S::LOADS]) {   // (where there is no page: from the first, of no account)
 #pragma unroll
     for (int i = 0; i < S::LOADS; ++i) {
       const int token = i * S::PER + st, sixteen = __builtin_amdgcn_readfirstlane(token >> 4);   // (a wave's tokens of a pass share theirs)
-      const int page = __builtin_amdgcn_readlane(pages, sixteen), in = (t * S::TOKENS + 16 * sixteen) % a.cache.page_tokens + (token & 15);
-      if (page >= 0) {
-        kr[i] = ((const uint4 *)(a.cache.plane<T>(page, 0, kvh) + in * HD))[sc16];
-        vr[i] = ((const uint4 *)(a.cache.plane<T>(page, 1, kvh) + in * HD))[sc16];
-      } else {
-        kr[i] = make_uint4(0, 0, 0, 0);
-        vr[i] = make_uint4(0, 0, 0, 0);
-      }
+      int index, in;
+      place_of(a.cache, 4 * t + sixteen, index, in);
+      to[i] = ((const ca_u32x4 *)(a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, sixteen), 0), which, kvh) + (in + (token & 15)) * HD))[sc16];
     }
   };
-  auto store = [&](int t, int buf) {
-    if (t * S::TOKENS + S::TOKENS - 1 > least) {
-      bool bad = false;
-#pragma unroll
-      for (int i = 0; i < S::LOADS; ++i) {
-        const int token = t * S::TOKENS + i * S::PER + st;
-        if (token >= end) vr[i] = make_uint4(0, 0, 0, 0);
-        else if (token > least) bad |= ca_only_numbers<T>(vr[i]);
-      }
-      if (bad) s_bad = 1;
-    }
+  auto clean = [&](int t, unsigned here) {   // values behind `least`, and of no page
+    if (t * S::TOKENS + S::TOKENS - 1 <= least && here == 15u) return;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < S::LOADS; ++i) {
-      const int token = i * S::PER + st, at = token * S::ROW + ((sc16 ^ ca_turn<T, HD>(token)) << 4);
-      *(uint4 *)(lds + 2 * buf * S::BYTES + at) = kr[i];
-      *(uint4 *)(lds + (2 * buf + 1) * S::BYTES + at) = vr[i];
+      const int in = i * S::PER + st, token = t * S::TOKENS + in;
+      if (token >= end || !((here >> (in >> 4)) & 1)) vr[i] = ca_u32x4{0, 0, 0, 0};
+      else if (token > least) bad |= ca_only_numbers<T>(vr[i]);
+    }
+    if (bad) s_bad = 1;
+  };
+  auto store = [&](char *to, const ca_u32x4 (&from)[S::LOADS]) {
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      const int token = i * S::PER + st;
+      *(ca_u32x4 *)(to + token * S::ROW + ((sc16 ^ ca_turn<T, HD>(token)) << 4)) = from[i];
     }
   };
+  auto keys_at = [&](int t) { return lds + ((t - first) & 1) * S::BYTES; };
+  auto values_at = [&](int t) { return lds + (2 + ((t - first) & 1)) * S::BYTES; };
 
-  ca_f32x16 o[HD / 32];
+  ca_f32x16 o[HD / 32], sc[2];   // unfinished sums [head element][pair], scores [token][pair]
+  uint32_t pr[16];               // probabilities in bf16, two a register
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float top = -INFINITY, sum = 0.f;   // the sum: of this lane's tokens
 
-  int pages = pages_at(first), next_pages = pages_at(first + 1);
-  __syncthreads();   // (s_bad)
-  if (first < stop) {
-    load(first, pages);
-    store(first, 0);
-  }
-  __syncthreads();
-  for (int t = first; t < stop; ++t) {
-    const int buf = (t - first) & 1, t0 = t * S::TOKENS;
-    const unsigned here = (unsigned)__ballot(pages >= 0) & 15u;
-    pages = next_pages;
-    if (t + 1 < stop) {
-      load(t + 1, pages);
-      next_pages = pages_at(t + 2);
+  auto scores = [&](int t) {
+    const char *lk = keys_at(t) + col * S::ROW;
+    auto key = [&](int b, int i) { return *(const ca_u32x4 *)(lk + 32 * b * S::ROW + (((2 * i + half) ^ ca_turn<T, HD>(col)) << 4)); };
+    // operands are read two steps ahead of their use (the barriers hold the order: without them each read is waited for at once)
+    ca_u32x4 k[3][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) k[i][b] = key(b, i);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      if (i + 2 < STEPS)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) k[(i + 2) % 3][b] = key(b, i + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ca_operand(k[i % 3][b]), ca_operand(q[i]), sc[b], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (works && t0 <= wave_most) {
-      const char *lk = lds + 2 * buf * S::BYTES, *lv = lk + S::BYTES;
-      ca_f32x16 sc[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-          const uint4 k = *(const uint4 *)(lk + (32 * b + col) * S::ROW + (((2 * i + half) ^ ca_turn<T, HD>(col)) << 4));
-          if constexpr (BF) {
-            sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ca_operand(k), ca_operand(q[i]), sc[b], 0, 0, 0);
-          } else {
-            const float4 x = __builtin_bit_cast(float4, k), y = __builtin_bit_cast(float4, q[i]);
-            sc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, sc[b], 0, 0, 0);
-            sc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, sc[b], 0, 0, 0);
-            sc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, sc[b], 0, 0, 0);
-            sc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, sc[b], 0, 0, 0);
-          }
-        }
-      }
-      if (t0 + S::TOKENS - 1 > wave_least || here != 15u) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int token = 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
-            if (t0 + token > limit || !((here >> (2 * b + (r >> 3))) & 1)) sc[b][r] = -INFINITY;
-          }
-      }
-      float big = sc[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) big = fmaxf(big, sc[b][r]);
-      big = ca_max_halves(big) * a.factor;
-      // a pair's maximum follows once it is 2^8 behind: sums in fp32 have room for that
-      const bool behind = big > top + 8.f;
-      if (__any(behind)) {
-        const float up = behind ? big : top, f = ca_exp2(top - (up == -INFINITY ? 0.f : up));
-        top = up;
-        sum *= f;
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= f;
-      }
-      const float base = top == -INFINITY ? 0.f : top;
+  };
+  auto softmax = [&](int t, unsigned here) {
+    const int t0 = t * S::TOKENS;
+    if (t0 + S::TOKENS - 1 > wave_least || here != 15u) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          sc[b][r] = ca_exp2(fmaf(sc[b][r], a.factor, -base));
-          sum += sc[b][r];
+          const int token = 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
+          if (t0 + token > limit || !((here >> (2 * b + (r >> 3))) & 1)) sc[b][r] = -INFINITY;
         }
+    }
+    float big = sc[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) big = fmaxf(big, sc[b][r]);
+    big = ca_max_halves(big) * a.factor;
+    // a pair's maximum follows once it is 2^8 behind: sums in fp32 have room for that
+    const bool behind = big > top + 8.f;
+    if (__any(behind)) {
+      const float up = behind ? big : top, f = ca_exp2(top - (up == -INFINITY ? 0.f : up));
+      top = up;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= f;
+    }
+    const float base = top == -INFINITY ? 0.f : top;
+    float s2[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        if constexpr (BF) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {   // 16 tokens
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack_bf16(sc[b][8 * j + 2 * e], sc[b][8 * j + 2 * e + 1]);
-            const ca_bf16x8 pr = ca_operand(make_uint4(w[0], w[1], w[2], w[3]));
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d) {
-              union { ca_s16x4 h[2]; ca_bf16x8 v; } x;
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int token = 32 * b + 16 * j + 8 * i + 4 * half + ((lane >> 2) & 3), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                x.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) ca_s16x4 *)(lv + token * S::ROW + ((c ^ ca_turn<T, HD>(token)) << 4) + 8 * (lane & 1)));
-              }
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v, pr, o[d], 0, 0, 0);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int token = 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d) {
-              const int c = 8 * d + (col >> 2);
-              const float v = *(const float *)(lv + token * S::ROW + ((c ^ ca_turn<T, HD>(token)) << 4) + 4 * (col & 3));
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[b][r], o[d], 0, 0, 0);
-            }
-          }
-        }
+        sc[b][r] = ca_exp2(fmaf(sc[b][r], a.factor, -base));
+        s2[b] += sc[b][r];
+        if (r & 1) pr[8 * b + (r >> 1)] = pack_bf16(sc[b][r - 1], sc[b][r]);
       }
+    sum += s2[0] + s2[1];
+  };
+  auto values = [&](int t) {
+    const char *lv = values_at(t);
+    auto value = [&](int step, int d) {   // 16 tokens a step
+      union { ca_s16x4 h[2]; ca_bf16x8 v; } x;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int token = 16 * step + 8 * i + 4 * half + ((lane >> 2) & 3), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        x.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) ca_s16x4 *)(lv + token * S::ROW + ((c ^ ca_turn<T, HD>(token)) << 4) + 8 * (lane & 1)));
+      }
+      return x.v;
+    };
+    ca_bf16x8 v[2][HD / 32];
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) v[0][d] = value(0, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j < 3)
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) v[(j + 1) & 1][d] = value(j + 1, d);
+      __builtin_amdgcn_sched_barrier(0);
+      const ca_bf16x8 p8 = ca_operand(ca_u32x4{pr[4 * j], pr[4 * j + 1], pr[4 * j + 2], pr[4 * j + 3]});
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[j & 1][d], p8, o[d], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (t + 1 < stop) store(t + 1, buf ^ 1);
+  };
+
+  // A tile's values are followed by the next one's scores, so keys come one tile ahead of values: during tile t the buffers hold keys of t + 1
+  // (and take those of t + 2) and values of t (and take those of t + 1).
+  int pages_v = pages_at(first), pages_k = pages_at(first + 1), pages_next = pages_at(first + 2);
+  unsigned here = (unsigned)__ballot(pages_v >= 0) & 15u;
+  __syncthreads();   // (s_bad)
+  if (first < stop) {
+    load(first, pages_v, 0, kr);
+    load(first, pages_v, 1, vr);
+    store(keys_at(first), kr);
+    load(first + 1, pages_k, 0, kr);
+    clean(first, here);
+    store(values_at(first), vr);
+    store(keys_at(first + 1), kr);
+    __syncthreads();
+    scores(first);
+  }
+  __syncthreads();   // (the first tile's keys are done with)
+  for (int t = first; t < stop; ++t) {
+    pages_v = pages_k;
+    pages_k = pages_next;
+    const unsigned here_next = (unsigned)__ballot(pages_v >= 0) & 15u;
+    if (t + 1 < stop) {
+      pages_next = pages_at(t + 3);
+      load(t + 2, pages_k, 0, kr);
+      load(t + 1, pages_v, 1, vr);
+    }
+    if (works && t * S::TOKENS <= wave_most) {
+      softmax(t, here);
+      __builtin_amdgcn_s_setprio(1);   // (the other wave's exponentials give way to these matrix instructions)
+      values(t);
+      scores(t + 1);
+      __builtin_amdgcn_s_setprio(0);
+    }
+    here = here_next;
+    if (t + 1 < stop) {
+      clean(t + 1, here);
+      store(keys_at(t + 2), kr);
+      store(values_at(t + 1), vr);
+    }
     __syncthreads();
   }
 
@@ -642,27 +642,14 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && HD * sizeof(T) == 51
     }
   }
   if (!live) return;
-  const long long at = ((long long)split * a.batch.m + r0) * a.n_q_heads + h;
-  const float inv = a.splits > 1 ? 1.f : sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e0 = 32 * d + 8 * i + 4 * half;
-      const float4 y = make_float4(o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv);
-      if (a.splits > 1) *(float4 *)(a.part + at * HD + e0) = y;
-      else if constexpr (BF) *(uint2 *)((T *)a.out + r0 * a.out_stride + (long long)h * HD + e0) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-      else *(float4 *)((T *)a.out + r0 * a.out_stride + (long long)h * HD + e0) = y;
-    }
-  if (half == 0) {
-    if (a.splits > 1) a.part_ml[at] = make_float2(top, sum);
-    else if (a.lse) a.lse[(long long)r0 * a.n_q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
-  }
+    for (int i = 0; i < 4; ++i)
+      finish<T, HD>(a, split, r0, h, 32 * d + 8 * i + 4 * half, ca_f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, top, sum);
 }
 
 // ------------------------------------------------------------------ the parts together
-
-constexpr int MOST_SPLITS = 64;
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
@@ -710,11 +697,7 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
       for (int e = 0; e < 4; ++e) y[e] += g < 0.f ? 0.f : g == 0.f && !(fabsf(v[e]) < INFINITY) ? v[e] : v[e] * g;   // (an infinity stays one)
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  T *out = (T *)a.out + r * a.out_stride + i % a.n_q_heads * HD + e0;
-  if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
-  else *(float4 *)out = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-  if (a.lse && e0 == 0) a.lse[i] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+  write_result<T, HD>(a, r, (int)(i % a.n_q_heads), e0, y, m, l);
 }
 
 }  // namespace spark

@@ -9,6 +9,8 @@ struct CacheView {
   void *pool;             // of the layer: its first page's keys of head 0
   long long page_stride;  // elements
   int n_pages, n_kv_heads, page_tokens, head_dim;
+  int sixteens;           // page_tokens / 16
+  uint32_t reciprocal;    // 2^32 / sixteens rounded up, 0 for one
   // keys (which 0) or values (1) of a head in a page: [page_tokens][head_dim]
   template <typename T> __device__ __forceinline__ T *plane(int page, int which, int head) const {
     return (T *)pool + page * page_stride + (long long)(which * n_kv_heads + head) * page_tokens * head_dim;
@@ -42,6 +44,13 @@ __device__ __forceinline__ Sequence sequence(const BatchView &b, int s, int page
   q.length = cut(b.lengths[s], 0, b.max_pages * page_tokens);
   q.pages = b.table + (long long)s * b.max_pages;
   return q;
+}
+
+// Which of a sequence's pages holds its slots 16 n .. 16 n + 15, and from which of the page's tokens on.  n is below 2^20 and a page
+// has at most 2^12 sixteens, so the product with the rounded reciprocal is off by less than one sixteenth of a page: exact.
+__device__ __forceinline__ void place_of(const CacheView &c, int n, int &index, int &token) {
+  index = c.reciprocal ? (int)__umulhi((uint32_t)n, c.reciprocal) : n;
+  token = (n - index * c.sixteens) * 16;
 }
 
 // the page of a slot, -1 where there is none

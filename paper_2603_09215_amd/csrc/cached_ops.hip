@@ -40,7 +40,9 @@ bool rows_ok(const void *p, size_t align, int64_t stride, int64_t heads, const s
 
 CacheView view(const spark_cache *c) {
   const long long layer = 2ll * c->n_kv_heads * c->page_tokens * c->head_dim;
-  return CacheView{(char *)c->pool + c->layer * layer * type_bytes(c->dtype), layer * c->n_layers, c->n_pages, c->n_kv_heads, c->page_tokens, c->head_dim};
+  const uint32_t sixteens = c->page_tokens / 16;
+  return CacheView{(char *)c->pool + c->layer * layer * type_bytes(c->dtype), layer * c->n_layers, c->n_pages, c->n_kv_heads, c->page_tokens, c->head_dim,
+                   (int)sixteens, sixteens == 1 ? 0u : (uint32_t)(((1ull << 32) + sixteens - 1) / sixteens)};
 }
 BatchView view(const spark_cache_batch *b) { return BatchView{b->starts, b->lengths, b->table, b->m, b->n, b->max_pages}; }
 int status() { return hipGetLastError() == hipSuccess ? SPARK_OK : SPARK_EHIP; }
@@ -53,22 +55,8 @@ template <typename F> void by_cache(int dtype, int head_dim, F f) {
   else head_dim == 64 ? f(bf16_t{}, H64{}) : f(bf16_t{}, H128{});
 }
 
-// How attention is cut: `pairs` (row, head) pairs a tile, at most `tiles` tiles for each kv head, their tokens in `splits` parts
-struct AttendPlan {
-  int pairs, splits;
-  long long tiles;
-};
-AttendPlan attend_plan(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, int n_cu) {
-  AttendPlan p;
-  const long long group = n_q_heads / c->n_kv_heads, m = b->m, mean = std::max<long long>(1, m * group / b->n), slots = (long long)b->max_pages * c->page_tokens;
-  const bool wide = c->dtype == SPARK_DTYPE_FP32 && c->head_dim == 128;   // (queries and sums take twice the registers)
-  p.pairs = mean <= 16 ? 16 : mean <= 64 ? 32 : mean <= 128 || wide ? 128 : 256;
-  // (every sequence adds at most one tile that is not full)
-  p.tiles = std::min(m * ((group + p.pairs - 1) / p.pairs), m * group / p.pairs + b->n);
-  const long long wgs = p.tiles * c->n_kv_heads;
-  const int piece = p.pairs <= 32 ? 32 : 64;
-  p.splits = (int)std::max<long long>(1, std::min<long long>({(long long)std::sqrt(2.0 * slots / piece), (p.pairs <= 32 ? 2 : 1) * n_cu / wgs, MOST_SPLITS}));
-  return p;
+AttendPlan plan_of(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, int n_cu) {
+  return attend_plan(c->dtype == SPARK_DTYPE_FP32, c->head_dim, c->n_kv_heads, n_q_heads / c->n_kv_heads, b->m, b->n, (long long)b->max_pages * c->page_tokens, n_cu);
 }
 size_t attend_workspace(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads, const AttendPlan &p) {
   return p.splits == 1 ? 0 : (size_t)p.splits * b->m * n_q_heads * (c->head_dim + 2) * sizeof(float);
@@ -149,7 +137,7 @@ int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batc
   if (batch->m == 0 || batch->n == 0) return SPARK_OK;
   const int n_cu = compute_units();
   if (n_cu <= 0) return SPARK_EHIP;
-  *bytes = attend_workspace(cache, batch, n_q_heads, attend_plan(cache, batch, n_q_heads, n_cu));
+  *bytes = attend_workspace(cache, batch, n_q_heads, plan_of(cache, batch, n_q_heads, n_cu));
   return SPARK_OK;
 }
 
@@ -161,7 +149,7 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
   if (batch->m == 0 || batch->n == 0) return SPARK_OK;
   const int n_cu = compute_units();
   if (n_cu <= 0) return SPARK_EHIP;
-  const AttendPlan plan = attend_plan(cache, batch, n_q_heads, n_cu);
+  const AttendPlan plan = plan_of(cache, batch, n_q_heads, n_cu);
   const size_t need = attend_workspace(cache, batch, n_q_heads, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SPARK_ENOMEM;
   if (need > 0 && !aligned(workspace, 16)) return SPARK_EINVAL;
@@ -183,14 +171,11 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
     auto go = [&](auto kern, int threads, size_t lds, bool allowed) {
       if ((ok = allowed)) kern<<<grid, threads, lds, stream>>>(a);
     };
-    if (plan.pairs <= 32) {
-      if (plan.pairs == 16) go(cached_stream_k<T, HD, 1>, 256, Stream<T, HD, 1>::LDS, true);
-      else go(cached_stream_k<T, HD, 2>, 256, Stream<T, HD, 2>::LDS, true);
-    } else if (plan.pairs == 128) {
-      go(cached_tile_k<T, HD, 4>, 256, Tile<T, HD, 4>::LDS, allow_lds<cached_tile_k<T, HD, 4>>(Tile<T, HD, 4>::LDS));
-    } else if constexpr (HD * sizeof(T) < 512) {
-      go(cached_tile_k<T, HD, 8>, 512, Tile<T, HD, 8>::LDS, allow_lds<cached_tile_k<T, HD, 8>>(Tile<T, HD, 8>::LDS));
+    if constexpr (sizeof(T) == 2) {   // (fp32 has no tiles)
+      if (plan.pairs == 128) go(cached_tile_k<HD, 4>, 256, Tile<HD, 4>::LDS, allow_lds<cached_tile_k<HD, 4>>(Tile<HD, 4>::LDS));
+      else if (plan.pairs == 256) go(cached_tile_k<HD, 8>, 512, Tile<HD, 8>::LDS, allow_lds<cached_tile_k<HD, 8>>(Tile<HD, 8>::LDS));
     }
+    if (plan.pairs == 16) go(cached_stream_k<T, HD>, 256, Stream<T, HD>::LDS, true);
     if (ok && plan.splits > 1) {
       const long long vectors = (long long)batch->m * n_q_heads, each = 256 / (HD / 4);
       cached_join_k<T, HD><<<(unsigned)((vectors + each - 1) / each), 256, 0, stream>>>(a);

@@ -1,0 +1,50 @@
+// How attention over a paged cache is cut (cached_attend.h): plain arithmetic on its sizes.
+#pragma once
+#include <algorithm>
+
+namespace spark {
+
+constexpr int MOST_SPLITS = 64;
+
+// `tiles` tiles of `pairs` (row, head) pairs at most for each kv head, their tokens in `splits` parts
+struct AttendPlan {
+  int pairs, splits;
+  long long tiles;
+};
+
+// A kernel's step over `tokens` tokens: us with one workgroup to a compute unit, and with as many as there is room for
+struct AttendKind { int pairs, tokens, room; float us_one, us_full; };
+// [head_dim 128][kernel]: streams of pieces (four waves' pieces a step), tiles of four and of eight waves
+constexpr AttendKind ATTEND_BF16[2][3] = {{{16, 128, 2, 1.2f, 2.0f}, {128, 64, 2, 1.5f, 2.0f}, {256, 64, 1, 1.9f, 1.9f}},
+                                          {{16, 128, 2, 1.55f, 3.2f}, {128, 64, 2, 2.1f, 2.65f}, {256, 64, 1, 2.45f, 2.45f}}};
+constexpr AttendKind ATTEND_FP32[2] = {{16, 64, 2, 1.4f, 1.9f}, {16, 64, 2, 2.0f, 3.5f}};
+
+// The plan whose estimate is shortest: rounds of workgroups, each as many steps as its share of the slots has; parts are written, read and
+// joined by a launch of their own (4 us, 0.25 a part, and its bytes at 4 TB/s).  Slots and rows are what a call's tensors have room for: the
+// host does not know lengths, so a batch of short sequences in long tables is cut finer than it need be.  Steps' times
+// are fitted to sweeps of kernels and parts at 40 batches (1 to 64 sequences, 1 to 8191 rows, 300 to 8191 slots).
+inline AttendPlan attend_plan(bool fp32, int head_dim, int n_kv_heads, int group, int m, int n, long long slots, int n_cu) {
+  AttendPlan best{16, 1, 1};
+  float best_us = 1e30f;
+  const AttendKind *kinds = fp32 ? &ATTEND_FP32[head_dim == 128] : ATTEND_BF16[head_dim == 128];
+  for (int i = 0; i < (fp32 ? 1 : 3); ++i) {
+    const AttendKind &k = kinds[i];
+    // (every sequence adds at most one tile that is not full)
+    const long long tiles = std::min((long long)m * ((group + k.pairs - 1) / k.pairs), (long long)m * group / k.pairs + n);
+    const float all = (float)(tiles * n_kv_heads), steps = (float)((slots + k.tokens - 1) / k.tokens);
+    const float part_us = 0.25f + (float)m * group * n_kv_heads * head_dim * 8.0f / 4e6f;
+    for (int s = 1; s <= MOST_SPLITS && (s == 1 || s <= steps); ++s) {
+      const float wgs = all * s, load = std::min(1.0f, std::max(0.0f, wgs / n_cu - 1.0f));
+      const float rounds = std::max(1.0f, wgs / (k.room * n_cu));
+      const float us = rounds * (float)(long long)((steps + s - 1) / s) * (k.us_one + (k.us_full - k.us_one) * load) +
+                       (s > 1 ? 4.0f + s * part_us : 0.0f);
+      if (us < best_us) {
+        best_us = us;
+        best = AttendPlan{k.pairs, s, tiles};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace spark

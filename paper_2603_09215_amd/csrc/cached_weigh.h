@@ -40,12 +40,13 @@ __global__ void __launch_bounds__(256) cached_weigh_k(WeighArgs a) {
     // (a wave past the length works on nothing, and comes to the barriers)
     const int pages = pages_of(seq, a.cache, t0 / 16 + (lane & 1), seq.length);
     const unsigned here = (unsigned)__ballot(pages >= 0) & 3u;
-    uint4 k[STEPS];
+    ca_u32x4 k[STEPS];
     {
-      const int page = max(__shfl(pages, col >> 4, 64), 0), in = (t0 + 16 * (col >> 4)) % a.cache.page_tokens + (col & 15);
-      const uint4 *at = (const uint4 *)(a.cache.plane<T>(page, 0, kvh) + in * HD);
+      int index, in;
+      place_of(a.cache, t0 / 16 + (col >> 4), index, in);
+      const ca_u32x4 *at = (const ca_u32x4 *)(a.cache.plane<T>(max(__shfl(pages, col >> 4, 64), 0), 0, kvh) + (in + (col & 15)) * HD);
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) k[i] = here ? at[2 * i + half] : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < STEPS; ++i) k[i] = here ? at[2 * i + half] : ca_u32x4{0, 0, 0, 0};
     }
     float total = 0.f;
     for (int b = wave % a.way; b < blocks; b += a.way) {
@@ -53,9 +54,9 @@ __global__ void __launch_bounds__(256) cached_weigh_k(WeighArgs a) {
       if (t0 > last || !here) continue;
       const int p = min(b * 32 + col, pairs - 1), row = p / a.group, h = kvh * a.group + p % a.group;
       const T *at = (const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)h * HD;
-      uint4 q[STEPS];
+      ca_u32x4 q[STEPS];
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) q[i] = ca_signed<T>(((const uint4 *)at)[2 * i + half], a.flip);
+      for (int i = 0; i < STEPS; ++i) q[i] = ca_signed<T>(((const ca_u32x4 *)at)[2 * i + half], a.flip);
       const float lse = a.lse[(long long)(seq.row0 + row) * a.n_q_heads + h];
       const bool none = b * 32 + col >= pairs || lse == -INFINITY;
       if (half == 0) {

@@ -33,21 +33,35 @@ def _table(t, what: str, dims: int):
 
 def _heads(t, what: str, head_dim: int, dtypes, shape=None):
     """(address, stride from row to row) of [rows][heads][head_dim], heads next to each other in a row"""
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or not t.is_cuda or t.dtype not in dtypes:
+    try:
+        m, heads, hd = t.shape
+        stride, of_head, step = t.stride()
+        on_gpu = t.is_cuda and t.dtype in dtypes
+    except (AttributeError, TypeError, ValueError):
+        on_gpu = False
+    if not on_gpu:
         _refuse(f"{what}: a tensor [rows][heads][{head_dim}] on the GPU, of {' or '.join(str(d) for d in dtypes)}, is wanted")
-    m, heads, hd = t.shape
     if hd != head_dim or (shape is not None and (m, heads) != shape):
-        _refuse(f"{what} is {tuple(t.shape)}, {(*(shape or ('rows', 'heads')), head_dim)} is wanted")
-    stride, of_head, step = t.stride()
+        _refuse(f"{what} is {m} x {heads} x {hd}, {' x '.join(map(str, (*(shape or ('rows', 'heads')), head_dim)))} is wanted")
     if step != 1 or (of_head != hd and heads > 1) or (m > 1 and stride < heads * hd):
         _refuse(f"{what}: a row's heads must lie next to each other, and rows apart")
     return t.data_ptr(), stride if m > 1 else max(stride, heads * hd)
 
 
+def _call(what: str, cache, batch, tensors, written, call, *args):
+    """call(cache, batch, *args, stream) if all are on the cache's device; `written`: those given tensors that it changes"""
+    if batch.device != cache.device:
+        _refuse("the tensors are on different devices")
+    _launch(what, (cache.pool, *tensors), written, call, *args)
+
+
+_ROTATION_BYTES = C.sizeof(SparkRotation)
+
+
 class PagedCache:
     """Keys and values in pages: `pool` [page][layer][k|v][kv_head][token in its page][head_dim], fp32 or bf16, head_dim 64 or 128,
     pages of a multiple of 16 tokens."""
-    __slots__ = ("pool", "pages", "layers", "kv_heads", "page_tokens", "head_dim", "_views")
+    __slots__ = ("pool", "pages", "layers", "kv_heads", "page_tokens", "head_dim", "device", "_types", "_views", "_workspace")
 
     def __init__(self, pool: torch.Tensor):
         if not isinstance(pool, torch.Tensor) or pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_cuda or not pool.is_contiguous() or pool.dtype not in _DTYPE:
@@ -56,8 +70,9 @@ class PagedCache:
         if not (1 <= self.pages <= 1 << 24 and 1 <= self.layers <= 1 << 16 and 1 <= self.kv_heads <= 1 << 12 and 16 <= self.page_tokens <= 1 << 16 and
                 self.page_tokens % 16 == 0 and self.head_dim in (64, 128)):
             _refuse(f"pool: {tuple(pool.shape)}; pages of 16 to 65536 tokens, a multiple of 16, and heads of 64 or 128 are taken")
-        self.pool = pool
+        self.pool, self.device, self._types = pool, pool.device, (pool.dtype,)
         self._views = {}
+        self._workspace = {}   # sizes -> bytes
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, layers: int = 1, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
@@ -77,7 +92,7 @@ class CachedRows:
     """A batch of n sequences: rows starts[s] .. starts[s + 1] - 1 are the new ones of sequence s, which are the last of its lengths[s]
     slots; table [n][pages a sequence has at most] holds its pages.  All int32 on the GPU; what they hold is read by each
     call (it may change between calls and between replays of a graph)."""
-    __slots__ = ("starts", "lengths", "table", "n", "max_pages", "_batch")
+    __slots__ = ("starts", "lengths", "table", "n", "max_pages", "device", "_batch")
 
     def __init__(self, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
         self.starts, self.lengths, self.table = _table(starts, "starts", 1), _table(lengths, "lengths", 1), _table(table, "table", 2)
@@ -86,6 +101,9 @@ class CachedRows:
             _refuse(f"starts has {starts.shape[0]} entries, lengths {lengths.shape[0]}: {self.n + 1} and {self.n} are wanted")
         if self.n > 1 << 16 or not 1 <= self.max_pages <= 1 << 24:
             _refuse(f"table: {self.n} sequences of {self.max_pages} pages; up to 65536 of 1 to 2^24 are taken")
+        self.device = table.device
+        if starts.device != self.device or lengths.device != self.device:
+            _refuse("the tensors are on different devices")
         self._batch = SparkCacheBatch(C.sizeof(SparkCacheBatch), 0, self.n, self.max_pages, starts.data_ptr(), lengths.data_ptr(), table.data_ptr())
 
     def _of(self, m: int, cache: PagedCache) -> SparkCacheBatch:
@@ -130,11 +148,7 @@ class Rotation:
 
 
 def _gain(t, what: str, head_dim: int):
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (head_dim,) or not t.is_contiguous() or not t.is_cuda:
-        _refuse(f"{what}: fp32 [{head_dim}] on the GPU is wanted")
-    return t.data_ptr()
+    return None if t is None else _plain(t, what, head_dim)
 
 
 def _group(q_heads: int, cache: PagedCache):
@@ -152,26 +166,26 @@ def cached_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Page
     q_at, q_stride = _heads(q, "q", hd, _DTYPE)
     m, heads, _ = q.shape
     _group(heads, cache)
-    k_at, k_stride = _heads(k, "k", hd, (q.dtype,), (m, cache.kv_heads))
-    v_at, v_stride = _heads(v, "v", hd, (q.dtype,), (m, cache.kv_heads))
+    types, of_kv = (q.dtype,), (m, cache.kv_heads)
+    k_at, k_stride = _heads(k, "k", hd, types, of_kv)
+    v_at, v_stride = _heads(v, "v", hd, types, of_kv)
     given = (cache.pool,) if out is None else (cache.pool, out)
     if out is None:
         out = torch.empty(m, heads, hd, dtype=cache.pool.dtype, device=q.device)
-    out_at, out_stride = _heads(out, "out", hd, (cache.pool.dtype,), (m, heads))
+    out_at, out_stride = _heads(out, "out", hd, cache._types, (m, heads))
     if positions is not None and _table(positions, "positions", 1).shape[0] != m:
         _refuse(f"positions: {m} numbers are wanted")
     if not eps >= 0.0:
         _refuse("eps must not be negative")
-    if rotation is not None and rotation.rotary > hd:
-        _refuse(f"a rotation of {rotation.rotary} values and heads of {hd}")
-    freqs = None if rotation is None else rotation.freqs
-    turn = SparkRotation(C.sizeof(SparkRotation), 0 if freqs is None else rotation.rotary, 0 if freqs is None else rotation.interleaved,
-                         1.0 if freqs is None else rotation.amplitude, freqs.data_ptr() if freqs is not None and rotation.rotary else None,
+    rotary = 0 if rotation is None else rotation.rotary
+    if rotary > hd:
+        _refuse(f"a rotation of {rotary} values and heads of {hd}")
+    freqs = rotation.freqs if rotary else None
+    turn = SparkRotation(_ROTATION_BYTES, rotary, rotary and rotation.interleaved, rotation.amplitude if rotary else 1.0, freqs.data_ptr() if rotary else None,
                          None if positions is None else positions.data_ptr(), _gain(q_gain, "q_gain", hd), _gain(k_gain, "k_gain", hd), eps)
     if m and batch.n:
-        _launch("cached_append", (q, k, v, out, cache.pool, batch.table, batch.starts, batch.lengths, freqs, positions, q_gain, k_gain), given,
-                load_library().spark_cache_append, cache._view(layer), batch._of(m, cache), turn, heads, _DTYPE[q.dtype], q_at, q_stride, k_at, k_stride,
-                v_at, v_stride, out_at, out_stride)
+        _call("cached_append", cache, batch, (q, k, v, out, freqs, positions, q_gain, k_gain), given, load_library().spark_cache_append, cache._view(layer),
+              batch._of(m, cache), turn, heads, _DTYPE[q.dtype], q_at, q_stride, k_at, k_stride, v_at, v_stride, out_at, out_stride)
     return out
 
 
@@ -183,9 +197,10 @@ def _scale(scale, hd: int) -> float:
     return scale
 
 
-def _sums(t, what: str, m: int, heads: int):
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (m, heads) or not t.is_contiguous() or not t.is_cuda:
-        _refuse(f"{what}: contiguous fp32 [{m}][{heads}] on the GPU is wanted")
+def _plain(t, what: str, *shape):
+    """the address of a contiguous fp32 tensor of this shape"""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        _refuse(f"{what}: contiguous fp32 {shape} on the GPU is wanted")
     return t.data_ptr()
 
 
@@ -196,12 +211,15 @@ def _wide(what: str, at: int, stride: int):
 
 def attend_workspace_bytes(cache: PagedCache, batch: CachedRows, m: int, q_heads: int) -> int:
     """of cached_attend with m rows"""
-    _group(q_heads, cache)
-    size = C.c_size_t()
-    with torch.cuda.device(cache.pool.device):
-        if load_library().spark_cache_workspace_bytes(cache._view(0), batch._of(m, cache), q_heads, C.byref(size)):
-            _refuse(f"attention of {m} rows of {q_heads} heads")
-    return size.value
+    need = cache._workspace.get((m, q_heads, batch.n, batch.max_pages))
+    if need is None:
+        _group(q_heads, cache)
+        size = C.c_size_t()
+        with torch.cuda.device(cache.pool.device):
+            if load_library().spark_cache_workspace_bytes(cache._view(0), batch._of(m, cache), q_heads, C.byref(size)):
+                _refuse(f"attention of {m} rows of {q_heads} heads")
+        need = cache._workspace[m, q_heads, batch.n, batch.max_pages] = size.value
+    return need
 
 
 def cached_attend(q: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: int = 0, scale: float | None = None, causal: bool = True,
@@ -210,31 +228,27 @@ def cached_attend(q: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: 
     head_dim^-1/2; causal: a row sees the slots up to its own, else all of its sequence.  lse (fp32 [m][q_heads]) is given the
     logarithm of each row's sum.  A row that sees nothing: zeros, and minus infinity."""
     hd = cache.head_dim
-    at, stride = _heads(q, "q", hd, (cache.pool.dtype,))
+    at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape
     _group(heads, cache)
     given = tuple(t for t in (out, lse) if t is not None)
     if out is None:
         out = torch.empty(m, heads, hd, dtype=q.dtype, device=q.device)
-    out_at, out_stride = _heads(out, "out", hd, (q.dtype,), (m, heads))
+    out_at, out_stride = _heads(out, "out", hd, cache._types, (m, heads))
     _wide("q", at, stride)
     _wide("out", out_at, out_stride)
-    lse_at = None if lse is None else _sums(lse, "lse", m, heads)
+    lse_at = None if lse is None else _plain(lse, "lse", m, heads)
     scale = _scale(scale, hd)
     if m and batch.n:
         need = attend_workspace_bytes(cache, batch, m, heads)
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None   # (torch's allocator hands it on in stream order)
-        _launch("cached_attend", (q, out, lse, cache.pool, batch.table, batch.starts, batch.lengths), given, load_library().spark_cache_attend,
-                cache._view(layer), batch._of(m, cache), heads, at, stride, scale, int(causal), out_at, out_stride, lse_at,
-                None if ws is None else ws.data_ptr(), need)
+        _call("cached_attend", cache, batch, (q, out, lse), given, load_library().spark_cache_attend, cache._view(layer), batch._of(m, cache), heads, at, stride,
+              scale, int(causal), out_at, out_stride, lse_at, None if ws is None else ws.data_ptr(), need)
     return out
 
 
 def _weights(t, what: str, cache: PagedCache, batch: CachedRows):
-    shape = (batch.n, cache.kv_heads, batch.max_pages * cache.page_tokens)
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
-        _refuse(f"{what}: contiguous fp32 {shape} on the GPU is wanted")
-    return t.data_ptr()
+    return _plain(t, what, batch.n, cache.kv_heads, batch.max_pages * cache.page_tokens)
 
 
 def cached_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: int = 0, scale: float | None = None,
@@ -243,11 +257,11 @@ def cached_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: C
     that the batch's rows gave it, summed over rows and the heads of its group; q, scale and causal as cached_attend had them, lse
     from it.  Slots behind a sequence's length are left alone (zeros in a new result).  out may be before."""
     hd = cache.head_dim
-    at, stride = _heads(q, "q", hd, (cache.pool.dtype,))
+    at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape
     _group(heads, cache)
     _wide("q", at, stride)
-    lse_at = _sums(lse, "lse", m, heads)
+    lse_at = _plain(lse, "lse", m, heads)
     before_at = None if before is None else _weights(before, "before", cache, batch)
     if not math.isfinite(decay) or not math.isfinite(C.c_float(decay).value):
         _refuse("decay must be finite")
@@ -257,8 +271,8 @@ def cached_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: C
     out_at = _weights(out, "out", cache, batch)
     scale = _scale(scale, hd)
     if batch.n:
-        _launch("cached_weigh", (q, lse, before, out, cache.pool, batch.table, batch.starts, batch.lengths), given, load_library().spark_cache_weigh,
-                cache._view(layer), batch._of(m, cache), heads, at, stride, scale, int(causal), lse_at, before_at, decay, out_at)
+        _call("cached_weigh", cache, batch, (q, lse, before, out), given, load_library().spark_cache_weigh, cache._view(layer), batch._of(m, cache), heads, at, stride,
+              scale, int(causal), lse_at, before_at, decay, out_at)
     return out
 
 
@@ -283,7 +297,7 @@ def cached_evict(cache: PagedCache, batch: CachedRows, weights: torch.Tensor, ke
     kept = torch.empty(batch.n, cache.kv_heads, keep, dtype=torch.int32, device=weights.device)
     lengths = torch.empty(batch.n, dtype=torch.int32, device=weights.device)
     if batch.n:
-        _launch("cached_evict", (weights, weights_out, cache.pool, batch.table, batch.lengths, table_out), (cache.pool, weights if weights_out is None else weights_out),
-                load_library().spark_cache_evict, cache._view(layer), batch._of(0, cache), at, keep, first, recent,
-                None if table_out is None else table_out.data_ptr(), out_pages, out_at, kept.data_ptr(), lengths.data_ptr())
+        _call("cached_evict", cache, batch, (weights, weights_out, table_out), (cache.pool, weights if weights_out is None else weights_out),
+              load_library().spark_cache_evict, cache._view(layer), batch._of(0, cache), at, keep, first, recent,
+              None if table_out is None else table_out.data_ptr(), out_pages, out_at, kept.data_ptr(), lengths.data_ptr())
     return kept, lengths

@@ -9,6 +9,8 @@
 
 namespace spark {
 
+constexpr int APPEND_ROWS = 16;   // of a workgroup, at most
+
 struct AppendArgs {
   CacheView cache;
   BatchView batch;
@@ -36,15 +38,48 @@ __device__ __forceinline__ void cos_sin(double angle, float &c, float &s) {
   s = quarter == 0 ? sn : quarter == 1 ? cs : quarter == 2 ? -sn : -cs;
 }
 
-template <typename T> __device__ __forceinline__ void load4(const T *p, float *f) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 v = *(const float4 *)p;
-    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-  } else {
-    const uint2 v = *(const uint2 *)p;
-    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+// a lane's eight values as they lie: two fours, or (not aligned for that) one by one
+template <typename S, bool VEC> struct Eight;
+template <> struct Eight<float, true> {
+  float4 v[2];
+  __device__ __forceinline__ void load(const float *p, const int (&at)[8]) { v[0] = *(const float4 *)(p + at[0]); v[1] = *(const float4 *)(p + at[4]); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { x[4 * i] = v[i].x; x[4 * i + 1] = v[i].y; x[4 * i + 2] = v[i].z; x[4 * i + 3] = v[i].w; }
   }
+};
+template <> struct Eight<bf16_t, true> {
+  uint2 v[2];
+  __device__ __forceinline__ void load(const bf16_t *p, const int (&at)[8]) { v[0] = *(const uint2 *)(p + at[0]); v[1] = *(const uint2 *)(p + at[4]); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x[4 * i] = __uint_as_float(v[i].x << 16); x[4 * i + 1] = __uint_as_float(v[i].x & 0xffff0000u);
+      x[4 * i + 2] = __uint_as_float(v[i].y << 16); x[4 * i + 3] = __uint_as_float(v[i].y & 0xffff0000u);
+    }
+  }
+};
+template <typename S> struct Eight<S, false> {
+  S v[8];
+  __device__ __forceinline__ void load(const S *p, const int (&at)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[at[e]];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = Elem<S>::widen(v[e]);
+  }
+};
+// sum over the LANES (8 or 16) lanes of a head, the same bits in each
+template <int CTRL> __device__ __forceinline__ float add_lane(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int LANES> __device__ __forceinline__ float head_sum(float v) {
+  v = add_lane<0xb1>(v);    // neighbours,
+  v = add_lane<0x4e>(v);    // pairs of them,
+  v = add_lane<0x141>(v);   // fours (mirrored within eight)
+  if constexpr (LANES == 16) v = add_lane<0x140>(v);   // eights (mirrored within sixteen)
+  return v;
 }
 template <typename T> __device__ __forceinline__ void store_four(T *p, const float *f) {
   if constexpr (sizeof(T) == 4) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
@@ -58,93 +93,94 @@ template <typename T> __device__ __forceinline__ void store_four(T *p, const flo
 template <typename S, typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
   extern __shared__ float2 s_trig[];   // [rows][rotary / 2] cosine and sine
-  __shared__ int s_seq[4];
+  __shared__ int s_seq[APPEND_ROWS];
   constexpr int LANES = HD / 8;
   const int half = a.rotary / 2, row_first = blockIdx.x * a.rows, row_end = min(row_first + a.rows, a.batch.m);
-  // each row's sequence: the first that ends behind it, if it has begun (rows outside all of them: -1)
-  if ((int)threadIdx.x < row_end - row_first) {
-    const int r = row_first + threadIdx.x;
-    int lo = 0, hi = a.batch.n;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (a.batch.starts[mid + 1] > r) hi = mid;
-      else lo = mid + 1;
-    }
-    s_seq[threadIdx.x] = lo < a.batch.n && a.batch.starts[lo] <= r ? lo : -1;
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < (row_end - row_first) * half; i += blockDim.x) {
-    const int r = row_first + i / half, s = s_seq[i / half];
-    if (s < 0) continue;
-    int position;
-    if (a.positions) {
-      position = a.positions[r];
-    } else {
-      const Sequence q = sequence(a.batch, s, a.cache.page_tokens);
-      position = q.slot(r - q.row0);
-    }
-    float c, sn;
-    cos_sin((double)position * a.freqs[i % half], c, sn);
-    s_trig[i] = make_float2(c * a.amplitude, sn * a.amplitude);
-  }
-  __syncthreads();
-
-  const int groups = blockDim.x / LANES / a.rows, group = threadIdx.x / LANES, i = group / groups, r = row_first + i;
-  if (r >= row_end || s_seq[i] < 0) return;
-  const Sequence seq = sequence(a.batch, s_seq[i], a.cache.page_tokens);
-  const int slot = seq.slot(r - seq.row0), page = slot < 0 ? -1 : page_of(seq, slot, a.cache.page_tokens, a.cache.n_pages);
-  const int token = slot < 0 ? 0 : slot % a.cache.page_tokens;
+  const int groups = blockDim.x / LANES / a.rows, group = threadIdx.x / LANES, i = group / groups, r = min(row_first + i, a.batch.m - 1);
   const int c = threadIdx.x % LANES, p0 = 4 * c, nq = a.n_q_heads, nkv = a.cache.n_kv_heads;
-  // where a lane's eight values lie: VEC two fours, else pairs
+  // where a lane's eight values lie: VEC two fours, else the first of four pairs and the second of them
   const bool turned = p0 < half, apart = turned && !a.interleaved;
   int at[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if constexpr (VEC) {
       at[e] = apart ? p0 + (e & 3) + (e >> 2) * half : (turned ? 2 * p0 : a.rotary + 2 * (p0 - half)) + e;
-    } else {   // the first of four pairs, the second of them
+    } else {
       const int p = p0 + (e & 3);
       at[e] = p < half ? (a.interleaved ? 2 * p + (e >> 2) : p + (e >> 2) * half) : a.rotary + 2 * (p - half) + (e >> 2);
     }
   }
-  float cs[4], sn[4], gain[2][8];
+  const S *q = (const S *)a.q + r * a.q_stride, *k = (const S *)a.k + r * a.k_stride, *v = (const S *)a.v + r * a.v_stride;
+  auto source = [&](int h) { return h < nq ? q + h * HD : h < nq + nkv ? k + (h - nq) * HD : v + (h - nq - nkv) * HD; };
+  // the first head's values are on their way while the row's place and angles are found, each next one's while one is worked on
+  const int head_end = min((int)(blockIdx.y + 1) * a.heads_per_wg, nq + 2 * nkv);
+  int h = blockIdx.y * a.heads_per_wg + group % groups;
+  Eight<S, VEC> next;
+  if (h < head_end) next.load(source(h), at);
+
+  // each row's sequence: the first that ends behind it, if it has begun (rows outside all of them: -1)
+  if ((int)threadIdx.x < row_end - row_first) {
+    const int row = row_first + threadIdx.x;
+    int lo = 0, hi = a.batch.n;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (a.batch.starts[mid + 1] > row) hi = mid;
+      else lo = mid + 1;
+    }
+    s_seq[threadIdx.x] = lo < a.batch.n && a.batch.starts[lo] <= row ? lo : -1;
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < (row_end - row_first) * half; j += blockDim.x) {
+    const int row = row_first + j / half, s = s_seq[j / half];
+    if (s < 0) continue;
+    int position;
+    if (a.positions) {
+      position = a.positions[row];
+    } else {
+      const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
+      position = seq.slot(row - seq.row0);
+    }
+    float cosine, sine;
+    cos_sin((double)position * a.freqs[j % half], cosine, sine);
+    s_trig[j] = make_float2(cosine * a.amplitude, sine * a.amplitude);
+  }
+  __syncthreads();
+  if (row_first + i >= row_end || s_seq[i] < 0) return;
+  const Sequence seq = sequence(a.batch, s_seq[i], a.cache.page_tokens);
+  const int slot = seq.slot(r - seq.row0), page = slot < 0 ? -1 : page_of(seq, slot, a.cache.page_tokens, a.cache.n_pages);
+  const int token = slot < 0 ? 0 : slot % a.cache.page_tokens;
+  float cs[4], sn[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float2 v = p0 + e < half ? s_trig[i * half + p0 + e] : make_float2(1.f, 0.f);
-    cs[e] = v.x;
-    sn[e] = v.y;
+    const float2 t = p0 + e < half ? s_trig[i * half + p0 + e] : make_float2(1.f, 0.f);
+    cs[e] = t.x;
+    sn[e] = t.y;
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    gain[0][e] = a.q_gain ? a.q_gain[at[e]] : 1.f;
-    gain[1][e] = a.k_gain ? a.k_gain[at[e]] : 1.f;
-  }
-  const int head0 = blockIdx.y * a.heads_per_wg, head_end = min(head0 + a.heads_per_wg, nq + 2 * nkv);
-  const S *q = (const S *)a.q + r * a.q_stride, *k = (const S *)a.k + r * a.k_stride, *v = (const S *)a.v + r * a.v_stride;
   T *out = (T *)a.q_out + r * a.out_stride, *place = a.cache.plane<T>(max(page, 0), 0, 0) + token * HD;
   const long long plane = (long long)a.cache.page_tokens * HD;
-#pragma unroll 2
-  for (int h = head0 + group % groups; h < head_end; h += groups) {
+  int known = -1;
+  const float *gain_at = nullptr;
+  float gain[8];   // of queries, then of keys
+  for (; h < head_end; h += groups) {
     const int which = h < nq ? 0 : h < nq + nkv ? 1 : 2;
-    const S *src = which == 0 ? q + h * HD : which == 1 ? k + (h - nq) * HD : v + (h - nq - nkv) * HD;
     float x[8];
-    if constexpr (VEC) {
-      load4(src + at[0], x);
-      load4(src + at[4], x + 4);
-    } else {
+    next.get(x);
+    if (h + groups < head_end) next.load(source(h + groups), at);
+    if (which != known) {
+      known = which;
+      gain_at = which == 0 ? a.q_gain : which == 1 ? a.k_gain : nullptr;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = Elem<S>::widen(src[at[e]]);
+      for (int e = 0; e < 8; ++e) gain[e] = gain_at ? gain_at[at[e]] : 1.f;
     }
-    if (which == 0 ? a.q_gain != nullptr : which == 1 && a.k_gain != nullptr) {
+    if (gain_at) {
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
-#pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      sum = head_sum<LANES>(sum);
       if (sum > 1e-30f && sum < 1e37f) {
-        const float f = 1.0f / sqrtf(sum * (1.0f / HD) + (float)a.eps);
+        const float f = __builtin_amdgcn_rsqf(sum * (1.0f / HD) + (float)a.eps);   // (off by a last bit)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= f * (which == 0 ? gain[0][e] : gain[1][e]);
+        for (int e = 0; e < 8; ++e) x[e] *= f * gain[e];
       } else {   // squares that leave fp32's range (the same lanes for all of a head)
         double wide = 0.0;
 #pragma unroll
@@ -153,7 +189,7 @@ __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
         for (int o = LANES / 2; o > 0; o >>= 1) wide += __shfl_xor(wide, o, 64);
         const double f = 1.0 / sqrt(wide * (1.0 / HD) + a.eps);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)(x[e] * f * (which == 0 ? gain[0][e] : gain[1][e]));
+        for (int e = 0; e < 8; ++e) x[e] = (float)(x[e] * f * gain[e]);
       }
     }
     if (which < 2 && a.rotary) {

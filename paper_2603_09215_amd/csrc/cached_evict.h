@@ -14,6 +14,7 @@ struct EvictArgs {
   int out_pages, keep, first, recent;
 };
 
+typedef __attribute__((ext_vector_type(4))) uint32_t move_u32x4;
 constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
 
 // larger weight, larger key; -0 as +0; every NaN above all numbers
@@ -26,27 +27,32 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return float_order_key
 constexpr int EVICT_EACH = 8, EVICT_BINS = 2048;
 static_assert(EVICT_BINS == 2 * EVICT_THREADS && EVICT_WAVES == 16, "two digits a thread; waves fit a row of lanes");
 
+template <int CTRL, int ROWS> __device__ __forceinline__ unsigned add_from(unsigned v) {   // a lane's value from another one's, of some rows of 16
+  return v + (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
+}
+// inclusive sum over a wave's lanes
+__device__ __forceinline__ unsigned wave_scan(unsigned v) {
+  v = add_from<0x111, 0xf>(v);   // 1, 2, 4 and 8 to the right within sixteen
+  v = add_from<0x112, 0xf>(v);
+  v = add_from<0x114, 0xf>(v);
+  v = add_from<0x118, 0xf>(v);
+  v = add_from<0x142, 0xa>(v);   // the last of sixteen to the next sixteen,
+  return add_from<0x143, 0xc>(v);   // of 32 to the upper 32
+}
 // sum over the threads before this one in the workgroup, and over all of them
 __device__ __forceinline__ unsigned evict_scan(unsigned v, unsigned *s_wave, unsigned &total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  unsigned incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned up = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += up;
-  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned incl = wave_scan(v);
   __syncthreads();
   if (lane == 63) s_wave[wave] = incl;
   __syncthreads();
   unsigned w = s_wave[lane & 15];
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    const unsigned up = __shfl_up(w, o, 16);
-    if ((lane & 15) >= o) w += up;
-  }
-  total = __shfl(w, 15, 64);
-  const unsigned before = __shfl(w, max(wave - 1, 0), 64);
-  return incl - v + (wave ? before : 0u);
+  w = add_from<0x111, 0xf>(w);
+  w = add_from<0x112, 0xf>(w);
+  w = add_from<0x114, 0xf>(w);
+  w = add_from<0x118, 0xf>(w);
+  total = (unsigned)__builtin_amdgcn_readlane((int)w, 15);
+  return incl - v + (wave ? (unsigned)__builtin_amdgcn_readlane((int)w, wave - 1) : 0u);
 }
 
 __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
@@ -64,7 +70,8 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
   const bool some = need > 0;
   const int each = cut((length + EVICT_THREADS - 1) / EVICT_THREADS, 1, EVICT_EACH), chunk = each * EVICT_THREADS;
   float x[EVICT_EACH];
-  int held = -1;   // which chunk x is of
+  uint32_t key[EVICT_EACH];   // 0, which no weight has, for what is not chosen from: in the lowest place, never reached
+  int held = -1;              // which chunk they are of
   auto fetch = [&](int c0) {
     if (c0 == held) return;
     held = c0;
@@ -73,13 +80,18 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
       const int t = c0 + tid * each + e;
       x[e] = e < each && t < length ? w[t] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < EVICT_EACH; ++e) {
+      const int t = c0 + tid * each + e;
+      key[e] = e < each && t >= lo && t < hi ? weight_key(x[e]) : 0u;
+    }
   };
   if (some) {
     constexpr uint32_t ZERO = 0x80000000u;   // the key of nothing, which many slots may have: counted by waves
 #pragma unroll 1
     for (int digit = 0; digit < 3; ++digit) {
-      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, above = digit == 1 ? 21 : 10;
-      const unsigned mask = digit == 2 ? 1023u : 2047u;
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
+      const unsigned mask = digit == 2 ? 1023u : 2047u, span = digit == 0 ? ~0u : digit == 1 ? (1u << 21) - 1 : (1u << 10) - 1;   // keys with this prefix
       s_count[2 * tid] = 0;
       s_count[2 * tid + 1] = 0;
       __syncthreads();
@@ -89,14 +101,12 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
 #pragma unroll
         for (int e = 0; e < EVICT_EACH; ++e) {
           if (e < each) {
-            const int t = c0 + tid * each + e;
-            const uint32_t key = weight_key(x[e]);
-            const bool counts = t >= lo && t < hi && (digit == 0 || (key >> above) == (prefix >> above));
-            zeros += __popcll(__ballot(counts && key == ZERO));
-            if (counts && key != ZERO) atomicAdd(&s_count[(key >> shift) & mask], 1u);
+            const bool zero = key[e] == ZERO, counts = (key[e] ^ prefix) <= span;
+            zeros += __popcll(__ballot(zero));
+            if (counts && (key[e] & 0x7fffffffu)) atomicAdd(&s_count[(key[e] >> shift) & mask], 1u);
           }
         }
-        if (zeros && (tid & 63) == 0) atomicAdd(&s_count[(ZERO >> shift) & mask], zeros);
+        if (zeros && (ZERO ^ prefix) <= span && (tid & 63) == 0) atomicAdd(&s_count[(ZERO >> shift) & mask], zeros);
       }
       __syncthreads();
       // from the highest digit down, two a thread
@@ -118,10 +128,9 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
 #pragma unroll
     for (int e = 0; e < EVICT_EACH; ++e) {
       const int t = c0 + tid * each + e;
-      const uint32_t key = weight_key(x[e]);
       const bool middle = t >= lo && t < hi, there = e < each && t < length;
-      if (there && (!middle || (some && key > prefix))) above |= 1u << e;
-      if (there && some && middle && key == prefix) tie |= 1u << e;
+      if (there && (!middle || (some && key[e] > prefix))) above |= 1u << e;
+      if (there && some && middle && key[e] == prefix) tie |= 1u << e;
     }
     unsigned total;
     const unsigned before = evict_scan(__popc(above) | __popc(tie) << 16, s_wave, total);   // (8192 at most of each)
@@ -145,8 +154,11 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
 }
 
 // The move.  A vector is PIECES of 16 bytes; a workgroup takes of one sequence and head the keys or values, COLS pieces of each, and
-// goes through its share of the kept slots in rounds.  In place one workgroup has all of them: a round's entries are all
-// read before any is written, and it writes no slot past those that it has read, so nothing is lost.
+// goes through its share of the kept slots in rounds, MOVE_BATCH entries a thread on their way at a time (67 MB moved: 33 us one by
+// one, 27 in fours).  In place one workgroup has all of them: a round's entries are all read before any is
+// written, and it writes no slot past those that it has read, so nothing is lost.
+constexpr int MOVE_BATCH = 4;
+
 template <typename T, int HD, int COLS>
 __global__ void __launch_bounds__(1024) cached_move_k(EvictArgs a) {
   constexpr int SHARES = HD * (int)sizeof(T) / 16 / COLS;
@@ -157,19 +169,32 @@ __global__ void __launch_bounds__(1024) cached_move_k(EvictArgs a) {
   if (in_place && left == length) return;
   const int *kept = a.kept + (long long)sh * a.keep, *in = a.batch.table + (long long)s * a.batch.max_pages, *out = a.table_out + (long long)s * a.out_pages;
   const int piece = col * COLS + threadIdx.x % COLS, entries = blockDim.x / COLS;
-  for (int i0 = blockIdx.y * entries; i0 < left; i0 += gridDim.y * entries) {
-    const int i = i0 + threadIdx.x / COLS;
-    uint4 v = make_uint4(0, 0, 0, 0), *dst = nullptr;
-    if (i < left) {
-      const int t = cut(kept[i], 0, length - 1), from = in[t / pt], to = out[i / pt];
-      if ((unsigned)from < (unsigned)a.cache.n_pages) v = ((const uint4 *)(a.cache.plane<T>(from, which, head) + t % pt * HD))[piece];
-      if ((unsigned)to < (unsigned)a.cache.n_pages && !(in_place && t == i)) dst = (uint4 *)(a.cache.plane<T>(to, which, head) + i % pt * HD) + piece;
+  for (int i0 = blockIdx.y * MOVE_BATCH * entries; i0 < left; i0 += gridDim.y * MOVE_BATCH * entries) {
+    int t[MOVE_BATCH], from[MOVE_BATCH], to[MOVE_BATCH];
+    move_u32x4 v[MOVE_BATCH];
+#pragma unroll
+    for (int j = 0; j < MOVE_BATCH; ++j) t[j] = cut(kept[min(i0 + j * entries + (int)threadIdx.x / COLS, left - 1)], 0, length - 1);
+#pragma unroll
+    for (int j = 0; j < MOVE_BATCH; ++j) {
+      from[j] = in[t[j] / pt];
+      to[j] = out[min(i0 + j * entries + (int)threadIdx.x / COLS, left - 1) / pt];
+    }
+#pragma unroll
+    for (int j = 0; j < MOVE_BATCH; ++j) {
+      const bool there = (unsigned)from[j] < (unsigned)a.cache.n_pages;
+      const move_u32x4 x = ((const move_u32x4 *)(a.cache.plane<T>(there ? from[j] : 0, which, head) + t[j] % pt * HD))[piece];
+      v[j] = there ? x : move_u32x4{0, 0, 0, 0};
     }
     if (in_place) {
       wait_memory_ops();
       __syncthreads();
     }
-    if (dst) *dst = v;
+#pragma unroll
+    for (int j = 0; j < MOVE_BATCH; ++j) {
+      const int i = i0 + j * entries + (int)threadIdx.x / COLS;
+      if (i < left && (unsigned)to[j] < (unsigned)a.cache.n_pages && !(in_place && t[j] == i))
+        ((move_u32x4 *)(a.cache.plane<T>(to[j], which, head) + i % pt * HD))[piece] = v[j];
+    }
   }
 }
 

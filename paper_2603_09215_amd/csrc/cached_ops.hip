@@ -117,8 +117,12 @@ int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch,
   auto vec = [](const void *p, size_t bytes, int64_t stride) { return aligned(p, 4 * bytes) && stride % 4 == 0; };
   const bool wide = a.rotary % 8 == 0 && vec(q, sb, q_stride) && vec(k, sb, k_stride) && vec(v, sb, v_stride) && vec(q_out, cb, out_stride);
   const int heads = n_q_heads + 2 * cache->n_kv_heads;
-  a.rows = batch->m >= 2048 ? 4 : 1;
-  a.heads_per_wg = a.rows > 1 ? heads : 16;
+  // A workgroup's start (its rows' places and angles) takes some 3 us: about a thousand of them where there are rows enough, each with all
+  // of its rows' heads, and the heads dealt out where there are few.  (32 + 2 x 2 heads, normed: 8191 rows 44.5 us in eights, 49 in fours, 56
+  // in twos; 2000 rows 19 one by one, 14.4 in twos, 15.4 in fours; 512 rows 5.5 with half of the heads a workgroup, 7.1 with 16; one row 3.7 with 16, 4.5 with 40.)
+  a.rows = 1;
+  while (a.rows < APPEND_ROWS && batch->m / (2 * a.rows) >= 1000) a.rows *= 2;
+  a.heads_per_wg = batch->m >= 1000 ? heads : batch->m >= 256 ? std::max(16, (heads + 1) / 2) : 16;
   const dim3 grid((batch->m + a.rows - 1) / a.rows, (heads + a.heads_per_wg - 1) / a.heads_per_wg);
   const size_t lds = sizeof(float) * a.rows * a.rotary;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
@@ -190,6 +194,8 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
       ((uintptr_t)before & 3) || !aligned(out, 4) || !std::isfinite(scale) || scale == 0.f || !std::isfinite(decay))
     return SPARK_EINVAL;
   if (batch->n == 0) return SPARK_OK;
+  const int n_cu = compute_units();
+  if (n_cu <= 0) return SPARK_EHIP;
   WeighArgs a{};
   a.cache = view(cache); a.batch = view(batch);
   a.q = q; a.lse = lse; a.before = decay != 0.f ? before : nullptr; a.out = out; a.q_stride = q_stride;
@@ -197,12 +203,19 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
   a.factor = std::fabs(scale) * 1.44269504088896340736f;
   a.flip = scale < 0.f ? 0x80000000u : 0u;
   a.decay = decay;
-  // (from two blocks of pairs for each of four waves on)
-  a.way = (long long)batch->m * a.group / batch->n >= 256 ? 4 : 1;
-  const int slots = batch->max_pages * cache->page_tokens, each = 128 / a.way;
-  const dim3 grid(batch->n * cache->n_kv_heads, std::min((slots + each - 1) / each, 1024));
+  // Many pairs from a block for each of eight waves on (64 rows over 8191 slots, 32 + 2 heads: 16.7 us, a wave by itself 36; 8 rows of it 7.1 and 7.9; but 16 batches
+  // of 8 rows over 4095 slots 71 and 24).  Few: workgroups that stay for several pieces, as many as a compute unit has registers for (32 steps of 4095 slots, 28 + 4
+  // heads: three 24.6 us, two 28, four 31; fp32 two 64, three 77).
+  const bool many = (long long)batch->m * a.group / batch->n >= 256;
+  const int heads = batch->n * cache->n_kv_heads, pieces = (batch->max_pages * cache->page_tokens + 31) / 32;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
-    cached_weigh_k<decltype(t), decltype(hd)::value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a);
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    auto go = [&](auto kern, int each, int waves, int most) {
+      kern<<<dim3(heads, std::min((pieces + each - 1) / each, most)), 64 * waves, 0, (hipStream_t)hip_stream>>>(a);
+    };
+    if (many) go(cached_weigh_k<T, HD, true>, Weigh<T, true>::PIECES, Weigh<T, true>::WAVES, 4096);
+    else go(cached_weigh_k<T, HD, false>, Weigh<T, false>::PIECES, Weigh<T, false>::WAVES, std::max(1, (sizeof(T) * HD == 512 ? 2 : 3) * n_cu / heads));
   });
   return status();
 }
@@ -232,7 +245,7 @@ int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, 
     if (a.table_out == batch->table) {
       cached_move_k<T, HD, 8><<<heads * 2 * (PIECES / 8), 1024, 0, stream>>>(a);
     } else {
-      const int rounds = (keep * PIECES + 255) / 256;
+      const int rounds = (keep * PIECES + 256 * MOVE_BATCH - 1) / (256 * MOVE_BATCH);
       cached_move_k<T, HD, PIECES><<<dim3(heads * 2, std::min(rounds, 256)), 256, 0, stream>>>(a);
     }
   });

@@ -4,8 +4,10 @@
 //
 // With few rows bound by the keys' way through memory, with many by the exponentials.  A wave takes 32 tokens, whose keys stay in registers, and
 // goes through the (row, head) pairs in blocks of 32: scores S [pair][token] = Q K^T, so that a lane has 16 scores of one token and
-// its sum is one register.  With many pairs the four waves of a workgroup share the tokens and deal out the
-// blocks, and add up their sums in order; with few each has its own tokens.  Nothing is added by atomics.
+// its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens (in bf16 two pieces of 32, for each block's queries
+// come from L2, 134 MB for 1024 pairs of 8191 slots and two heads with one piece, which took 20 us), deal out the blocks, the next one's queries
+// on their way while one is worked on, and add up their sums in order.  Few: each wave has its own tokens, the next ones' keys are on
+// their way while they are worked on, and a single block's queries stay.  Nothing is added by atomics.
 #pragma once
 #include "cached_attend.h"
 
@@ -18,99 +20,180 @@ struct WeighArgs {
   const float *lse, *before;   // before: or nullptr
   float *out;
   long long q_stride;
-  int n_q_heads, group, causal, way;   // way: waves that share their tokens, 1 or 4
-  float factor, decay;                 // factor and flip as in AttendArgs
+  int n_q_heads, group, causal;
+  float factor, decay;         // factor and flip as in AttendArgs
   uint32_t flip;
 };
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) cached_weigh_k(WeighArgs a) {
+template <typename T, bool MANY> struct Weigh {
+  static constexpr int WAVES = MANY ? 8 : 4, WAY = MANY ? 8 : 1;            // of a workgroup; that share tokens
+  static constexpr int TB = MANY && sizeof(T) == 2 ? 2 : 1;                  // pieces of 32 tokens that a wave works on at a time
+  static constexpr int PIECES = WAVES / WAY * TB;                            // that a workgroup works on at a time
+};
+
+template <typename T, int HD, bool MANY>
+__global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) {
+  using W = Weigh<T, MANY>;
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int STEPS = HD * (int)sizeof(T) / 32;   // 16-byte pieces of a key or query that a lane holds
-  __shared__ float4 s_bias[4][8];   // of a wave's block of pairs: -lse log2 e,
-  __shared__ int4 s_limit[4][8];    // and the last slot seen
-  __shared__ float s_sum[4][32];
+  constexpr int STEPS = HD * (int)sizeof(T) / 32, TB = W::TB;   // 16-byte pieces of a key or query that a lane holds
+  __shared__ float4 s_bias[W::WAVES][8];   // of a wave's block of pairs: -lse log2 e,
+  __shared__ int4 s_limit[W::WAVES][8];    // and the last slot seen
+  __shared__ float s_sum[W::WAVES][TB][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int s = blockIdx.x / a.cache.n_kv_heads, kvh = blockIdx.x % a.cache.n_kv_heads;
   const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
-  const int pairs = seq.rows * a.group, blocks = (pairs + 31) / 32, own = 4 / a.way;
-  const int pieces = (seq.length + 31) / 32;
-  for (int y = blockIdx.y * own; y < pieces; y += gridDim.y * own) {
-    const int t0 = (y + wave / a.way) * 32, t = t0 + col;
-    // (a wave past the length works on nothing, and comes to the barriers)
-    const int pages = pages_of(seq, a.cache, t0 / 16 + (lane & 1), seq.length);
-    const unsigned here = (unsigned)__ballot(pages >= 0) & 3u;
-    ca_u32x4 k[STEPS];
-    {
+  const int pairs = seq.rows * a.group, blocks = (pairs + 31) / 32, pieces = (seq.length + 31) / 32;
+
+  // the pages of a piece's 16s (of TB pieces) in the first lanes
+  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, 2 * piece + (lane & (2 * TB - 1)), seq.length); };
+  auto load_keys = [&](int piece, int pages, ca_u32x4 (&k)[TB][STEPS]) {   // (where there is no page: from the first, of no account)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
       int index, in;
-      place_of(a.cache, t0 / 16 + (col >> 4), index, in);
-      const ca_u32x4 *at = (const ca_u32x4 *)(a.cache.plane<T>(max(__shfl(pages, col >> 4, 64), 0), 0, kvh) + (in + (col & 15)) * HD);
+      place_of(a.cache, 2 * (piece + j) + (col >> 4), index, in);
+      const ca_u32x4 *at = (const ca_u32x4 *)(a.cache.plane<T>(max(__shfl(pages, 2 * j + (col >> 4), 64), 0), 0, kvh) + (in + (col & 15)) * HD);
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) k[i] = here ? at[2 * i + half] : ca_u32x4{0, 0, 0, 0};
+      for (int i = 0; i < STEPS; ++i) k[j][i] = at[2 * i + half];
     }
-    float total = 0.f;
-    for (int b = wave % a.way; b < blocks; b += a.way) {
-      const int first = last_seen(seq, b * 32 / a.group, a.causal), last = last_seen(seq, min(b * 32 + 31, pairs - 1) / a.group, a.causal);
-      if (t0 > last || !here) continue;
-      const int p = min(b * 32 + col, pairs - 1), row = p / a.group, h = kvh * a.group + p % a.group;
-      const T *at = (const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)h * HD;
-      ca_u32x4 q[STEPS];
+  };
+  auto load_queries = [&](int b, ca_u32x4 (&q)[STEPS], float &lse) {
+    const int p = min(b * 32 + col, pairs - 1), row = p / a.group, h = kvh * a.group + p % a.group;   // (pairs past the last: that one, left out)
+    const ca_u32x4 *at = (const ca_u32x4 *)((const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)h * HD);
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) q[i] = ca_signed<T>(((const ca_u32x4 *)at)[2 * i + half], a.flip);
-      const float lse = a.lse[(long long)(seq.row0 + row) * a.n_q_heads + h];
-      const bool none = b * 32 + col >= pairs || lse == -INFINITY;
-      if (half == 0) {
-        ((float *)s_bias[wave])[col] = none ? 0.f : lse * -1.44269504088896340736f;
-        ((int *)s_limit[wave])[col] = none ? -1 : last_seen(seq, row, a.causal);
-      }
-      const bool masked = __any(none) || t0 + 31 > first || here != 3u;
-      ca_f32x16 sc;
+    for (int i = 0; i < STEPS; ++i) q[i] = at[2 * i + half];
+    lse = a.lse[(long long)(seq.row0 + row) * a.n_q_heads + h];
+  };
+  bool some_out = false;   // of the block in LDS: a pair that gives nothing
+  auto place_block = [&](int b, float lse) {
+    const bool none = b * 32 + col >= pairs || lse == -INFINITY;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (half == 0) {
+      ((float *)s_bias[wave])[col] = none ? 0.f : lse * -1.44269504088896340736f;
+      ((int *)s_limit[wave])[col] = none ? -1 : last_seen(seq, (b * 32 + col) / a.group, a.causal);
+    }
+    some_out = __any(none);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  float total[TB];
+  // what a block's pairs give tokens t0 + 32 j + col
+  auto add_block = [&](int b, int t0, const ca_u32x4 (&k)[TB][STEPS], const ca_u32x4 (&q)[STEPS]) {
+    const bool masked = some_out || t0 + 32 * TB - 1 > last_seen(seq, b * 32 / a.group, a.causal);
+    ca_f32x16 sc[TB];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+    for (int j = 0; j < TB; ++j)
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
+      for (int r = 0; r < 16; ++r) sc[j][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const ca_u32x4 qs = ca_signed<T>(q[i], a.flip);
+#pragma unroll
+      for (int j = 0; j < TB; ++j) {
         if constexpr (BF) {
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ca_operand(q[i]), ca_operand(k[i]), sc, 0, 0, 0);
+          sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ca_operand(qs), ca_operand(k[j][i]), sc[j], 0, 0, 0);
         } else {
-          const float4 x = __builtin_bit_cast(float4, q[i]), z = __builtin_bit_cast(float4, k[i]);
-          sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, z.x, sc, 0, 0, 0);
-          sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, z.y, sc, 0, 0, 0);
-          sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, z.z, sc, 0, 0, 0);
-          sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, z.w, sc, 0, 0, 0);
+          const ca_f32x4 x = __builtin_bit_cast(ca_f32x4, qs), z = __builtin_bit_cast(ca_f32x4, k[j][i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], z[e], sc[j], 0, 0, 0);
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {   // pairs 8 i + 4 half + 0..3
-        const float4 bias = s_bias[wave][2 * i + half];
-        const float bs[4] = {bias.x, bias.y, bias.z, bias.w};
-        float x[4];
+    for (int i = 0; i < 4; ++i) {   // pairs 8 i + 4 half + 0..3
+      const float4 bias = s_bias[wave][2 * i + half];
+      const float bs[4] = {bias.x, bias.y, bias.z, bias.w};
+      float x[TB][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = ca_exp2(fmaf(sc[4 * i + e], a.factor, bs[e]));
-        if (masked) {
-          const int4 limit = s_limit[wave][2 * i + half];
-          const int lim[4] = {limit.x, limit.y, limit.z, limit.w};
+      for (int j = 0; j < TB; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = t <= lim[e] ? x[e] : 0.f;
-        }
+        for (int e = 0; e < 4; ++e) x[j][e] = ca_exp2(fmaf(sc[j][4 * i + e], a.factor, bs[e]));
+      if (masked) {
+        const int4 limit = s_limit[wave][2 * i + half];
+        const int lim[4] = {limit.x, limit.y, limit.z, limit.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) total += x[e];
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[j][e] = t0 + 32 * j + col <= lim[e] ? x[j][e] : 0.f;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) total[j] += x[j][e];
     }
-    total = ca_sum_halves(total);
-    if (!((here >> (col >> 4)) & 1)) total = 0.f;
-    if (a.way > 1) {
-      if (half == 0) s_sum[wave][col] = total;
+  };
+  auto last_of = [&](int b) { return last_seen(seq, min(b * 32 + 31, pairs - 1) / a.group, a.causal); };   // what block b sees
+  auto write = [&](int piece, bool has_page, float sum) {
+    const int t = piece * 32 + col;
+    if (half || t >= seq.length) return;
+    const long long at = (long long)blockIdx.x * a.batch.max_pages * a.cache.page_tokens + t;
+    sum = has_page ? sum : 0.f;   // (slots of no page: whatever came of the first page's keys)
+    a.out[at] = a.before ? a.decay * a.before[at] + sum : sum;
+  };
+
+  const int step = gridDim.y * W::PIECES;
+  int piece = blockIdx.y * W::PIECES + wave / W::WAY * TB;
+  ca_u32x4 k[TB][STEPS], q[STEPS];
+  float lse = 0.f;
+  if constexpr (MANY) {
+    for (; piece < pieces; piece += step) {   // (the same for all of a workgroup)
+      const int pages = pages_at(piece), t0 = piece * 32;
+      const unsigned here = (unsigned)__ballot(pages >= 0);
+      load_keys(piece, pages, k);
+#pragma unroll
+      for (int j = 0; j < TB; ++j) total[j] = 0.f;
+      int b = wave;
+      while (b < blocks && t0 > last_of(b)) b += W::WAY;
+      ca_u32x4 ahead[STEPS];
+      float next_lse = 0.f;
+      if (b < blocks) load_queries(b, ahead, next_lse);
+      for (; b < blocks; b += W::WAY) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) q[i] = ahead[i];
+        lse = next_lse;
+        if (b + W::WAY < blocks) load_queries(b + W::WAY, ahead, next_lse);
+        place_block(b, lse);
+        add_block(b, t0, k, q);
+      }
+#pragma unroll
+      for (int j = 0; j < TB; ++j) {
+        total[j] = ca_sum_halves(total[j]);
+        if (half == 0) s_sum[wave][j][col] = total[j];
+      }
       __syncthreads();
-      total = s_sum[0][col] + s_sum[1][col] + s_sum[2][col] + s_sum[3][col];
+      if (wave < TB) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < W::WAVES; ++w) sum += s_sum[w][wave][col];
+        write(piece + wave, (here >> (2 * wave + (col >> 4))) & 1, sum);
+      }
       __syncthreads();
     }
-    if (half == 0 && wave % a.way == 0 && t < seq.length) {
-      const long long at = (long long)blockIdx.x * a.batch.max_pages * a.cache.page_tokens + t;
-      a.out[at] = a.before ? a.decay * a.before[at] + total : total;
+  } else {
+    ca_u32x4 ahead[TB][STEPS];
+    int pages = pages_at(piece), next_pages = pages_at(piece + step), held = -1;   // (-1 past the length)
+    if (piece < pieces) load_keys(piece, pages, ahead);
+    for (; piece < pieces; piece += step) {   // (a wave by itself)
+      const bool has_page = ((unsigned)__ballot(pages >= 0) >> (col >> 4)) & 1;
+      const int t0 = piece * 32;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) k[0][i] = ahead[0][i];
+      pages = next_pages;
+      if (piece + step < pieces) {
+        next_pages = pages_at(piece + 2 * step);
+        load_keys(piece + step, pages, ahead);
+      }
+      total[0] = 0.f;
+      for (int b = 0; b < blocks; ++b) {
+        if (t0 > last_of(b)) continue;
+        if (b != held) {
+          load_queries(b, q, lse);
+          place_block(b, lse);
+          held = b;
+        }
+        add_block(b, t0, k, q);
+      }
+      write(piece, has_page, ca_sum_halves(total[0]));
     }
   }
 }

@@ -452,7 +452,7 @@ typedef struct spark_cache_batch {
   uint32_t size;          /* sizeof(spark_cache_batch) */
   int32_t m;              /* rows of the row operands, up to 2^22 */
   int32_t n;              /* sequences, up to 2^16 */
-  int32_t max_pages;      /* pages a sequence has at most; slots (times page_tokens) up to 2^24 */
+  int32_t max_pages;      /* pages a sequence has at most; slots (times page_tokens) up to 2^23 */
   const int32_t *starts;  /* [n + 1] */
   const int32_t *lengths; /* [n] */
   const int32_t *table;   /* [n][max_pages] */
@@ -477,7 +477,7 @@ typedef struct spark_rotation {
 /* q [m][n_q_heads][head_dim], k and v [m][n_kv_heads][head_dim] of src_dtype, each with its stride, on their way
  * into the cache: queries turned and rounded once to the cache's type in q_out [m][n_q_heads][head_dim] (q itself
  * if the types and strides are the same), keys turned and values as they are, rounded once, to their rows' slots.
- * n_q_heads is a multiple of n_kv_heads, up to 2^12, and m * n_q_heads up to 2^28 (in all of these calls).  rotation [host] is read before the call returns. */
+ * n_q_heads is a multiple of n_kv_heads, up to 2^12, and m * n_q_heads up to 2^26 (in all of these calls).  rotation [host] is read before the call returns. */
 int spark_cache_append(const spark_cache *cache, const spark_cache_batch *batch, const spark_rotation *rotation,
                        int32_t n_q_heads, int32_t src_dtype, const void *q, int64_t q_stride, const void *k,
                        int64_t k_stride, const void *v, int64_t v_stride, void *q_out, int64_t out_stride,

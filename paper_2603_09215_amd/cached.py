@@ -55,13 +55,13 @@ def _call(what: str, cache, batch, tensors, written, call, *args):
     _launch(what, (cache.pool, *tensors), written, call, *args)
 
 
-_ROTATION_BYTES = C.sizeof(SparkRotation)
+_CACHE_BYTES, _BATCH_BYTES, _ROTATION_BYTES = C.sizeof(SparkCache), C.sizeof(SparkCacheBatch), C.sizeof(SparkRotation)
 
 
 class PagedCache:
     """Keys and values in pages: `pool` [page][layer][k|v][kv_head][token in its page][head_dim], fp32 or bf16, head_dim 64 or 128,
     pages of a multiple of 16 tokens."""
-    __slots__ = ("pool", "pages", "layers", "kv_heads", "page_tokens", "head_dim", "device", "_types", "_views", "_workspace")
+    __slots__ = ("pool", "pages", "layers", "kv_heads", "page_tokens", "head_dim", "device", "_types", "_workspace")
 
     def __init__(self, pool: torch.Tensor):
         if not isinstance(pool, torch.Tensor) or pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_cuda or not pool.is_contiguous() or pool.dtype not in _DTYPE:
@@ -71,7 +71,6 @@ class PagedCache:
                 self.page_tokens % 16 == 0 and self.head_dim in (64, 128)):
             _refuse(f"pool: {tuple(pool.shape)}; pages of 16 to 65536 tokens, a multiple of 16, and heads of 64 or 128 are taken")
         self.pool, self.device, self._types = pool, pool.device, (pool.dtype,)
-        self._views = {}
         self._workspace = {}   # sizes -> bytes
 
     @classmethod
@@ -79,20 +78,16 @@ class PagedCache:
         return cls(torch.empty(pages, layers, 2, kv_heads, page_tokens, head_dim, dtype=dtype, device=device))
 
     def _view(self, layer: int) -> SparkCache:
-        v = self._views.get(layer)
-        if v is None:
-            if not 0 <= layer < self.layers:
-                _refuse(f"layer {layer} of {self.layers}")
-            v = self._views[layer] = SparkCache(C.sizeof(SparkCache), _DTYPE[self.pool.dtype], self.pages, self.layers, self.kv_heads, self.page_tokens,
-                                                self.head_dim, layer, self.pool.data_ptr())
-        return v
+        if not 0 <= layer < self.layers:
+            _refuse(f"layer {layer} of {self.layers}")
+        return SparkCache(_CACHE_BYTES, _DTYPE[self.pool.dtype], self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim, layer, self.pool.data_ptr())
 
 
 class CachedRows:
     """A batch of n sequences: rows starts[s] .. starts[s + 1] - 1 are the new ones of sequence s, which are the last of its lengths[s]
     slots; table [n][pages a sequence has at most] holds its pages.  All int32 on the GPU; what they hold is read by each
     call (it may change between calls and between replays of a graph)."""
-    __slots__ = ("starts", "lengths", "table", "n", "max_pages", "device", "_batch")
+    __slots__ = ("starts", "lengths", "table", "n", "max_pages", "device")
 
     def __init__(self, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
         self.starts, self.lengths, self.table = _table(starts, "starts", 1), _table(lengths, "lengths", 1), _table(table, "table", 2)
@@ -104,15 +99,13 @@ class CachedRows:
         self.device = table.device
         if starts.device != self.device or lengths.device != self.device:
             _refuse("the tensors are on different devices")
-        self._batch = SparkCacheBatch(C.sizeof(SparkCacheBatch), 0, self.n, self.max_pages, starts.data_ptr(), lengths.data_ptr(), table.data_ptr())
 
     def _of(self, m: int, cache: PagedCache) -> SparkCacheBatch:
         """for calls on m rows"""
-        if m > 1 << 22 or self.max_pages * cache.page_tokens > 1 << 24 or self.n * cache.kv_heads > 1 << 20:
-            _refuse(f"{m} rows, {self.max_pages} pages of {cache.page_tokens}, {self.n} sequences with {cache.kv_heads} heads: up to 2^22 rows, 2^24 slots "
+        if m > 1 << 22 or self.max_pages * cache.page_tokens > 1 << 23 or self.n * cache.kv_heads > 1 << 20:
+            _refuse(f"{m} rows, {self.max_pages} pages of {cache.page_tokens}, {self.n} sequences with {cache.kv_heads} heads: up to 2^22 rows, 2^23 slots "
                     "a sequence and 2^20 heads of sequences are taken")
-        b = self._batch
-        return b if b.m == m else SparkCacheBatch(b.size, m, b.n, b.max_pages, b.starts, b.lengths, b.table)
+        return SparkCacheBatch(_BATCH_BYTES, m, self.n, self.max_pages, self.starts.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr())
 
 
 class Rotation:
@@ -151,9 +144,9 @@ def _gain(t, what: str, head_dim: int):
     return None if t is None else _plain(t, what, head_dim)
 
 
-def _group(q_heads: int, cache: PagedCache):
-    if not 1 <= q_heads <= 1 << 12 or q_heads % cache.kv_heads:
-        _refuse(f"{q_heads} query heads and {cache.kv_heads} of keys: a multiple is wanted, up to 4096")
+def _group(m: int, q_heads: int, cache: PagedCache):
+    if not 1 <= q_heads <= 1 << 12 or q_heads % cache.kv_heads or m * q_heads > 1 << 26:
+        _refuse(f"{m} rows of {q_heads} query heads and {cache.kv_heads} of keys: a multiple of these is wanted, up to 4096, and up to 2^26 with all rows'")
 
 
 def cached_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: int = 0, rotation: Rotation | None = None,
@@ -165,7 +158,7 @@ def cached_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Page
     hd = cache.head_dim
     q_at, q_stride = _heads(q, "q", hd, _DTYPE)
     m, heads, _ = q.shape
-    _group(heads, cache)
+    _group(m, heads, cache)
     types, of_kv = (q.dtype,), (m, cache.kv_heads)
     k_at, k_stride = _heads(k, "k", hd, types, of_kv)
     v_at, v_stride = _heads(v, "v", hd, types, of_kv)
@@ -213,7 +206,7 @@ def attend_workspace_bytes(cache: PagedCache, batch: CachedRows, m: int, q_heads
     """of cached_attend with m rows"""
     need = cache._workspace.get((m, q_heads, batch.n, batch.max_pages))
     if need is None:
-        _group(q_heads, cache)
+        _group(m, q_heads, cache)
         size = C.c_size_t()
         with torch.cuda.device(cache.pool.device):
             if load_library().spark_cache_workspace_bytes(cache._view(0), batch._of(m, cache), q_heads, C.byref(size)):
@@ -230,7 +223,7 @@ def cached_attend(q: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: 
     hd = cache.head_dim
     at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape
-    _group(heads, cache)
+    _group(m, heads, cache)
     given = tuple(t for t in (out, lse) if t is not None)
     if out is None:
         out = torch.empty(m, heads, hd, dtype=q.dtype, device=q.device)
@@ -259,7 +252,7 @@ def cached_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: C
     hd = cache.head_dim
     at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape
-    _group(heads, cache)
+    _group(m, heads, cache)
     _wide("q", at, stride)
     lse_at = _plain(lse, "lse", m, heads)
     before_at = None if before is None else _weights(before, "before", cache, batch)

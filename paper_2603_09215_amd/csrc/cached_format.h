@@ -46,8 +46,9 @@ __device__ __forceinline__ Sequence sequence(const BatchView &b, int s, int page
   return q;
 }
 
-// Which of a sequence's pages holds its slots 16 n .. 16 n + 15, and from which of the page's tokens on.  n is below 2^20 and a page
-// has at most 2^12 sixteens, so the product with the rounded reciprocal is off by less than one sixteenth of a page: exact.
+// Which of a sequence's pages holds its slots 16 n .. 16 n + 15, and from which of the page's tokens on.  n stays below 2^20 (2^19
+// sixteens of a sequence, and the few that are asked for ahead) and a page has at most 2^12, so the product with the rounded
+// reciprocal, off by less than n / 2^32 of 2^12 parts, is exact when cut.
 __device__ __forceinline__ void place_of(const CacheView &c, int n, int &index, int &token) {
   index = c.reciprocal ? (int)__umulhi((uint32_t)n, c.reciprocal) : n;
   token = (n - index * c.sixteens) * 16;

@@ -25,10 +25,10 @@ bool sizes_ok(const spark_cache *c, const spark_cache_batch *b) {
          within(c->n_layers, 1, 1 << 16) && within(c->n_kv_heads, 1, 1 << 12) && within(c->page_tokens, 16, 1 << 16) && c->page_tokens % 16 == 0 &&
          (c->head_dim == 64 || c->head_dim == 128) && within(c->layer, 0, c->n_layers - 1) && within(b->m, 0, 1 << 22) && within(b->n, 0, 1 << 16) &&
          (int64_t)b->n * c->n_kv_heads <= 1 << 20 &&
-         within(b->max_pages, 1, 1 << 24) && (int64_t)b->max_pages * c->page_tokens <= 1 << 24;
+         within(b->max_pages, 1, 1 << 24) && (int64_t)b->max_pages * c->page_tokens <= 1 << 23;
 }
 bool heads_ok(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_heads) {
-  return within(n_q_heads, 1, 1 << 12) && n_q_heads % c->n_kv_heads == 0 && (int64_t)b->m * n_q_heads <= 1 << 28;
+  return within(n_q_heads, 1, 1 << 12) && n_q_heads % c->n_kv_heads == 0 && (int64_t)b->m * n_q_heads <= 1 << 26;
 }
 bool batch_ok(const spark_cache *c, const spark_cache_batch *b) {
   return sizes_ok(c, b) && aligned(c->pool, 16) && aligned(b->starts, 4) && aligned(b->lengths, 4) && aligned(b->table, 4);

@@ -75,6 +75,8 @@ def test_caches_and_batches(lib):
             assert call(lib, b=batch(**kw)) == EINVAL, (call, kw)
         for heads in (0, -2, 3, (1 << 12) + 2):
             assert call(lib, heads=heads) == EINVAL, (call, heads)
+        wide = dict(qs=4096, os=4096) if call is not weigh else dict(qs=4096)
+        assert call(lib, b=batch(m=1 << 22), heads=32, **wide) == EINVAL
 
 
 def test_append_arguments(lib):

@@ -112,3 +112,4 @@ def test_sizes_past_the_calls_limits():
         b.n, b.max_pages = n, pages
         refused(lambda: b._of(m, c), "are taken")
     refused(lambda: cached.cached_append(on(3, 6, 64), on(3, 4, 64), on(3, 4, 64), cached.PagedCache(on(4, 2, 2, 4, 16, 64)), b), "a multiple")
+    refused(lambda: cached._group((1 << 14) + 1, 1 << 12, c), "2\\^26")

@@ -1,0 +1,356 @@
+"""Attention over a paged cache and its slots' weights at lengths that take every kernel and several parts, against the formulas in 64 bits;
+graphs, streams, large pools, and the operators one behind the other."""
+import math
+
+import pytest
+import torch
+
+import cached_ref as ref
+from test_gpu_cached import gpu, make_batch, near, rows_of, same
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = {"fp32": F32, "bf16": BF16}
+
+# (rows, length) of each sequence, page, query heads, kv heads, head_dim, type, causal
+LONG = [
+    ([(1, 3000), (1, 700), (1, 1)], 64, 7, 1, 128, "bf16", True),
+    ([(1, 100), (1, 90)], 16, 4, 2, 64, "bf16", True),
+    ([(1, 2900)], 80, 16, 4, 64, "bf16", True),
+    ([(1, 120)], 64, 28, 4, 128, "bf16", True),
+    ([(3, 2000), (0, 1500), (7, 1999)], 48, 24, 1, 128, "bf16", False),
+    ([(300, 1000)], 64, 28, 4, 128, "bf16", True),
+    ([(130, 3000), (5, 2990)], 16, 16, 2, 128, "bf16", True),
+    ([(500, 500), (400, 450)], 64, 28, 4, 128, "bf16", True),
+    ([(900, 901)], 16, 14, 2, 64, "bf16", True),
+    ([(700, 2500)], 64, 28, 4, 128, "bf16", True),
+    ([(2500, 2600), (10, 2000)], 80, 28, 4, 128, "bf16", True),
+    ([(1500, 1500)], 32, 28, 2, 64, "bf16", True),
+    ([(1500, 4000)], 64, 32, 2, 64, "bf16", False),
+    ([(3500, 3500)], 64, 32, 2, 64, "bf16", True),
+    ([(1, 2000), (1, 1999)], 64, 7, 1, 128, "fp32", True),
+    ([(40, 60)], 16, 28, 4, 128, "fp32", True),
+    ([(200, 600), (180, 300)], 48, 14, 2, 64, "fp32", True),
+    ([(1, 4000), (30, 2000)], 16, 4, 2, 64, "fp32", False),
+]
+
+
+def attend_64(q, pool, b, layer, scale, causal):
+    """(out, tolerance, lse, tolerance) as cached_ref.attend, on the GPU, a head at a time"""
+    m, nq, hd = q.shape
+    group, u = nq // pool.shape[3], ref.U
+    out, lse = torch.full((m, nq, hd), math.nan, dtype=torch.float64), torch.full((m, nq), math.nan, dtype=torch.float64)
+    tol, lse_tol = torch.zeros_like(out), torch.zeros_like(lse)
+    step = ref.half_step(pool.dtype)
+    for s in range(b.n):
+        r0, rows, length = b.row0[s], b.rows[s], b.length[s]
+        if rows == 0:
+            continue
+        slot = torch.arange(length, device="cuda")
+        table = torch.tensor(b.table[s], device="cuda")
+        page = table[slot // b.pt]
+        there = (page >= 0) & (page < b.n_pages)
+        page = page.clamp(0, b.n_pages - 1).long()
+        last = torch.arange(length - rows, length, device="cuda")
+        limit = last if causal else torch.where(last < 0, -1, length - 1)
+        sees = (slot[None] <= limit[:, None]) & there[None]
+        for h in range(nq):
+            k, v = (torch.where(there[:, None], pool[page, layer, w, h // group, slot % b.pt].double(), 0.0) for w in (0, 1))
+            x = q[r0:r0 + rows, h].double()
+            sc = (x @ k.t().contiguous() * scale).masked_fill(~sees, -math.inf)
+            off = (x.abs() @ k.abs().t().contiguous() * abs(scale) * (hd + 3) * u).masked_fill(~sees, 0.0)
+            top = sc.amax(1, keepdim=True)
+            top = torch.where(top == -math.inf, 0.0, top)
+            p = torch.exp(sc - top)
+            total = p.sum(1, keepdim=True)
+            none = total == 0
+            p = p / torch.where(none, 1.0, total)
+            n = sees.sum(1, keepdim=True)
+            each = off + off.amax(1, keepdim=True) + (4 + 2 * torch.where(sees, top - sc, 0.0)) * 2 * u
+            o, mags = p @ v, p @ v.abs()
+            share = (p * each).sum(1, keepdim=True)
+            t = (p * each) @ v.abs() + mags * (share + 4 * (n + 16) * u) + step * o.abs()
+            if pool.dtype == BF16:
+                t = t + step * mags
+            out[r0:r0 + rows, h], tol[r0:r0 + rows, h] = o.cpu(), t.cpu()
+            lse[r0:r0 + rows, h] = torch.where(none, -math.inf, top + torch.log(total))[:, 0].cpu()
+            lse_tol[r0:r0 + rows, h] = (share + off.amax(1, keepdim=True) + (n + 16) * 2 * u + 4 * u * (top.abs() + torch.where(none, 0.0, total.log())))[:, 0].cpu()
+    return out, tol, lse, lse_tol
+
+
+def weigh_64(q, lse, pool, b, scale, causal):
+    """(weights without earlier ones, tolerance) as cached_ref.weigh, on the GPU"""
+    nkv, nq, hd, u = pool.shape[3], q.shape[1], q.shape[2], ref.U
+    group = nq // nkv
+    out = torch.full((b.n, nkv, b.slots), math.nan, dtype=torch.float64)
+    tol = torch.zeros_like(out)
+    for s in range(b.n):
+        r0, rows, length = b.row0[s], b.rows[s], b.length[s]
+        out[s, :, :length] = 0.0
+        if rows == 0:
+            continue
+        slot = torch.arange(length, device="cuda")
+        page = torch.tensor(b.table[s], device="cuda")[slot // b.pt].long()
+        limit = torch.arange(length - rows, length, device="cuda") if causal else torch.full((rows,), length - 1, device="cuda")
+        sees = slot[None] <= limit[:, None]
+        for h in range(nq):
+            k = pool[page, 0, 0, h // group, slot % b.pt].double()
+            x, l = q[r0:r0 + rows, h].double(), lse[r0:r0 + rows, h, None].double()
+            sc = x @ k.t().contiguous() * scale
+            off = x.abs() @ k.abs().t().contiguous() * abs(scale) * (hd + 3) * u
+            p = torch.exp(sc - l).masked_fill(~sees, 0.0)
+            out[s, h // group, :length] += p.sum(0).cpu()
+            tol[s, h // group, :length] += (p * (off + (4 + 2 * (sc - l).abs() + l.abs()) * 2 * u)).sum(0).cpu()
+        tol[s] += (rows * group + 2) * u * torch.nan_to_num(out[s]).abs()
+    return out, tol
+
+
+def full_pool(pages, layers, nkv, page, hd, dtype, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(pages, layers, 2, nkv, page, hd, generator=g, device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("shape,page,nq,nkv,hd,dtype,causal", LONG)
+def test_long(shape, page, nq, nkv, hd, dtype, causal):
+    c, dtype = gpu(), TYPES[dtype]
+    starts, lengths, table, pages, m = make_batch(shape, page, 41, before=1, behind=2)
+    b = ref.Batch(starts, lengths, table, m, pages, page)
+    pool = full_pool(pages, 1, nkv, page, hd, dtype, 42)
+    for s in range(b.n):   # rubbish behind the lengths
+        for t in range(b.length[s], b.slots):
+            pool[b.page(s, t), :, :, :, t % page] = math.nan if t % 2 else math.inf
+    q = rows_of(m, nq, hd, dtype, 43)
+    cache, batch = c.PagedCache(pool), c.CachedRows(starts.cuda(), lengths.cuda(), table.cuda())
+    lse = torch.full((m, nq), 7.0, device="cuda")
+    out = c.cached_attend(q, cache, batch, causal=causal, lse=lse, out=torch.full_like(q, 7.0))
+    want, tol, want_lse, lse_tol = attend_64(q, pool, b, 0, hd ** -0.5, causal)
+    near(lse, want_lse, lse_tol, "lse")
+    near(out, want, tol, "out")
+    nobody = want_lse.isnan()
+    assert bool((out.cpu()[nobody] == 7).all()) and bool((lse.cpu()[nobody] == 7).all())
+    # as a whole: half a step of each result is the rounding that there has to be, and bf16 rounds the probabilities too; errors of random signs
+    there = ~nobody
+    off = (out.cpu().double() - want)[there]
+    if dtype == BF16:
+        assert float(off.norm() / want[there].norm()) < 2.0 ** -8
+    assert same(c.cached_attend(q, cache, batch, causal=causal)[there.any(1).cuda()], out[there.any(1).cuda()])
+    weights = c.cached_weigh(q, lse, cache, batch, causal=causal)
+    want, tol = weigh_64(q, lse, pool, b, hd ** -0.5, causal)
+    near(weights, want, tol, "weights")
+    assert bool((weights.cpu()[want.isnan()] == 0).all())
+
+
+@pytest.mark.parametrize("shape,nq,nkv,hd", [([(1, 1500)], 7, 1, 128), ([(200, 1500)], 28, 4, 128), ([(1200, 1300)], 28, 4, 64)])
+def test_no_number_behind_other_parts(shape, nq, nkv, hd):
+    """an infinite value in a row's own slot, where tokens are cut in parts: it is the result of the rows that see it, and of no other"""
+    c = gpu()
+    starts, lengths, table, pages, m = make_batch(shape, 64, 44)
+    b = ref.Batch(starts, lengths, table, m, pages, 64)
+    pool = full_pool(pages, 1, nkv, 64, hd, BF16, 45)
+    q = rows_of(m, nq, hd, BF16, 46)
+    batch = c.CachedRows(starts.cuda(), lengths.cuda(), table.cuda())
+    clean = c.cached_attend(q, c.PagedCache(pool), batch)
+    row = shape[0][0] // 3
+    slot = b.slot(0, row)
+    for value in (math.inf, math.nan):
+        bad = pool.clone()
+        bad[b.page(0, slot), 0, 1, :, slot % 64, hd - 1] = value
+        got = c.cached_attend(q, c.PagedCache(bad), batch)
+        assert same(got[:row], clean[:row])
+        hit = got[row:, :, -1].float()
+        assert bool(hit.isnan().all()) if math.isnan(value) else bool((hit == value).all())
+        assert bool(torch.isfinite(got[row:, :, :-1]).all())
+
+
+def test_the_same_page_twice():
+    """two sequences, and two places of one, may read one page"""
+    c = gpu()
+    starts, lengths = torch.tensor([0, 2, 5], dtype=torch.int32), torch.tensor([60, 40], dtype=torch.int32)
+    table = torch.tensor([[3, 1, 3, 0], [1, 3, 1, 2]], dtype=torch.int32)
+    b = ref.Batch(starts, lengths, table, 5, 4, 16)
+    pool = full_pool(4, 1, 2, 16, 64, F32, 47)
+    q = rows_of(5, 4, 64, F32, 48)
+    lse = torch.empty(5, 4, device="cuda")
+    out = c.cached_attend(q, c.PagedCache(pool), c.CachedRows(starts.cuda(), lengths.cuda(), table.cuda()), lse=lse)
+    want, tol, want_lse, lse_tol = ref.attend(q.cpu(), pool.cpu(), b, 0, 64 ** -0.5)
+    near(out, want, tol, "out")
+    near(lse, want_lse, lse_tol, "lse")
+
+
+def test_offsets_past_32_bits():
+    """pages whose elements lie past 2^32: the same bits as in a small pool"""
+    c = gpu()
+    layers, nkv, page, hd, pages = 64, 4, 64, 128, 1100
+    big = torch.empty(pages, layers, 2, nkv, page, hd, dtype=BF16, device="cuda")   # 9 GB, 4.6e9 elements
+    assert big.numel() > 1 << 32
+    g = torch.Generator(device="cuda").manual_seed(49)
+    where = [1099, 1050, 1098, 1030]
+    small = torch.randn(4, 1, 2, nkv, page, hd, generator=g, device="cuda").to(BF16)
+    starts, lengths = torch.tensor([0, 3, 4], dtype=torch.int32, device="cuda"), torch.tensor([100, 70], dtype=torch.int32, device="cuda")
+    results = []
+    for pool, layer, ids in ((small, 0, [0, 1, 2, 3]), (big, layers - 1, where)):
+        if pool is big:
+            big[where, layer] = start
+        else:
+            start = small[:, 0].clone()
+        cache, batch = c.PagedCache(pool), c.CachedRows(starts, lengths, torch.tensor(ids, dtype=torch.int32, device="cuda").view(2, 2))
+        q, k, v = (rows_of(4, h, hd, F32, 50 + i) for i, h in enumerate((8, nkv, nkv)))
+        q = c.cached_append(q, k, v, cache, batch, layer=layer, rotation=c.Rotation(hd))
+        lse = torch.empty(4, 8, device="cuda")
+        out = c.cached_attend(q, cache, batch, layer=layer, lse=lse)
+        w = c.cached_weigh(q, lse, cache, batch, layer=layer)
+        kept, new = c.cached_evict(cache, batch, w, 50, 1, 4, layer=layer)
+        results.append((q, lse, out, w, kept, new, pool[ids, layer].clone()))
+    for x, y in zip(*results):
+        assert same(x, y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_graph_of_all_four(dtype):
+    """captured once, replayed with other lengths, positions, pages and values in between, against eager calls each time"""
+    c = gpu()
+    nq, nkv, hd, page, pages = 8, 2, 64, 16, 64
+    starts = torch.tensor([0, 1, 5], dtype=torch.int32, device="cuda")
+    lengths, table = torch.tensor([300, 80], dtype=torch.int32, device="cuda"), torch.arange(48, dtype=torch.int32, device="cuda").view(2, 24)
+    spare = torch.arange(48, 64, dtype=torch.int32, device="cuda").view(2, 8)
+    pool, q, k, v = full_pool(pages, 1, nkv, page, hd, dtype, 51), *(rows_of(5, h, hd, F32, 52 + i) for i, h in enumerate((nq, nkv, nkv)))
+    positions = torch.arange(5, dtype=torch.int32, device="cuda")
+    turn, gain = c.Rotation(hd), torch.rand(hd, device="cuda")
+    weights = torch.zeros(2, nkv, 24 * page, device="cuda")
+
+    def step(cache, batch, weights):
+        turned = c.cached_append(q, k, v, cache, batch, rotation=turn, q_gain=gain, k_gain=gain, positions=positions)
+        lse = torch.empty(5, nq, device="cuda")
+        out = c.cached_attend(turned, cache, batch, lse=lse)
+        c.cached_weigh(turned, lse, cache, batch, before=weights, decay=0.5, out=weights)
+        moved = torch.zeros_like(weights)
+        kept, new = c.cached_evict(cache, batch, weights, 100, 4, 8, table_out=spare, weights_out=moved)
+        return turned, lse, out, kept, new, moved
+
+    cache, batch = c.PagedCache(pool), c.CachedRows(starts, lengths, table)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(cache, batch, weights)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = step(cache, batch, weights)
+    g = torch.Generator().manual_seed(53)
+    for trial in range(4):
+        lengths.copy_(torch.tensor([[384, 5], [1, 384], [200, 199], [7, 100]][trial], dtype=torch.int32))
+        table.copy_(torch.randperm(48, generator=g).view(2, 24).int())
+        positions.copy_(torch.randint(0, 100000, (5,), generator=g).int())
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g))
+        weights.copy_(torch.rand(weights.shape, generator=g))
+        other, other_weights = c.PagedCache(pool.clone()), weights.clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        want = step(other, batch, other_weights)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert same(x, y), trial
+        assert same(pool, other.pool) and same(weights, other_weights)
+
+
+def test_two_streams_at_once():
+    c = gpu()
+    shapes = [[(1, 4000)] * 4, [(300, 1500)]]
+    calls = []
+    for i, shape in enumerate(shapes):
+        starts, lengths, table, pages, m = make_batch(shape, 64, 54 + i)
+        calls.append((rows_of(m, 28, 128, BF16, 56 + i), c.PagedCache(full_pool(pages, 1, 4, 64, 128, BF16, 58 + i)), c.CachedRows(starts.cuda(), lengths.cuda(), table.cuda())))
+    want = [c.cached_attend(*a) for a in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[], []]
+    for _ in range(5):
+        for i, (s, a) in enumerate(zip(streams, calls)):
+            with torch.cuda.stream(s):
+                got[i].append(c.cached_attend(*a))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(same(x, want[i]) for x in got[i])
+
+
+def test_gradients_and_versions():
+    from paper_2603_09215_amd import SparkError
+    c = gpu()
+    starts, lengths, table, pages, m = make_batch([(2, 20)], 16, 60)
+    cache, batch = c.PagedCache(full_pool(pages, 1, 1, 16, 64, F32, 61)), c.CachedRows(starts.cuda(), lengths.cuda(), table.cuda())
+    q, k, v = (rows_of(m, h, 64, F32, 62 + i) for i, h in enumerate((2, 1, 1)))
+    wanted = q.clone().requires_grad_()
+    lse, w = torch.zeros(m, 2, device="cuda"), torch.zeros(1, 1, 32, device="cuda")
+    for call in (lambda: c.cached_append(wanted, k, v, cache, batch), lambda: c.cached_append(q, k, wanted[:, :1], cache, batch),
+                 lambda: c.cached_append(q, k, v, cache, batch, q_gain=torch.ones(64, device="cuda", requires_grad=True)), lambda: c.cached_attend(wanted, cache, batch),
+                 lambda: c.cached_weigh(wanted, lse, cache, batch), lambda: c.cached_evict(cache, batch, w.clone().requires_grad_(), 10)):
+        with pytest.raises(SparkError, match="no derivatives"):
+            call()
+    with torch.no_grad():
+        assert same(c.cached_attend(wanted, cache, batch), c.cached_attend(q, cache, batch))
+    for call, tensors in ((lambda: c.cached_append(q, k, v, cache, batch, out=q), (cache.pool, q)), (lambda: c.cached_attend(q, cache, batch, lse=lse), (lse,)),
+                          (lambda: c.cached_weigh(q, lse, cache, batch, before=w, out=w), (w,)), (lambda: c.cached_evict(cache, batch, w, 10), (cache.pool, w))):
+        before = [t._version for t in tensors]
+        call()
+        assert all(t._version > x for t, x in zip(tensors, before))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_dialogues_with_eviction(dtype, in_place):
+    """prompts, steps and evictions of two dialogues with two layers, as a program runs them: every result is attention over the keys and values that were
+    written for the slots that are still kept (taken from the cache when they were written), in 64 bits"""
+    c = gpu()
+    nq, nkv, hd, page, layers, most, keep, recent = 6, 2, 64, 16, 2, 8, 70, 10
+    group, scale = nq // nkv, hd ** -0.5
+    cache = c.PagedCache(full_pool(4 * most, layers, nkv, page, hd, dtype, 70))
+    tables = [torch.randperm(4 * most)[:2 * most].view(2, most).int().cuda()]
+    tables.append(torch.tensor(sorted(set(range(4 * most)) - set(tables[0].flatten().tolist())), dtype=torch.int32).view(2, most).cuda())
+    turn, gain = c.Rotation(32, interleaved=True), torch.rand(hd, device="cuda") + 0.5
+    lengths, position = [0, 0], [0, 0]
+    weights = [torch.zeros(2, nkv, most * page, device="cuda") for _ in range(layers)]
+    shadow = [[[[] for _ in range(nkv)] for _ in range(2)] for _ in range(layers)]   # [layer][dialogue][head] -> (key, value) of each slot
+    table = tables[0]
+    for rows in [(40, 61), (1, 1), (1, 1), (30, 1), (1, 1), (1, 25), (1, 1)]:
+        starts = torch.tensor([0, rows[0], sum(rows)], dtype=torch.int32, device="cuda")
+        lengths = [a + r for a, r in zip(lengths, rows)]
+        batch = c.CachedRows(starts, torch.tensor(lengths, dtype=torch.int32, device="cuda"), table)
+        positions = torch.cat([torch.arange(p, p + r) for p, r in zip(position, rows)]).int().cuda()
+        position = [p + r for p, r in zip(position, rows)]
+        m = sum(rows)
+        for layer in range(layers):
+            qkv = torch.randn(m, (nq + 2 * nkv) * hd, device="cuda").to(dtype)
+            q, k, v = (t.unflatten(1, (-1, hd)) for t in qkv.split([nq * hd, nkv * hd, nkv * hd], 1))
+            turned = c.cached_append(q, k, v, cache, batch, layer=layer, rotation=turn, q_gain=gain, k_gain=gain, positions=positions)
+            lse = torch.empty(m, nq, device="cuda")
+            out = c.cached_attend(turned, cache, batch, layer=layer, lse=lse)
+            c.cached_weigh(turned, lse, cache, batch, layer=layer, before=weights[layer], decay=0.9, out=weights[layer])
+            pool, tab = cache.pool.cpu(), table.cpu()
+            want, tol = torch.zeros(m, nq, hd, dtype=torch.float64), torch.zeros(m, nq, hd, dtype=torch.float64)
+            for s in range(2):
+                for h in range(nkv):
+                    kept = shadow[layer][s][h]
+                    for t in range(lengths[s] - rows[s], lengths[s]):
+                        kept.append(tuple(pool[tab[s, t // page], layer, w, h, t % page].double() for w in (0, 1)))
+                    assert len(kept) == lengths[s]
+                    keys, values = (torch.stack([x[w] for x in kept]) for w in (0, 1))
+                    # one page each that holds it all, for the reference
+                    flat = torch.zeros(1, 1, 2, 1, lengths[s], hd, dtype=dtype)
+                    flat[0, 0, 0, 0], flat[0, 0, 1, 0] = keys.to(dtype), values.to(dtype)
+                    one = ref.Batch([0, rows[s]], [lengths[s]], [[0]], rows[s], 1, lengths[s])
+                    part = turned.cpu()[int(starts[s]):int(starts[s + 1]), h * group:(h + 1) * group]
+                    a, b_, _, _ = ref.attend(part, flat, one, 0, scale)
+                    want[int(starts[s]):int(starts[s + 1]), h * group:(h + 1) * group], tol[int(starts[s]):int(starts[s + 1]), h * group:(h + 1) * group] = a, b_
+            near(out, want, tol, f"layer {layer} of {rows}")
+        if max(lengths) > keep:
+            other = tables[1] if table is tables[0] else tables[0]
+            for layer in range(layers):
+                before = weights[layer].cpu()
+                kept, new = c.cached_evict(cache, batch, weights[layer], keep, 2, recent, layer=layer, table_out=None if in_place else other)
+                for s in range(2):
+                    for h in range(nkv):
+                        stay = ref.choose(before[s, h].tolist(), lengths[s], keep, 2, recent)
+                        assert kept[s, h, :len(stay)].tolist() == stay
+                        shadow[layer][s][h] = [shadow[layer][s][h][t] for t in stay]
+            lengths = new.tolist()
+            table = table if in_place else other

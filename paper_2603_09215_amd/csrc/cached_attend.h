@@ -121,13 +121,30 @@ __device__ __forceinline__ int last_seen(const Sequence &q, int row, int causal)
   return slot < 0 ? -1 : causal ? slot : q.length - 1;
 }
 
-// the page of each 16 slots from slot 16 (first + i) on in lane i; -1 past `end` or where there is none
-__device__ __forceinline__ int pages_of(const Sequence &q, const CacheView &c, int sixteen, int end) {
-  if (sixteen * 16 >= end) return -1;
-  int index, token;
-  place_of(c, sixteen, index, token);
-  const int p = q.pages[index];
-  return (unsigned)p < (unsigned)c.n_pages ? p : -1;
+// Where sixteen slots of a sequence lie, in a lane of their own: asked for some steps ahead of their use, so what comes of the table
+// is looked at only then.
+struct Asked { int page, token; };      // as the table has it, -1 past `end`
+struct Found { int there, low, high; };   // is there a page, and their bytes from the first page's start on (of the first page where there is none)
+__device__ __forceinline__ Asked ask(const Sequence &q, const CacheView &c, int sixteen, int end) {
+  Asked r{-1, 0};
+  if (sixteen * 16 < end) {
+    int index;
+    place_of(c, sixteen, index, r.token);
+    r.page = q.pages[index];
+  }
+  return r;
+}
+template <int ROW> __device__ __forceinline__ Found find(const Asked &a, const CacheView &c, int type_bytes) {
+  Found f;
+  f.there = (unsigned)a.page < (unsigned)c.n_pages;
+  const unsigned long long at = (unsigned long long)(f.there ? a.page : 0) * (unsigned long long)(c.page_stride * type_bytes) + (unsigned)(a.token * ROW);
+  f.low = (int)(uint32_t)at;
+  f.high = (int)(uint32_t)(at >> 32);
+  return f;
+}
+// the start of the sixteen that lane i found, in the plane that begins at `plane` in the first page
+__device__ __forceinline__ const char *at_lane(const char *plane, const Found &f, int i) {
+  return plane + ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane(f.high, i) << 32 | (uint32_t)__builtin_amdgcn_readlane(f.low, i));
 }
 
 template <typename T, int HD>
@@ -186,9 +203,12 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
   if (threadIdx.x == 0) s_bad = 0;
 
   // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
-  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, piece * S::BLOCKS + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
+  auto ask_piece = [&](int piece) { return ask(seq, a.cache, piece * S::BLOCKS + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
+  constexpr int ROW = HD * (int)sizeof(T);
+  const char *keys = (const char *)a.cache.plane<T>(0, 0, kvh), *values = (const char *)a.cache.plane<T>(0, 1, kvh);
   int piece = first + wave;
-  int pages = pages_at(piece), next_pages = pages_at(piece + S::WAVES);
+  Found found = find<ROW>(ask_piece(piece), a.cache, sizeof(T));
+  Asked asked = ask_piece(piece + S::WAVES);
   const int mine = pair0 + min(col, pairs - 1), my_row = mine / a.group;   // (pairs past the last: that one, not written)
   const int limit = last_seen(seq, my_row, a.causal);
   ca_u32x4 q[S::STEPS];
@@ -205,31 +225,27 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
   ca_u32x4 kr[S::BLOCKS][S::STEPS], vr[S::V_LOADS];
   char *s_v = (char *)ca_smem + wave * S::V_BYTES;
   constexpr int LPT = HD / 8;   // bf16: lanes a token's values take
-  auto load_keys = [&](int piece, int pages) {   // (where there is no page: from the first, of no account)
+  auto load_keys = [&]() {
 #pragma unroll
     for (int i = 0; i < S::BLOCKS; ++i) {
-      int index, in;
-      place_of(a.cache, piece * S::BLOCKS + i, index, in);
-      const ca_u32x4 *k = (const ca_u32x4 *)(a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, i), 0), 0, kvh) + (in + col) * HD) + quad;
+      const char *k = at_lane(keys, found, i);
 #pragma unroll
-      for (int e = 0; e < S::STEPS; ++e) kr[i][e] = k[4 * e];
+      for (int e = 0; e < S::STEPS; ++e) kr[i][e] = *(const ca_u32x4 *)(k + (unsigned)(col * ROW + 64 * e + 16 * quad));
     }
   };
-  auto load_values = [&](int piece, int pages) {
+  auto load_values = [&]() {
 #pragma unroll
     for (int i = 0; i < S::BLOCKS; ++i) {
-      int index, in;
-      place_of(a.cache, piece * S::BLOCKS + i, index, in);
-      const T *v = a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, i), 0), 1, kvh) + in * HD;
+      const char *v = at_lane(values, found, i);
       if constexpr (BF) {
         constexpr int EACH = S::V_LOADS / S::BLOCKS;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) vr[i * EACH + e] = ((const ca_u32x4 *)v)[e * 64 + lane];
+        for (int e = 0; e < EACH; ++e) vr[i * EACH + e] = *(const ca_u32x4 *)(v + (unsigned)(1024 * e + 16 * lane));
       } else {
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vr[d][e] = ((const uint32_t *)v)[(4 * quad + e) * HD + 16 * d + col];
+          for (int e = 0; e < 4; ++e) vr[d][e] = *(const uint32_t *)(v + (unsigned)((4 * quad + e) * ROW + 64 * d + 4 * col));
       }
     }
   };
@@ -260,12 +276,12 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
   };
 
   if (piece < stop) {
-    load_keys(piece, pages);
-    load_values(piece, pages);
+    load_keys();
+    load_values();
   }
   __syncthreads();   // (s_bad)
   for (; piece < stop; piece += S::WAVES) {
-    const unsigned here = (unsigned)__ballot(pages >= 0) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
+    const unsigned here = (unsigned)__ballot(found.there) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
     const int t0 = piece * S::TOKENS;
     ca_f32x4 sc[S::BLOCKS];
 #pragma unroll
@@ -282,10 +298,10 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
         }
       }
     }
-    pages = next_pages;
     if (piece + S::WAVES < stop) {
-      next_pages = pages_at(piece + 2 * S::WAVES);
-      load_keys(piece + S::WAVES, pages);
+      found = find<ROW>(asked, a.cache, sizeof(T));
+      asked = ask_piece(piece + 2 * S::WAVES);
+      load_keys();
     }
     const bool masked = t0 + S::TOKENS - 1 > least || here != (1u << S::BLOCKS) - 1;
     if (masked) {
@@ -309,7 +325,7 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
 #pragma unroll
       for (int d = 0; d < S::V_LOADS; ++d) va[d] = __builtin_bit_cast(ca_f32x4, vr[d]);
     }
-    if (piece + S::WAVES < stop) load_values(piece + S::WAVES, pages);
+    if (piece + S::WAVES < stop) load_values();
 
     float big = -INFINITY;
 #pragma unroll
@@ -414,7 +430,9 @@ template <int HD, int WAVES> struct Tile {
   static constexpr int ROW = HD * (int)sizeof(bf16_t), LPT = ROW / 16;                   // bytes of a token, lanes that they take
   static constexpr int PER = 64 * WAVES / LPT, LOADS = TOKENS / PER;                // tokens of a pass of loads, passes
   static constexpr int BYTES = TOKENS * ROW;
-  static constexpr size_t LDS = 4 * (size_t)BYTES;                                  // keys and values, two buffers
+  static constexpr int O_PITCH = 36;                                                // floats of a pair, of 32 elements
+  static constexpr size_t TILES = 4 * (size_t)BYTES, SUMS = sizeof(float) * PAIRS * (O_PITCH + 2);   // keys and values, two buffers; later results
+  static constexpr size_t LDS = TILES > SUMS ? TILES : SUMS;
 };
 
 template <int HD, int WAVES>
@@ -437,7 +455,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
   if (threadIdx.x == 0) s_bad = 0;
 
   const int p = pair0 + min(wave * 32 + col, pairs - 1), row = p / a.group;
-  const bool live = wave * 32 + col < pairs, works = wave * 32 < pairs;
+  const bool works = wave * 32 < pairs;
   const int limit = last_seen(seq, row, a.causal);
   const int wave_least = last_seen(seq, (pair0 + min(wave * 32, pairs - 1)) / a.group, a.causal);
   const int wave_most = last_seen(seq, (pair0 + min(wave * 32 + 31, pairs - 1)) / a.group, a.causal);
@@ -451,15 +469,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
   char *lds = (char *)ca_smem;
   const int st = threadIdx.x / S::LPT, sc16 = threadIdx.x % S::LPT;   // this thread's token in a pass, and 16 bytes of it
   ca_u32x4 kr[S::LOADS], vr[S::LOADS];
-  // the pages of a tile's four 16s in lanes 0..3
-  auto pages_at = [&](int t) { return pages_of(seq, a.cache, 4 * t + (lane & 3), t < stop ? end : 0); };
-  auto load = [&](int t, int pages, int which, ca_u32x4 (&to)[S::LOADS]) {   // (where there is no page: from the first, of no account)
+  // a tile's four 16s are found by lanes 0..3; a wave's tokens of a pass lie in one of them
+  auto ask_tile = [&](int t) { return ask(seq, a.cache, 4 * t + (lane & 3), t < stop ? end : 0); };
+  const char *planes[2] = {(const char *)a.cache.plane<T>(0, 0, kvh), (const char *)a.cache.plane<T>(0, 1, kvh)};
+  const unsigned in_sixteen = (st & 15) * S::ROW + 16 * sc16;
+  const int sixteen = __builtin_amdgcn_readfirstlane(st >> 4);
+  auto load = [&](const Found &f, int which, ca_u32x4 (&to)[S::LOADS]) {
 #pragma unroll
     for (int i = 0; i < S::LOADS; ++i) {
-      const int token = i * S::PER + st, sixteen = __builtin_amdgcn_readfirstlane(token >> 4);   // (a wave's tokens of a pass share theirs)
-      int index, in;
-      place_of(a.cache, 4 * t + sixteen, index, in);
-      to[i] = ((const ca_u32x4 *)(a.cache.plane<T>(max(__builtin_amdgcn_readlane(pages, sixteen), 0), which, kvh) + (in + (token & 15)) * HD))[sc16];
+      static_assert(S::PER % 16 == 0, "whole 16s a pass");
+      to[i] = *(const ca_u32x4 *)(at_lane(planes[which], f, i * (S::PER / 16) + sixteen) + in_sixteen);
     }
   };
   auto clean = [&](int t, unsigned here) {   // values behind `least`, and of no page
@@ -585,29 +604,31 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
 
   // A tile's values are followed by the next one's scores, so keys come one tile ahead of values: during tile t the buffers hold keys of t + 1
   // (and take those of t + 2) and values of t (and take those of t + 1).
-  int pages_v = pages_at(first), pages_k = pages_at(first + 1), pages_next = pages_at(first + 2);
-  unsigned here = (unsigned)__ballot(pages_v >= 0) & 15u;
+  Asked asked[3] = {ask_tile(first), ask_tile(first + 1), ask_tile(first + 2)};
+  Found found = find<S::ROW>(asked[0], a.cache, sizeof(T)), found_keys = find<S::ROW>(asked[1], a.cache, sizeof(T));
+  unsigned here = (unsigned)__ballot(found.there) & 15u;
   __syncthreads();   // (s_bad)
   if (first < stop) {
-    load(first, pages_v, 0, kr);
-    load(first, pages_v, 1, vr);
+    ca_u32x4 second[S::LOADS];
+    load(found, 0, kr);
+    load(found, 1, vr);
+    load(found_keys, 0, second);
     store(keys_at(first), kr);
-    load(first + 1, pages_k, 0, kr);
     clean(first, here);
     store(values_at(first), vr);
-    store(keys_at(first + 1), kr);
+    store(keys_at(first + 1), second);
     __syncthreads();
     scores(first);
   }
   __syncthreads();   // (the first tile's keys are done with)
   for (int t = first; t < stop; ++t) {
-    pages_v = pages_k;
-    pages_k = pages_next;
-    const unsigned here_next = (unsigned)__ballot(pages_v >= 0) & 15u;
+    found = found_keys;
+    found_keys = find<S::ROW>(asked[2], a.cache, sizeof(T));
+    const unsigned here_next = (unsigned)__ballot(found.there) & 15u;
     if (t + 1 < stop) {
-      pages_next = pages_at(t + 3);
-      load(t + 2, pages_k, 0, kr);
-      load(t + 1, pages_v, 1, vr);
+      asked[2] = ask_tile(t + 3);
+      load(found_keys, 0, kr);   // of t + 2
+      load(found, 1, vr);        // of t + 1
     }
     if (works && t * S::TOKENS <= wave_most) {
       softmax(t, here);
@@ -626,7 +647,6 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
   }
 
   sum = ca_sum_halves(sum);
-  const int r0 = seq.row0 + row, h = kvh * a.group + p % a.group;
   if (s_bad) {   // (the last store lies before the last barrier)
     for (int t = max(first * S::TOKENS, least + 1); t < min(end, stop * S::TOKENS); ++t) {
       const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
@@ -641,12 +661,35 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
         }
     }
   }
-  if (!live) return;
+  // Through LDS, 32 elements at a time, so that eight lanes write 32 elements of a pair next to each other (straight from the registers, where a
+  // store's lanes are 16 bytes of 64 rows: 542 us for 8191 rows instead of 523).
+  float *s_o = (float *)ca_smem + wave * 32 * S::O_PITCH;
+  float2 *s_ml = (float2 *)((float *)ca_smem + S::PAIRS * S::O_PITCH) + wave * 32;
+  if (half == 0) s_ml[col] = make_float2(top, sum);
+  int out_row[4], out_head[4];   // -1: no pair
 #pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
+  for (int i = 0; i < 4; ++i) {
+    const int c = wave * 32 + 8 * i + (lane >> 3), pc = pair0 + c;
+    out_row[i] = c < pairs ? seq.row0 + pc / a.group : -1;
+    out_head[i] = kvh * a.group + pc % a.group;
+  }
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      finish<T, HD>(a, split, r0, h, 32 * d + 8 * i + 4 * half, ca_f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, top, sum);
+      *(ca_f32x4 *)(s_o + col * S::O_PITCH + 8 * i + 4 * half) = ca_f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 8 * i + (lane >> 3);
+      const float2 ml = s_ml[c];
+      if (out_row[i] >= 0)
+        finish<T, HD>(a, split, out_row[i], out_head[i], 32 * d + 4 * (lane & 7), *(const ca_f32x4 *)(s_o + c * S::O_PITCH + 4 * (lane & 7)), ml.x, ml.y);
+    }
+  }
 }
 
 // ------------------------------------------------------------------ the parts together

@@ -177,7 +177,8 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
     };
     if constexpr (sizeof(T) == 2) {   // (fp32 has no tiles)
       if (plan.pairs == 128) go(cached_tile_k<HD, 4>, 256, Tile<HD, 4>::LDS, allow_lds<cached_tile_k<HD, 4>>(Tile<HD, 4>::LDS));
-      else if (plan.pairs == 256) go(cached_tile_k<HD, 8>, 512, Tile<HD, 8>::LDS, allow_lds<cached_tile_k<HD, 8>>(Tile<HD, 8>::LDS));
+      if constexpr (HD == 128)
+        if (plan.pairs == 256) go(cached_tile_k<HD, 8>, 512, Tile<HD, 8>::LDS, allow_lds<cached_tile_k<HD, 8>>(Tile<HD, 8>::LDS));
     }
     if (plan.pairs == 16) go(cached_stream_k<T, HD>, 256, Stream<T, HD>::LDS, true);
     if (ok && plan.splits > 1) {

@@ -14,9 +14,10 @@ struct AttendPlan {
 
 // A kernel's step over `tokens` tokens: us with one workgroup to a compute unit, and with as many as there is room for
 struct AttendKind { int pairs, tokens, room; float us_one, us_full; };
-// [head_dim 128][kernel]: streams of pieces (four waves' pieces a step), tiles of four and of eight waves
-constexpr AttendKind ATTEND_BF16[2][3] = {{{16, 128, 2, 1.2f, 2.0f}, {128, 64, 2, 1.5f, 2.0f}, {256, 64, 1, 1.9f, 1.9f}},
-                                          {{16, 128, 2, 1.55f, 3.2f}, {128, 64, 2, 2.1f, 2.65f}, {256, 64, 1, 2.45f, 2.45f}}};
+// [head_dim 128][kernel]: streams of pieces (four waves' pieces a step), tiles of four waves and of eight (which heads of 64 gain nothing by: 95 us and 83 for
+// 4000 rows of 16 heads; of 128: 528 and 545 for 8191 rows of 28)
+constexpr AttendKind ATTEND_BF16[2][3] = {{{16, 128, 2, 1.2f, 2.0f}, {128, 64, 2, 1.3f, 1.35f}, {}},
+                                          {{16, 128, 2, 1.55f, 3.2f}, {128, 64, 2, 1.83f, 2.2f}, {256, 64, 1, 2.17f, 2.17f}}};
 constexpr AttendKind ATTEND_FP32[2] = {{16, 64, 2, 1.4f, 1.9f}, {16, 64, 2, 2.0f, 3.5f}};
 
 // The plan whose estimate is shortest: rounds of workgroups, each as many steps as its share of the slots has; parts are written, read and
@@ -29,6 +30,7 @@ inline AttendPlan attend_plan(bool fp32, int head_dim, int n_kv_heads, int group
   const AttendKind *kinds = fp32 ? &ATTEND_FP32[head_dim == 128] : ATTEND_BF16[head_dim == 128];
   for (int i = 0; i < (fp32 ? 1 : 3); ++i) {
     const AttendKind &k = kinds[i];
+    if (k.pairs == 0) continue;
     // (every sequence adds at most one tile that is not full)
     const long long tiles = std::min((long long)m * ((group + k.pairs - 1) / k.pairs), (long long)m * group / k.pairs + n);
     const float all = (float)(tiles * n_kv_heads), steps = (float)((slots + k.tokens - 1) / k.tokens);

@@ -44,16 +44,17 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
   const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
   const int pairs = seq.rows * a.group, blocks = (pairs + 31) / 32, pieces = (seq.length + 31) / 32;
 
-  // the pages of a piece's 16s (of TB pieces) in the first lanes
-  auto pages_at = [&](int piece) { return pages_of(seq, a.cache, 2 * piece + (lane & (2 * TB - 1)), seq.length); };
-  auto load_keys = [&](int piece, int pages, ca_u32x4 (&k)[TB][STEPS]) {   // (where there is no page: from the first, of no account)
+  // the 16s of TB pieces are found by the first lanes
+  auto ask_piece = [&](int piece) { return ask(seq, a.cache, 2 * piece + (lane & (2 * TB - 1)), seq.length); };
+  constexpr int ROW = HD * (int)sizeof(T);
+  const char *keys = (const char *)a.cache.plane<T>(0, 0, kvh);
+  auto load_keys = [&](const Found &f, ca_u32x4 (&k)[TB][STEPS]) {
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      int index, in;
-      place_of(a.cache, 2 * (piece + j) + (col >> 4), index, in);
-      const ca_u32x4 *at = (const ca_u32x4 *)(a.cache.plane<T>(max(__shfl(pages, 2 * j + (col >> 4), 64), 0), 0, kvh) + (in + (col & 15)) * HD);
+      const char *lower = at_lane(keys, f, 2 * j), *upper = at_lane(keys, f, 2 * j + 1);
+      const char *at = (col >> 4 ? upper : lower) + ((col & 15) * ROW + 16 * half);
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) k[j][i] = at[2 * i + half];
+      for (int i = 0; i < STEPS; ++i) k[j][i] = *(const ca_u32x4 *)(at + 32 * i);
     }
   };
   auto load_queries = [&](int b, ca_u32x4 (&q)[STEPS], float &lse) {
@@ -137,9 +138,10 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
   float lse = 0.f;
   if constexpr (MANY) {
     for (; piece < pieces; piece += step) {   // (the same for all of a workgroup)
-      const int pages = pages_at(piece), t0 = piece * 32;
-      const unsigned here = (unsigned)__ballot(pages >= 0);
-      load_keys(piece, pages, k);
+      const Found found = find<ROW>(ask_piece(piece), a.cache, sizeof(T));
+      const int t0 = piece * 32;
+      const unsigned here = (unsigned)__ballot(found.there);
+      load_keys(found, k);
 #pragma unroll
       for (int j = 0; j < TB; ++j) total[j] = 0.f;
       int b = wave;
@@ -171,17 +173,19 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
     }
   } else {
     ca_u32x4 ahead[TB][STEPS];
-    int pages = pages_at(piece), next_pages = pages_at(piece + step), held = -1;   // (-1 past the length)
-    if (piece < pieces) load_keys(piece, pages, ahead);
+    Found found = find<ROW>(ask_piece(piece), a.cache, sizeof(T));
+    Asked asked = ask_piece(piece + step);
+    int held = -1;
+    if (piece < pieces) load_keys(found, ahead);
     for (; piece < pieces; piece += step) {   // (a wave by itself)
-      const bool has_page = ((unsigned)__ballot(pages >= 0) >> (col >> 4)) & 1;
+      const bool has_page = ((unsigned)__ballot(found.there) >> (col >> 4)) & 1;
       const int t0 = piece * 32;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) k[0][i] = ahead[0][i];
-      pages = next_pages;
       if (piece + step < pieces) {
-        next_pages = pages_at(piece + 2 * step);
-        load_keys(piece + step, pages, ahead);
+        found = find<ROW>(asked, a.cache, sizeof(T));
+        asked = ask_piece(piece + 2 * step);
+        load_keys(found, ahead);
       }
       total[0] = 0.f;
       for (int b = 0; b < blocks; ++b) {

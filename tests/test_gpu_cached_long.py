@@ -24,6 +24,7 @@ LONG = [
     ([(500, 500), (400, 450)], 64, 28, 4, 128, "bf16", True),
     ([(900, 901)], 16, 14, 2, 64, "bf16", True),
     ([(700, 2500)], 64, 28, 4, 128, "bf16", True),
+    ([(547, 2040)], 64, 28, 4, 128, "bf16", True),
     ([(2500, 2600), (10, 2000)], 80, 28, 4, 128, "bf16", True),
     ([(1500, 1500)], 32, 28, 2, 64, "bf16", True),
     ([(1500, 4000)], 64, 32, 2, 64, "bf16", False),

@@ -204,21 +204,25 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
   a.factor = std::fabs(scale) * 1.44269504088896340736f;
   a.flip = scale < 0.f ? 0x80000000u : 0u;
   a.decay = decay;
+  a.reciprocal = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   // Many pairs from a block for each of eight waves on (64 rows over 8191 slots, 32 + 2 heads: 16.7 us, a wave by itself 36; 8 rows of it 7.1 and 7.9; but 16 batches
   // of 8 rows over 4095 slots 71 and 24).  Few: workgroups that stay for several pieces, as many as a compute unit has registers for (32 steps of 4095 slots, 28 + 4
   // heads: three 24.6 us, two 28, four 31; fp32 two 64, three 77).
   const bool many = (long long)batch->m * a.group / batch->n >= 256;
   const int heads = batch->n * cache->n_kv_heads, pieces = (batch->max_pages * cache->page_tokens + 31) / 32;
+  bool ok = true;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    auto go = [&](auto kern, int each, int waves, int most) {
-      kern<<<dim3(heads, std::min((pieces + each - 1) / each, most)), 64 * waves, 0, (hipStream_t)hip_stream>>>(a);
+    auto go = [&](auto kern, int each, int waves, int most, size_t lds = 0) {
+      kern<<<dim3(heads, std::min((pieces + each - 1) / each, most)), 64 * waves, lds, (hipStream_t)hip_stream>>>(a);
     };
-    if (many) go(cached_weigh_k<T, HD, true>, Weigh<T, true>::PIECES, Weigh<T, true>::WAVES, 4096);
-    else go(cached_weigh_k<T, HD, false>, Weigh<T, false>::PIECES, Weigh<T, false>::WAVES, std::max(1, (sizeof(T) * HD == 512 ? 2 : 3) * n_cu / heads));
+    if (many) {
+      constexpr size_t lds = Weigh<T, true>::lds(HD);
+      if ((ok = allow_lds<cached_weigh_k<T, HD, true>>(lds))) go(cached_weigh_k<T, HD, true>, Weigh<T, true>::PIECES, Weigh<T, true>::WAVES, 4096, lds);
+    } else go(cached_weigh_k<T, HD, false>, Weigh<T, false>::PIECES, Weigh<T, false>::WAVES, std::max(1, (sizeof(T) * HD == 512 ? 2 : 3) * n_cu / heads));
   });
-  return status();
+  return ok ? status() : SPARK_EHIP;
 }
 
 int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, const float *weights, int32_t keep, int32_t first, int32_t recent,

@@ -2,12 +2,14 @@
 //
 //   out[t] = decay before[t] + sum over rows r that see t, heads h of the group: exp(scale q_rh . k_t - lse_rh)
 //
-// With few rows bound by the keys' way through memory, with many by the exponentials.  A wave takes 32 tokens, whose keys stay in registers, and
-// goes through the (row, head) pairs in blocks of 32: scores S [pair][token] = Q K^T, so that a lane has 16 scores of one token and
-// its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens (in bf16 two pieces of 32, for each block's queries
-// come from L2, 134 MB for 1024 pairs of 8191 slots and two heads with one piece, which took 20 us), deal out the blocks, the next one's queries
-// on their way while one is worked on, and add up their sums in order.  Few: each wave has its own tokens, the next ones' keys are on
-// their way while they are worked on, and a single block's queries stay.  Nothing is added by atomics.
+// With few rows bound by the keys' way through memory, with many by the exponentials and the queries' way out of L2.  A wave takes 32 tokens, whose keys
+// stay in registers, and goes through the (row, head) pairs in blocks of 32: scores S [pair][token] = Q K^T, so that a lane has 16 scores of one
+// token and its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens (in bf16 two pieces of 32, for each block's
+// queries come from L2, 134 MB for 1024 pairs of 8191 slots and two heads with one piece, which took 20 us; each wave loads an eighth of the keys,
+// 14.1 us, where each loading them all took 16.2), deal out the blocks, the next one's queries on their way while one is worked on, and add up
+// their sums in order.  (Without the exponentials 13 of 16, without the queries 13.7, with a quarter of the blocks 9; sixteen waves 14.8.)  Few:
+// each wave has its own tokens, the next ones' keys are on their way while they are worked on, and a single block's queries stay.
+// Nothing is added by atomics.
 #pragma once
 #include "cached_attend.h"
 
@@ -21,6 +23,7 @@ struct WeighArgs {
   float *out;
   long long q_stride;
   int n_q_heads, group, causal;
+  uint32_t reciprocal;         // 2^32 / group rounded up, 0 for one
   float factor, decay;         // factor and flip as in AttendArgs
   uint32_t flip;
 };
@@ -29,6 +32,7 @@ template <typename T, bool MANY> struct Weigh {
   static constexpr int WAVES = MANY ? 8 : 4, WAY = MANY ? 8 : 1;            // of a workgroup; that share tokens
   static constexpr int TB = MANY && sizeof(T) == 2 ? 2 : 1;                  // pieces of 32 tokens that a wave works on at a time
   static constexpr int PIECES = WAVES / WAY * TB;                            // that a workgroup works on at a time
+  static constexpr size_t lds(int hd) { return MANY ? (WAVES + TB) * 32 * hd * sizeof(T) : 0; }   // a block of queries a wave, the keys
 };
 
 template <typename T, int HD, bool MANY>
@@ -39,6 +43,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
   __shared__ float4 s_bias[W::WAVES][8];   // of a wave's block of pairs: -lse log2 e,
   __shared__ int4 s_limit[W::WAVES][8];    // and the last slot seen
   __shared__ float s_sum[W::WAVES][TB][32];
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int s = blockIdx.x / a.cache.n_kv_heads, kvh = blockIdx.x % a.cache.n_kv_heads;
   const Sequence seq = sequence(a.batch, s, a.cache.page_tokens);
@@ -57,12 +62,44 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       for (int i = 0; i < STEPS; ++i) k[j][i] = *(const ca_u32x4 *)(at + 32 * i);
     }
   };
+  // Queries of block b and their lse.  As operands (few pairs), or whole rows in the lanes' order (many: 16.2 us for 1024 pairs
+  // of 8191 slots and two heads, where 32 bytes of each of 32 rows a load took 16.9), which `turn` makes operands of.
+  constexpr int VECS = 2 * STEPS;   // of a query
   auto load_queries = [&](int b, ca_u32x4 (&q)[STEPS], float &lse) {
-    const int p = min(b * 32 + col, pairs - 1), row = p / a.group, h = kvh * a.group + p % a.group;   // (pairs past the last: that one, left out)
-    const ca_u32x4 *at = (const ca_u32x4 *)((const T *)a.q + (seq.row0 + row) * a.q_stride + (long long)h * HD);
+    const int first = b * 32 / a.group, past = b * 32 - first * a.group, most = pairs - 1 - b * 32;   // (pairs past the last: that one, left out)
+    auto place = [&](int pair, int &h) {   // its row; (numbers below 2^13 by one of at most 2^12: exact)
+      const int n = past + min(pair, most), r = a.reciprocal ? (int)__umulhi((uint32_t)n, a.reciprocal) : n;
+      h = kvh * a.group + n - r * a.group;
+      return seq.row0 + first + r;
+    };
+    int h;
+    const long long row = place(col, h);
+    lse = a.lse[row * a.n_q_heads + h];
+    if constexpr (MANY) {
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) q[i] = at[2 * i + half];
-    lse = a.lse[(long long)(seq.row0 + row) * a.n_q_heads + h];
+      for (int i = 0; i < STEPS; ++i) {
+        const long long r = place(i * (64 / VECS) + lane / VECS, h);
+        q[i] = ((const ca_u32x4 *)((const T *)a.q + r * a.q_stride + (long long)h * HD))[lane % VECS];
+      }
+    } else {
+      const ca_u32x4 *at = (const ca_u32x4 *)((const T *)a.q + row * a.q_stride + (long long)h * HD);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) q[i] = at[2 * i + half];
+    }
+  };
+  auto turn = [&](const ca_u32x4 (&in)[STEPS], ca_u32x4 (&q)[STEPS]) {   // through LDS, a row's pieces turned by its number
+    ca_u32x4 *block = (ca_u32x4 *)s_dyn + wave * 32 * VECS;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int row = i * (64 / VECS) + lane / VECS;
+      block[row * VECS + ((lane ^ row) & (VECS - 1))] = in[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) q[i] = block[col * VECS + ((2 * i + half) ^ (col & (VECS - 1)))];
   };
   bool some_out = false;   // of the block in LDS: a pair that gives nothing
   auto place_block = [&](int b, float lse) {
@@ -138,20 +175,38 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
   float lse = 0.f;
   if constexpr (MANY) {
     for (; piece < pieces; piece += step) {   // (the same for all of a workgroup)
-      const Found found = find<ROW>(ask_piece(piece), a.cache, sizeof(T));
+      const Asked asked = ask_piece(piece);
       const int t0 = piece * 32;
-      const unsigned here = (unsigned)__ballot(found.there);
-      load_keys(found, k);
-#pragma unroll
-      for (int j = 0; j < TB; ++j) total[j] = 0.f;
       int b = wave;
       while (b < blocks && t0 > last_of(b)) b += W::WAY;
       ca_u32x4 ahead[STEPS];
       float next_lse = 0.f;
       if (b < blocks) load_queries(b, ahead, next_lse);
-      for (; b < blocks; b += W::WAY) {
+      const Found found = find<ROW>(asked, a.cache, sizeof(T));
+      const unsigned here = (unsigned)__ballot(found.there);
+      // each wave loads its share of the keys; through LDS all have them all
+      constexpr int TOKENS = 64 / VECS;
+      ca_u32x4 share[32 * TB / (W::WAVES * TOKENS)];
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) q[i] = ahead[i];
+      for (int j = 0; j < 32 * TB / (W::WAVES * TOKENS); ++j) {
+        const int token = (j * W::WAVES + wave) * TOKENS;
+        share[j] = ((const ca_u32x4 *)(at_lane(keys, found, token / 16) + (token % 16 + lane / VECS) * ROW))[lane % VECS];
+      }
+      ca_u32x4 *block = (ca_u32x4 *)s_dyn + W::WAVES * 32 * VECS;
+#pragma unroll
+      for (int j = 0; j < 32 * TB / (W::WAVES * TOKENS); ++j) {
+        const int token = (j * W::WAVES + wave) * TOKENS + lane / VECS;
+        block[token * VECS + ((lane ^ token) & (VECS - 1))] = share[j];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < TB; ++j) {
+        total[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) k[j][i] = block[(32 * j + col) * VECS + ((2 * i + half) ^ (col & (VECS - 1)))];
+      }
+      for (; b < blocks; b += W::WAY) {
+        turn(ahead, q);
         lse = next_lse;
         if (b + W::WAY < blocks) load_queries(b + W::WAY, ahead, next_lse);
         place_block(b, lse);

@@ -205,11 +205,14 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
   a.flip = scale < 0.f ? 0x80000000u : 0u;
   a.decay = decay;
   a.reciprocal = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
-  // Many pairs from a block for each of eight waves on (64 rows over 8191 slots, 32 + 2 heads: 16.7 us, a wave by itself 36; 8 rows of it 7.1 and 7.9; but 16 batches
-  // of 8 rows over 4095 slots 71 and 24).  Few: workgroups that stay for several pieces, as many as a compute unit has registers for (32 steps of 4095 slots, 28 + 4
-  // heads: three 24.6 us, two 28, four 31; fp32 two 64, three 77).
-  const bool many = (long long)batch->m * a.group / batch->n >= 256;
+  // Many pairs from a block for each of eight waves on (32 + 2 heads, bf16, 64 rows over 8191 slots: 13.9 us, a wave by itself 33), and in bf16 from two
+  // blocks on where a round of workgroups does it (8 rows 5.0 and 7.4; 2 rows 4.6 and 4.5; of two sequences, so in two rounds, 8.5 and 7.6; of 16 over 4095
+  // slots 31 and 22; fp32 8 rows 19 and 18, of two sequences 34 and 19).  Few: workgroups that stay for several pieces, as many as a compute unit
+  // has registers for (32 steps of 4095 slots, 28 + 4 heads: three 24.6 us, two 28, four 31; fp32 two 64, three 77).
   const int heads = batch->n * cache->n_kv_heads, pieces = (batch->max_pages * cache->page_tokens + 31) / 32;
+  const long long pairs = (long long)batch->m * a.group / batch->n;   // of a sequence and head, on average
+  const bool round = cache->dtype == SPARK_DTYPE_BF16 && (long long)heads * ((pieces + 1) / 2) <= n_cu;
+  const bool many = pairs >= 256 || (round && pairs > 32);
   bool ok = true;
   by_cache(cache->dtype, cache->head_dim, [&](auto t, auto hd) {
     using T = decltype(t);

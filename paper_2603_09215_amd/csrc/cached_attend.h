@@ -694,7 +694,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
 
 // ------------------------------------------------------------------ the parts together
 
-constexpr int JOIN_AHEAD = 4;   // parts on their way (a row of 28 heads in 32 parts of a context of 8192, both launches: one 12.7 us, four 10.9, eight 10.5, sixteen 10.3; 511 rows in 4 parts: 39.8, 40.1, 40.5, 44.3)
+constexpr int JOIN_AHEAD = 4;   // parts on their way (one step of 28 heads over 1537 slots in 13 parts, both launches: one 12.7 us, four 10.9, eight 10.5, sixteen 10.3; 511 rows in 4 parts: 39.8, 40.1, 40.5, 44.3)
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {

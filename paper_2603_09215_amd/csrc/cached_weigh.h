@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
     }
   };
   // Queries of block b and their lse.  As operands (few pairs), or whole rows in the lanes' order (many: 16.2 us for 1024 pairs
-  // of 8191 slots and two heads, where 32 bytes of each of 32 rows a load took 16.9), which `turn` makes operands of.
+  // of 8191 slots and two heads, where 32 bytes of each of 32 rows a load took 16.9) that go to LDS.
   constexpr int VECS = 2 * STEPS;   // of a query
   auto load_queries = [&](int b, ca_u32x4 (&q)[STEPS], float &lse) {
     const int first = b * 32 / a.group, past = b * 32 - first * a.group, most = pairs - 1 - b * 32;   // (pairs past the last: that one, left out)
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       for (int i = 0; i < STEPS; ++i) q[i] = at[2 * i + half];
     }
   };
-  auto turn = [&](const ca_u32x4 (&in)[STEPS], ca_u32x4 (&q)[STEPS]) {   // through LDS, a row's pieces turned by its number
+  auto turn = [&](const ca_u32x4 (&in)[STEPS]) {   // to LDS, a row's pieces turned by its number
     ca_u32x4 *block = (ca_u32x4 *)s_dyn + wave * 32 * VECS;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -96,11 +96,8 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       const int row = i * (64 / VECS) + lane / VECS;
       block[row * VECS + ((lane ^ row) & (VECS - 1))] = in[i];
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) q[i] = block[col * VECS + ((2 * i + half) ^ (col & (VECS - 1)))];
   };
+  auto turned = [&](int row, int i) { return ((const ca_u32x4 *)s_dyn)[row * VECS + ((2 * i + half) ^ (col & (VECS - 1)))]; };   // (row mod 32 is col)
   bool some_out = false;   // of the block in LDS: a pair that gives nothing
   auto place_block = [&](int b, float lse) {
     const bool none = b * 32 + col >= pairs || lse == -INFINITY;
@@ -125,7 +122,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       for (int r = 0; r < 16; ++r) sc[j][r] = 0.f;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-      const ca_u32x4 qs = ca_signed<T>(q[i], a.flip);
+      const ca_u32x4 qs = ca_signed<T>(MANY ? turned(wave * 32 + col, i) : q[i], a.flip);
 #pragma unroll
       for (int j = 0; j < TB; ++j) {
         if constexpr (BF) {
@@ -203,10 +200,10 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       for (int j = 0; j < TB; ++j) {
         total[j] = 0.f;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) k[j][i] = block[(32 * j + col) * VECS + ((2 * i + half) ^ (col & (VECS - 1)))];
+        for (int i = 0; i < STEPS; ++i) k[j][i] = turned((W::WAVES + j) * 32 + col, i);
       }
       for (; b < blocks; b += W::WAY) {
-        turn(ahead, q);
+        turn(ahead);
         lse = next_lse;
         if (b + W::WAY < blocks) load_queries(b + W::WAY, ahead, next_lse);
         place_block(b, lse);

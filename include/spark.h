@@ -451,7 +451,7 @@ typedef struct spark_cache {
 typedef struct spark_cache_batch {
   uint32_t size;          /* sizeof(spark_cache_batch) */
   int32_t m;              /* rows of the row operands, up to 2^22 */
-  int32_t n;              /* sequences, up to 2^16 */
+  int32_t n;              /* sequences, up to 2^16, and times the cache's n_kv_heads up to 2^20 */
   int32_t max_pages;      /* pages a sequence has at most; slots (times page_tokens) up to 2^23 */
   const int32_t *starts;  /* [n + 1] */
   const int32_t *lengths; /* [n] */
@@ -492,7 +492,7 @@ int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batc
 /* out [m][n_q_heads][head_dim] = sum over the slots t that a row sees of p_t v_t, p = softmax(scale q . k_t), query head h
  * with kv head h / (n_q_heads / n_kv_heads); q and out of the cache's type, 16-byte aligned, strides multiples of 8 elements.
  * lse (or NULL) fp32 [m][n_q_heads]: log sum exp(scale q . k_t).  A row that sees nothing gets zeros, and minus infinity
- * in lse.  scale is finite and not 0.  Scores, maxima and sums are fp32; with a bf16 cache the probabilities go into their products with the
+ * in lse.  scale is not 0 and at most 2^127.  Scores, maxima and sums are fp32; with a bf16 cache the probabilities go into their products with the
  * values rounded to bf16, relative to the largest one so far. */
 int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q,
                        int64_t q_stride, float scale, int32_t causal, void *out, int64_t out_stride, float *lse,

@@ -185,8 +185,8 @@ def cached_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Page
 def _scale(scale, hd: int) -> float:
     if scale is None:
         return hd ** -0.5
-    if not math.isfinite(scale) or C.c_float(scale).value in (0.0, math.inf, -math.inf):
-        _refuse("scale must be finite and not 0")
+    if not abs(scale) <= 2.0 ** 127 or C.c_float(scale).value == 0.0:
+        _refuse("a scale up to 2^127, and not 0, is wanted")
     return scale
 
 
@@ -284,7 +284,9 @@ def cached_evict(cache: PagedCache, batch: CachedRows, weights: torch.Tensor, ke
         n, out_pages = _table(table_out, "table_out", 2).shape
         if n != batch.n or out_pages * cache.page_tokens < keep or out_pages > 1 << 24:
             _refuse(f"table_out is {n} x {out_pages}: pages for {keep} slots of {batch.n} sequences are wanted")
-        if batch.n and table_out.data_ptr() == batch.table.data_ptr():
+        if n and table_out.data_ptr() == batch.table.data_ptr():
+            if n > 1 and out_pages != batch.max_pages:
+                _refuse("table_out is a part of the batch's table")
             table_out = None
     out_at = at if weights_out is None else _weights(weights_out, "weights_out", cache, batch)
     kept = torch.empty(batch.n, cache.kv_heads, keep, dtype=torch.int32, device=weights.device)

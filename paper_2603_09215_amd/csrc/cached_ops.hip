@@ -33,6 +33,7 @@ bool heads_ok(const spark_cache *c, const spark_cache_batch *b, int32_t n_q_head
 bool batch_ok(const spark_cache *c, const spark_cache_batch *b) {
   return sizes_ok(c, b) && aligned(c->pool, 16) && aligned(b->starts, 4) && aligned(b->lengths, 4) && aligned(b->table, 4);
 }
+bool scale_ok(float scale) { return scale != 0.f && std::fabs(scale) <= 0x1p127f; }   // (times log2 e it is a number still)
 // rows of `heads` vectors
 bool rows_ok(const void *p, size_t align, int64_t stride, int64_t heads, const spark_cache *c) {
   return aligned(p, align) && within(stride, heads * c->head_dim, (int64_t)1 << 40);
@@ -148,7 +149,7 @@ int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batc
 int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
                        int32_t causal, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || !rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 ||
-      !rows_ok(out, 16, out_stride, n_q_heads, cache) || out_stride % 8 || ((uintptr_t)lse & 3) || !std::isfinite(scale) || scale == 0.f)
+      !rows_ok(out, 16, out_stride, n_q_heads, cache) || out_stride % 8 || ((uintptr_t)lse & 3) || !scale_ok(scale))
     return SPARK_EINVAL;
   if (batch->m == 0 || batch->n == 0) return SPARK_OK;
   const int n_cu = compute_units();
@@ -192,7 +193,7 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
 int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q, int64_t q_stride, float scale,
                       int32_t causal, const float *lse, const float *before, float decay, float *out, void *hip_stream) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, batch, n_q_heads) || (batch->m > 0 && (!rows_ok(q, 16, q_stride, n_q_heads, cache) || q_stride % 8 || !aligned(lse, 4))) ||
-      ((uintptr_t)before & 3) || !aligned(out, 4) || !std::isfinite(scale) || scale == 0.f || !std::isfinite(decay))
+      ((uintptr_t)before & 3) || !aligned(out, 4) || !scale_ok(scale) || !std::isfinite(decay))
     return SPARK_EINVAL;
   if (batch->n == 0) return SPARK_OK;
   const int n_cu = compute_units();
@@ -222,7 +223,7 @@ int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, 
     };
     if (many) {
       constexpr size_t lds = Weigh<T, true>::lds(HD);
-      if ((ok = allow_lds<cached_weigh_k<T, HD, true>>(lds))) go(cached_weigh_k<T, HD, true>, Weigh<T, true>::PIECES, Weigh<T, true>::WAVES, 4096, lds);
+      if ((ok = allow_lds<cached_weigh_k<T, HD, true>>(lds))) go(cached_weigh_k<T, HD, true>, Weigh<T, true>::PIECES, Weigh<T, true>::WAVES, std::max(1, (1 << 16) / heads), lds);
     } else go(cached_weigh_k<T, HD, false>, Weigh<T, false>::PIECES, Weigh<T, false>::WAVES, std::max(1, (sizeof(T) * HD == 512 ? 2 : 3) * n_cu / heads));
   });
   return ok ? status() : SPARK_EHIP;
@@ -235,7 +236,8 @@ int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, 
     return SPARK_EINVAL;
   const int64_t slots = (int64_t)batch->max_pages * cache->page_tokens;
   if (first < 0 || recent < 0 || !within(keep, 1, slots) || (int64_t)first + recent > keep ||
-      (table_out && (!within(out_pages, 1, 1 << 24) || (int64_t)out_pages * cache->page_tokens < keep)))
+      (table_out && (!within(out_pages, 1, 1 << 24) || (int64_t)out_pages * cache->page_tokens < keep)) ||
+      (table_out && table_out == batch->table && out_pages != batch->max_pages && batch->n > 1))
     return SPARK_EINVAL;
   if (batch->n == 0) return SPARK_OK;
   EvictArgs a{};
@@ -251,10 +253,10 @@ int spark_cache_evict(const spark_cache *cache, const spark_cache_batch *batch, 
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value, PIECES = HD * sizeof(T) / 16;
     if (a.table_out == batch->table) {
-      cached_move_k<T, HD, 8><<<heads * 2 * (PIECES / 8), 1024, 0, stream>>>(a);
+      cached_move_k<T, HD, 8><<<heads * 2 * (PIECES / 8), heads > 1 << 18 ? 256 : 1024, 0, stream>>>(a);   // (a launch takes less than 2^32 threads)
     } else {
       const int rounds = (keep * PIECES + 256 * MOVE_BATCH - 1) / (256 * MOVE_BATCH);
-      cached_move_k<T, HD, PIECES><<<dim3(heads * 2, std::min(rounds, 256)), 256, 0, stream>>>(a);
+      cached_move_k<T, HD, PIECES><<<dim3(heads * 2, std::min(rounds, std::max(1, std::min(256, (1 << 20) / heads)))), 256, 0, stream>>>(a);
     }
   });
   return status();

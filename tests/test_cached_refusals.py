@@ -120,4 +120,13 @@ def test_evict_arguments(lib):
                dict(lengths=P + 2), dict(keep=0), dict(keep=-1), dict(keep=65), dict(first=-1), dict(recent=-1), dict(first=18), dict(first=1 << 30, recent=1 << 30),
                dict(table=P, pages=1), dict(table=P, pages=0), dict(table=P, pages=-5), dict(table=P + 2, pages=4), dict(table=P, pages=(1 << 24) + 1)):
         assert evict(lib, **kw) == EINVAL, kw
+    assert evict(lib, table=P, pages=3) == EINVAL   # the batch's own table in other rows
     assert evict(lib, b=batch(n=0)) == 0
+
+
+def test_scales(lib):
+    for call in (attend, weigh):
+        for scale in (2.0 ** 127 * 1.01, -2.0 ** 127 * 1.01, 0.0, -0.0, 1e-46, float("inf"), float("nan")):
+            assert call(lib, scale=scale) == EINVAL, (call, scale)
+        for scale in (2.0 ** 127, -2.0 ** 127, 1e-45):
+            assert call(lib, scale=scale, b=batch(n=0)) == 0

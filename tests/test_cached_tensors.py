@@ -103,6 +103,10 @@ def test_evict(it):
                dict(weights=on(2, 1, 32, dtype=F32)), dict(weights_out=on(2, 2, 31, dtype=F32)), dict(table_out=on(2, 1, dtype=torch.int64)), dict(table_out=on(1, 1, dtype=I32)),
                dict(keep=17, table_out=on(2, 1, dtype=I32))):
         refused(lambda: cached.cached_evict(**{**dict(cache=c, batch=b, weights=w, keep=16), **kw}))
+    refused(lambda: cached.cached_evict(c, b, w, 16, table_out=b.table.view(-1)[:2].view(2, 1)), "a part of")
+    for scale in (0.0, 1e-50, 3e38, math.inf, math.nan):
+        refused(lambda: cached._scale(scale, 64), "scale")
+    assert cached._scale(None, 64) == 0.125 and cached._scale(-2.0 ** 127, 64) == -2.0 ** 127
 
 
 def test_sizes_past_the_calls_limits():

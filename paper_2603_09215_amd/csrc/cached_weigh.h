@@ -6,8 +6,8 @@
 // stay in registers, and goes through the (row, head) pairs in blocks of 32: scores S [pair][token] = Q K^T, so that a lane has 16 scores of one
 // token and its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens (in bf16 two pieces of 32, for each block's
 // queries come from L2, 134 MB for 1024 pairs of 8191 slots and two heads with one piece, which took 20 us; each wave loads an eighth of the keys,
-// 14.1 us, where each loading them all took 16.2), deal out the blocks, the next one's queries on their way while one is worked on, and add up
-// their sums in order.  (Without the exponentials 13 of 16, without the queries 13.7, with a quarter of the blocks 9; sixteen waves 14.8.)  Few:
+// 14.1 us, where each loading them all took 16.2; and operands of queries read from LDS as they are used 12.3), deal out the blocks, the next one's queries on their way while one is worked on, and add up
+// their sums in order.  (Of 16.2: without the exponentials 13, without the queries 13.7, with a quarter of the blocks 9.  Sixteen waves 14.8 against 14.1.)  Few:
 // each wave has its own tokens, the next ones' keys are on their way while they are worked on, and a single block's queries stay.
 // Nothing is added by atomics.
 #pragma once

@@ -165,6 +165,7 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
   a.factor = std::fabs(scale) * 1.44269504088896340736f;
   a.flip = scale < 0.f ? 0x80000000u : 0u;
   a.splits = plan.splits;
+  a.by_row = attend_tiles_by_row(plan.pairs, a.group, batch->m, batch->n);
   a.part = (float *)workspace;
   a.part_ml = (float2 *)(a.part + (size_t)plan.splits * batch->m * n_q_heads * cache->head_dim);
   hipStream_t stream = (hipStream_t)hip_stream;

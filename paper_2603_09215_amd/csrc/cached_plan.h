@@ -12,6 +12,11 @@ struct AttendPlan {
   long long tiles;
 };
 
+// Tiles are numbered by rows, or by pairs with one more for each sequence: whichever takes fewer numbers.  Neither is fewer than there are.
+inline long long attend_numbers_by_row(int pairs, int group, int m) { return (long long)m * ((group + pairs - 1) / pairs); }
+inline long long attend_numbers_by_pair(int pairs, int group, int m, int n) { return (long long)m * group / pairs + n; }
+inline bool attend_tiles_by_row(int pairs, int group, int m, int n) { return attend_numbers_by_row(pairs, group, m) <= attend_numbers_by_pair(pairs, group, m, n); }
+
 // A kernel's step over `tokens` tokens: us with one workgroup to a compute unit, and with as many as there is room for
 struct AttendKind { int pairs, tokens, room; float us_one, us_full; };
 // [head_dim 128][kernel]: streams of pieces (four waves' pieces a step), tiles of four waves and of eight (which heads of 64 gain nothing by: 95 us and 83 for
@@ -31,8 +36,7 @@ inline AttendPlan attend_plan(bool fp32, int head_dim, int n_kv_heads, int group
   for (int i = 0; i < (fp32 ? 1 : 3); ++i) {
     const AttendKind &k = kinds[i];
     if (k.pairs == 0) continue;
-    // (every sequence adds at most one tile that is not full)
-    const long long tiles = std::min((long long)m * ((group + k.pairs - 1) / k.pairs), (long long)m * group / k.pairs + n);
+    const long long tiles = std::min(attend_numbers_by_row(k.pairs, group, m), attend_numbers_by_pair(k.pairs, group, m, n));
     const float all = (float)(tiles * n_kv_heads), steps = (float)((slots + k.tokens - 1) / k.tokens);
     const float part_us = 0.25f + (float)m * group * n_kv_heads * head_dim * 8.0f / 4e6f;
     for (int s = 1; s <= MOST_SPLITS && (s == 1 || s <= steps); ++s) {

@@ -696,36 +696,41 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
 
 // ------------------------------------------------------------------ the parts together
 
-constexpr int JOIN_AHEAD = 4;   // parts on their way (one step of 28 heads over 1537 slots in 13 parts, both launches: one 12.7 us, four 10.9, eight 10.5, sixteen 10.3; 511 rows in 4 parts: 39.8, 40.1, 40.5, 44.3)
+constexpr int JOIN_AHEAD = 4;   // parts on their way (511 rows of 28 heads in 4 parts: one 39.8 us, two launches, four 40.1, eight 40.5, sixteen 44.3)
 
-template <typename T, int HD>
+// GROUPS of lanes to a vector, each with every GROUPS-th part, whose sums are added in their order.
+template <typename T, int HD, int GROUPS>
 __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
   constexpr int LANES = HD / 4;
-  const long long i = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (i >= (long long)a.batch.m * a.n_q_heads) return;
+  static_assert(GROUPS == 1 || GROUPS * LANES == 256, "several groups are a workgroup");
+  const long long i = (long long)blockIdx.x * (256 / LANES / GROUPS) + threadIdx.x / (LANES * GROUPS);
+  if (i >= (long long)a.batch.m * a.n_q_heads) return;   // (several groups: of all of a workgroup)
   const int r = (int)(i / a.n_q_heads), e0 = threadIdx.x % LANES * 4;
-  const int lane = threadIdx.x % LANES;
-  bool ours = false;   // somebody's row
-  for (int s = lane; s < a.batch.n; s += LANES) ours |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1];
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES % GROUPS;
   const long long step = (long long)a.batch.m * a.n_q_heads;
-  // the parts' maxima and sums, one or a few a lane
-  constexpr int EACH = MOST_SPLITS / LANES;
-  float f[EACH], l = 0.f, m = -INFINITY;
-  float2 ml[EACH];
-  // the first parts are on their way while these are looked at
+  // the first parts are on their way while all maxima and sums are looked at
   const float *part = a.part + i * HD + e0;
   ca_f32x4 v[JOIN_AHEAD];
+  float2 ml[JOIN_AHEAD];
   auto fetch = [&](int s0) {
 #pragma unroll
-    for (int k = 0; k < JOIN_AHEAD; ++k) v[k] = *(const ca_f32x4 *)(part + min(s0 + k, a.splits - 1) * step * HD);
+    for (int k = 0; k < JOIN_AHEAD; ++k) {
+      const int s = min(s0 + k * GROUPS, a.splits - 1);
+      v[k] = *(const ca_f32x4 *)(part + s * step * HD);
+      ml[k] = a.part_ml[s * step + i];
+    }
   };
-  fetch(0);
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    const int s = j * LANES + lane;
-    ml[j] = s < a.splits ? a.part_ml[s * step + i] : make_float2(-INFINITY, 0.f);
-    m = fmaxf(m, ml[j].x);
+  fetch(group);
+  bool ours = false;   // somebody's row
+  for (int s = lane; s < a.batch.n; s += LANES) ours |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1];
+  float l = 0.f, m = -INFINITY;
+  for (int s = lane; s < a.splits; s += LANES) {
+    const float2 x = a.part_ml[s * step + i];
+    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
+    l = (l == 0.f ? 0.f : l * ca_exp2(m - base)) + (x.y == 0.f ? 0.f : x.y * ca_exp2(x.x - base));
+    m = top;
   }
+  const float mine = m;
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor(m, o, LANES));
@@ -733,23 +738,27 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
   }
   if (!ours) return;
   const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    f[j] = ml[j].y == 0.f ? -1.f : ca_exp2(ml[j].x - base);   // (-1: its sums were not written)
-    l += ml[j].y == 0.f ? 0.f : ml[j].y * f[j];
-  }
+  l = l == 0.f ? 0.f : l * ca_exp2(mine - base);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, LANES);
   ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.splits; s0 += JOIN_AHEAD) {
-    if (s0 > 0) fetch(s0);
+  for (int s0 = group; s0 < a.splits; s0 += JOIN_AHEAD * GROUPS) {
+    if (s0 > group) fetch(s0);
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k) {
-      const int s = s0 + k;
-      const float g = s >= a.splits ? -1.f : __shfl(EACH == 1 || s < LANES ? f[0] : EACH == 2 || s < 2 * LANES ? f[1] : s < 3 * LANES ? f[EACH - 2] : f[EACH - 1], s % LANES, LANES);
+      const bool none = s0 + k * GROUPS >= a.splits || ml[k].y == 0.f;   // (its sums were not written)
+      const float g = none ? 0.f : ca_exp2(ml[k].x - base);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += g < 0.f ? 0.f : g == 0.f && !(fabsf(v[k][e]) < INFINITY) ? v[k][e] : v[k][e] * g;   // (an infinity stays one)
+      for (int e = 0; e < 4; ++e) y[e] += none ? 0.f : g == 0.f && !(fabsf(v[k][e]) < INFINITY) ? v[k][e] : v[k][e] * g;   // (an infinity stays one)
     }
+  }
+  if constexpr (GROUPS > 1) {
+    __shared__ ca_f32x4 s_y[GROUPS][LANES];
+    s_y[group][lane] = y;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int j = 1; j < GROUPS; ++j) y += s_y[j][lane];
   }
   write_result<T, HD>(a, r, (int)(i % a.n_q_heads), e0, y, m, l);
 }

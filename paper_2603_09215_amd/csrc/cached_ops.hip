@@ -185,7 +185,8 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
     if (plan.pairs == 16) go(cached_stream_k<T, HD>, 256, Stream<T, HD>::LDS, true);
     if (ok && plan.splits > 1) {
       const long long vectors = (long long)batch->m * n_q_heads, each = 256 / (HD / 4);
-      cached_join_k<T, HD><<<(unsigned)((vectors + each - 1) / each), 256, 0, stream>>>(a);
+      if (join_by_workgroups(vectors)) cached_join_k<T, HD, 256 / (HD / 4)><<<(unsigned)vectors, 256, 0, stream>>>(a);
+      else cached_join_k<T, HD, 1><<<(unsigned)((vectors + each - 1) / each), 256, 0, stream>>>(a);
     }
   });
   return ok ? status() : SPARK_EHIP;

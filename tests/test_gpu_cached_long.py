@@ -33,6 +33,11 @@ LONG = [
     ([(40, 60)], 16, 28, 4, 128, "fp32", True),
     ([(200, 600), (180, 300)], 48, 14, 2, 64, "fp32", True),
     ([(1, 4000), (30, 2000)], 16, 4, 2, 64, "fp32", False),
+    ([(30, 60)], 16, 4, 2, 64, "fp32", True),
+    ([(8190, 8190)], 64, 7, 1, 128, "bf16", True),
+    ([(800, 20000)], 64, 28, 4, 128, "bf16", True),
+    ([(1, 30000)], 64, 8, 1, 128, "bf16", True),
+    ([(2, 9001)], 64, 8, 2, 64, "fp32", True),
 ]
 
 

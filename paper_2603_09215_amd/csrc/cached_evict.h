@@ -15,7 +15,6 @@ struct EvictArgs {
 };
 
 typedef __attribute__((ext_vector_type(4))) uint32_t move_u32x4;
-constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
 
 // larger weight, larger key; -0 as +0; every NaN above all numbers
 __device__ __forceinline__ uint32_t weight_key(float w) { return float_order_key(w + 0.f); }
@@ -23,9 +22,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return float_order_key
 // What is kept, one workgroup a sequence and head, up to eight slots in a row to a thread.  The `need` heaviest of the slots between the first
 // and the recent ones: the key of the last of them by digits of 11, 11 and 10 bits from the top, counted in LDS, each over the slots that share
 // the digits found so far; then the slots above that key and the first of those that have it are written in slot
-// order.  Places are counts of what stays before them, so nothing depends on the order of threads.  Up to 8192 slots are read once.
+// order.  Places are counts of what stays before them, so nothing depends on the order of threads.  Up to eight slots a thread are read once.
+// Bound by its barriers and, with many slots, by one compute unit's instructions a head: four heads of 4097 slots take 10 us, 64 of up to 8191 15, four of 60000 142.
 constexpr int EVICT_EACH = 8, EVICT_BINS = 2048;
-static_assert(EVICT_BINS == 2 * EVICT_THREADS && EVICT_WAVES == 16, "two digits a thread; waves fit a row of lanes");
 
 template <int CTRL, int ROWS> __device__ __forceinline__ unsigned add_from(unsigned v) {   // a lane's value from another one's, of some rows of 16
   return v + (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
@@ -40,13 +39,14 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v) {
   return add_from<0x143, 0xc>(v);   // of 32 to the upper 32
 }
 // sum over the threads before this one in the workgroup, and over all of them
-__device__ __forceinline__ unsigned evict_scan(unsigned v, unsigned *s_wave, unsigned &total) {
+template <int WAVES> __device__ __forceinline__ unsigned evict_scan(unsigned v, unsigned *s_wave, unsigned &total) {
+  static_assert(WAVES <= 16, "waves fit a row of lanes");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned incl = wave_scan(v);
   __syncthreads();
   if (lane == 63) s_wave[wave] = incl;
   __syncthreads();
-  unsigned w = s_wave[lane & 15];
+  unsigned w = (lane & 15) < WAVES ? s_wave[lane & 15] : 0u;
   w = add_from<0x111, 0xf>(w);
   w = add_from<0x112, 0xf>(w);
   w = add_from<0x114, 0xf>(w);
@@ -55,8 +55,10 @@ __device__ __forceinline__ unsigned evict_scan(unsigned v, unsigned *s_wave, uns
   return incl - v + (wave ? (unsigned)__builtin_amdgcn_readlane((int)w, wave - 1) : 0u);
 }
 
-__global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
-  __shared__ unsigned s_count[EVICT_BINS], s_wave[EVICT_WAVES], s_digit, s_before;
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) cached_choose_k(EvictArgs a) {
+  constexpr int WAVES = THREADS / 64, DIGITS = EVICT_BINS / THREADS;   // DIGITS: a thread's
+  __shared__ unsigned s_count[EVICT_BINS], s_wave[WAVES], s_digit, s_before;
   const int s = blockIdx.x / a.cache.n_kv_heads, tid = threadIdx.x;
   const int slots = a.batch.max_pages * a.cache.page_tokens, length = cut(a.batch.lengths[s], 0, slots);
   const float *w = a.weights + (long long)blockIdx.x * slots;
@@ -68,7 +70,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
   const int lo = all ? 0 : a.first, hi = all ? 0 : length - a.recent;   // what is chosen from
   unsigned need = all ? 0u : (unsigned)(a.keep - a.first - a.recent), prefix = 0;
   const bool some = need > 0;
-  const int each = cut((length + EVICT_THREADS - 1) / EVICT_THREADS, 1, EVICT_EACH), chunk = each * EVICT_THREADS;
+  const int each = cut((length + THREADS - 1) / THREADS, 1, EVICT_EACH), chunk = each * THREADS;
   float x[EVICT_EACH];
   uint32_t key[EVICT_EACH];   // 0, which no weight has, for what is not chosen from: in the lowest place, never reached
   int held = -1;              // which chunk they are of
@@ -92,8 +94,8 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
     for (int digit = 0; digit < 3; ++digit) {
       const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
       const unsigned mask = digit == 2 ? 1023u : 2047u, span = digit == 0 ? ~0u : digit == 1 ? (1u << 21) - 1 : (1u << 10) - 1;   // keys with this prefix
-      s_count[2 * tid] = 0;
-      s_count[2 * tid + 1] = 0;
+#pragma unroll
+      for (int j = 0; j < DIGITS; ++j) s_count[j * THREADS + tid] = 0;
       __syncthreads();
       for (int c0 = 0; c0 < length; c0 += chunk) {
         fetch(c0);
@@ -109,12 +111,19 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
         if (zeros && (ZERO ^ prefix) <= span && (tid & 63) == 0) atomicAdd(&s_count[(ZERO >> shift) & mask], zeros);
       }
       __syncthreads();
-      // from the highest digit down, two a thread
-      const unsigned d0 = EVICT_BINS - 1 - 2 * tid, n0 = s_count[d0], n1 = s_count[d0 - 1];
-      unsigned total;
-      const unsigned before = evict_scan(n0 + n1, s_wave, total);
-      if (before < need && need <= before + n0) { s_digit = d0; s_before = before; }
-      else if (before + n0 < need && need <= before + n0 + n1) { s_digit = d0 - 1; s_before = before + n0; }
+      // from the highest digit down, DIGITS a thread
+      unsigned n[DIGITS], sum = 0, total;
+#pragma unroll
+      for (int j = 0; j < DIGITS; ++j) sum += n[j] = s_count[EVICT_BINS - 1 - DIGITS * tid - j];
+      unsigned before = evict_scan<WAVES>(sum, s_wave, total);
+#pragma unroll
+      for (int j = 0; j < DIGITS; ++j) {
+        if (before < need && need <= before + n[j]) {
+          s_digit = EVICT_BINS - 1 - DIGITS * tid - j;
+          s_before = before;
+        }
+        before += n[j];
+      }
       __syncthreads();
       prefix |= s_digit << shift;
       need -= s_before;   // of those with this key so far
@@ -133,7 +142,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
       if (there && some && middle && key[e] == prefix) tie |= 1u << e;
     }
     unsigned total;
-    const unsigned before = evict_scan(__popc(above) | __popc(tie) << 16, s_wave, total);   // (8192 at most of each)
+    const unsigned before = evict_scan<WAVES>(__popc(above) | __popc(tie) << 16, s_wave, total);   // (8192 at most of each)
     unsigned ties = base_ties + (before >> 16), place = base + (before & 0xffffu) + min(ties, need);
 #pragma unroll
     for (int e = 0; e < EVICT_EACH; ++e) {
@@ -148,9 +157,9 @@ __global__ void __launch_bounds__(EVICT_THREADS) cached_choose_k(EvictArgs a) {
     base += total & 0xffffu;
     base_ties += total >> 16;
   }
-  for (int t = left + tid; t < a.keep; t += EVICT_THREADS) kept[t] = -1;
+  for (int t = left + tid; t < a.keep; t += THREADS) kept[t] = -1;
   __syncthreads();
-  for (int t = left + tid; t < length; t += EVICT_THREADS) w_out[t] = 0.f;
+  for (int t = left + tid; t < length; t += THREADS) w_out[t] = 0.f;
 }
 
 // The move.  A vector is PIECES of 16 bytes; a workgroup takes of one sequence and head the keys or values, COLS pieces of each, and

@@ -101,6 +101,42 @@ def test_evict_to_other_pages_with_many_heads():
     assert torch.equal(pool[:pages], start)
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("kind", ["plain", "ties", "zeros", "nan"])
+def test_evict_more_slots_than_a_workgroup_holds(kind, in_place):
+    c = gpu()
+    nkv, page, pages, keep, first, recent = 2, 32, 626, 9001, 5, 77
+    length = page * pages - 3
+    g = torch.Generator(device="cuda").manual_seed(68)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.randn(pages + 300, 1, 2, nkv, page, 64, generator=g, device="cuda").to(BF16)
+    start = pool.clone()
+    weights = torch.randn(1, nkv, page * pages, generator=g, device="cuda")
+    if kind == "ties":
+        weights = torch.randint(0, 3, weights.shape, generator=g, device="cuda").float()
+    elif kind == "zeros":
+        weights = torch.where(weights < 0, 0.0, -0.0)
+    elif kind == "nan":
+        weights[weights > 1.5] = float("nan")
+    given = weights.clone()
+    order = torch.where(given.isnan(), float("inf"), given)[0, :, first:length - recent].argsort(dim=1, descending=True, stable=True)[:, :keep - first - recent] + first
+    ends = torch.cat([torch.arange(first, device="cuda"), torch.arange(length - recent, length, device="cuda")])
+    want = torch.cat([ends.expand(nkv, -1), order], dim=1).sort(dim=1).values
+    table = torch.randperm(pages, generator=g, device="cuda").int().view(1, pages)
+    to = None if in_place else (pages + torch.randperm(300, generator=g, device="cuda")[:282]).int().view(1, 282)
+    batch = c.CachedRows(torch.zeros(2, **i32), torch.tensor([length], **i32), table)
+    kept, left = c.cached_evict(c.PagedCache(pool), batch, weights, keep, first, recent, table_out=to)
+    assert torch.equal(kept[0].long(), want) and int(left) == keep
+    new = torch.where(given[0].isnan(), 99.0, given[0])
+    now = torch.where(weights[0].isnan(), 99.0, weights[0])
+    assert torch.equal(now[:, :keep], new.gather(1, want)) and not bool(now[:, keep:length].any()) and torch.equal(now[:, length:], new[:, length:])
+    slot, there = torch.arange(keep, device="cuda"), (table if to is None else to)[0].long()
+    for h in range(nkv):
+        for which in range(2):
+            x = start[table[0].long()[want[h] // page], 0, which, h, want[h] % page]
+            assert torch.equal(pool[there[slot // page], 0, which, h, slot % page], x)
+
+
 FIRST_CALLS = """
 import torch
 from paper_2603_09215_amd import cached as c

@@ -211,6 +211,8 @@ def attend_workspace_bytes(cache: PagedCache, batch: CachedRows, m: int, q_heads
         with torch.cuda.device(cache.pool.device):
             if load_library().spark_cache_workspace_bytes(cache._view(0), batch._of(m, cache), q_heads, C.byref(size)):
                 _refuse(f"attention of {m} rows of {q_heads} heads")
+        if len(cache._workspace) >= 4096:   # (a program with ever new sizes)
+            cache._workspace.clear()
         need = cache._workspace[m, q_heads, batch.n, batch.max_pages] = size.value
     return need
 

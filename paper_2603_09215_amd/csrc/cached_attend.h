@@ -697,7 +697,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
 
 // ------------------------------------------------------------------ the parts together
 
-constexpr int JOIN_AHEAD = 4;   // parts on their way (511 rows of 28 heads in 4 parts: one 39.8 us, two launches, four 40.1, eight 40.5, sixteen 44.3)
+constexpr int JOIN_AHEAD = 4;   // parts on their way (both launches, a group of lanes to a vector: one step of 28 heads in 13 parts, one 12.7 us, four 10.9, eight 10.5, sixteen 10.3;
+                                // 511 rows in 4 parts 39.8, 40.1, 40.5, 44.3)
 
 // GROUPS of lanes to a vector, each with every GROUPS-th part, whose sums are added in their order.
 template <typename T, int HD, int GROUPS>

@@ -16,7 +16,8 @@
 //
 // Slots that a row does not see: their scores are replaced, not added to.  Their values meet zeros, and zero times infinity is
 // NaN, so behind the first row's last slot values that are no numbers go in as zeros, and what the rows that do see
-// them get from them is added at the end (a probability is positive: infinity stays, NaN too).
+// them get from them is added at the end (a probability is positive: infinity stays, NaN too).  Slots that all rows see are not
+// looked at: if sums that are no numbers come of them, the tile is worked on AGAIN, and takes them all so.
 #pragma once
 #include "cached_format.h"
 #include "cached_plan.h"
@@ -63,6 +64,23 @@ template <typename T> __device__ __forceinline__ bool ca_only_numbers(ca_u32x4 &
   }
   v = ca_u32x4{w[0], w[1], w[2], w[3]};
   return bad;
+}
+// The slots of a tile whose values went in as zeros lie in first .. last.  Some of its sums are no numbers: again.
+struct BadSlots { int first, last, again; };
+__device__ __forceinline__ void note_bad(BadSlots &b, int slot) {
+  atomicMin(&b.first, slot);
+  atomicMax(&b.last, slot);
+}
+// (the second time nothing of the first is to be kept for it in registers)
+template <bool AGAIN> __device__ __forceinline__ int this_thread() {
+  int i = threadIdx.x;
+  if constexpr (AGAIN) asm volatile("" : "+v"(i));
+  return i;
+}
+template <bool AGAIN> __device__ __forceinline__ int this_block() {
+  int i = blockIdx.x;
+  if constexpr (AGAIN) asm volatile("" : "+s"(i));
+  return i;
 }
 __device__ __forceinline__ float ca_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // a value of the other half of the wave, and this one
@@ -186,23 +204,24 @@ template <typename T, int HD> struct Stream {
   static_assert(LDS >= (size_t)WAVES * V_BYTES, "values and sums share it");
 };
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
+// false, with nothing written: sums that are no numbers (AGAIN takes no value that is none into its sums)
+template <typename T, int HD, bool AGAIN>
+__device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad) {
   using S = Stream<T, HD>;
   constexpr bool BF = sizeof(T) == 2;
   extern __shared__ uint4 ca_smem[];
+  const int thread = this_thread<AGAIN>(), block = this_block<AGAIN>();
   __shared__ float s_max[S::WAVES][S::PAIRS], s_sum[S::WAVES][S::PAIRS];
-  __shared__ int s_bad;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
-  const int nkv = a.cache.n_kv_heads, kvh = blockIdx.x % nkv, split = blockIdx.x / nkv % a.splits;
+  const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), col = lane & 15, quad = lane >> 4;
+  const int nkv = a.cache.n_kv_heads, kvh = block % nkv, split = block / nkv % a.splits;
   Sequence seq;
   int tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, block / nkv / a.splits, seq, tile, count)) return true;
   const int pair0 = tile * S::PAIRS, pairs = min(S::PAIRS, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
   const int first = split * share, stop = min(all, first + share);   // pieces
-  if (threadIdx.x == 0) s_bad = 0;
+  const int sure = AGAIN ? -1 : least;   // values up to this slot go in as they are
 
   // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
   auto ask_piece = [&](int piece) { return ask(seq, a.cache, piece * S::BLOCKS + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
@@ -223,7 +242,6 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
   float top = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d) o[d] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
-
   ca_u32x4 kr[S::BLOCKS][S::STEPS], vr[S::V_LOADS];
   char *s_v = (char *)ca_smem + wave * S::V_BYTES;
   constexpr int LPT = HD / 8;   // bf16: lanes a token's values take
@@ -251,37 +269,44 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
       }
     }
   };
-  // values behind `least`, and of no page
+  // values behind `sure`, and of no page
   auto clean = [&](int piece, unsigned here) {
     const int t0 = piece * S::TOKENS;
-    bool bad = false;
     if constexpr (BF) {
 #pragma unroll
       for (int e = 0; e < S::V_LOADS; ++e) {
         const int in = (e * 64 + lane) / LPT;
         if (t0 + in >= end || !((here >> (in / 16)) & 1)) vr[e] = ca_u32x4{0, 0, 0, 0};
-        else if (t0 + in > least) bad |= ca_only_numbers<T>(vr[e]);
+        else if (t0 + in > sure && ca_only_numbers<T>(vr[e])) note_bad(s_bad, t0 + in);
       }
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int t = t0 + 4 * quad + e;
+        bool bad = false;
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) {
-          const bool none = (vr[d][e] & 0x7f800000u) == 0x7f800000u;
-          bad |= none && t > least && t < end && here;
-          if (t >= end || !here || (none && t > least)) vr[d][e] = 0u;
+          const bool none = (vr[d][e] & 0x7f800000u) == 0x7f800000u && t > sure;
+          bad |= none;
+          if (t >= end || !here || none) vr[d][e] = 0u;
         }
+        if (bad && t < end && here) note_bad(s_bad, t);
       }
     }
-    if (bad) s_bad = 1;
   };
 
+  float *s_o = (float *)ca_smem;
+  auto most = [&](int c) {
+    float m = s_max[0][c];
+#pragma unroll
+    for (int w = 1; w < S::WAVES; ++w) m = fmaxf(m, s_max[w][c]);
+    return m;
+  };
+  __syncthreads();   // (s_bad)
   if (piece < stop) {
     load_keys();
     load_values();
   }
-  __syncthreads();   // (s_bad)
   for (; piece < stop; piece += S::WAVES) {
     const unsigned here = (unsigned)__ballot(found.there) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
     const int t0 = piece * S::TOKENS;
@@ -305,7 +330,7 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
       asked = ask_piece(piece + 2 * S::WAVES);
       load_keys();
     }
-    const bool masked = t0 + S::TOKENS - 1 > least || here != (1u << S::BLOCKS) - 1;
+    const bool masked = t0 + S::TOKENS - 1 > sure || here != (1u << S::BLOCKS) - 1;
     if (masked) {
       clean(piece, here);
 #pragma unroll
@@ -377,24 +402,23 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
   }
 
   // the waves' sums brought to one maximum and added in order
-  float *s_o = (float *)ca_smem;
   sum += __shfl_xor(sum, 16, 64);
   sum = ca_sum_halves(sum);
   if (quad == 0) { s_max[wave][col] = top; s_sum[wave][col] = sum; }
   __syncthreads();   // (and every wave is done with its values)
-  auto most = [&](int c) {
-    float m = s_max[0][c];
+  const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
+  bool numbers = true;
 #pragma unroll
-    for (int w = 1; w < S::WAVES; ++w) m = fmaxf(m, s_max[w][c]);
-    return m;
-  };
-  {
-    const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
+  for (int d = 0; d < HD / 16; ++d) {
+    const ca_f32x4 x = o[d] * f;
+    *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = x;
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = o[d] * f;
+    for (int e = 0; e < 4; ++e) numbers &= fabsf(x[e]) < INFINITY;
   }
+  if (!AGAIN && !numbers) s_bad.again = 1;
   __syncthreads();
-  for (int i = threadIdx.x; i < pairs * (HD / 4); i += 64 * S::WAVES) {
+  if (!AGAIN && __builtin_amdgcn_readfirstlane(s_bad.again)) return false;
+  for (int i = thread; i < pairs * (HD / 4); i += 64 * S::WAVES) {
     const int c = i / (HD / 4), e0 = i % (HD / 4) * 4, p = pair0 + c;
     const float m = most(c);
     float l = 0.f;
@@ -405,9 +429,9 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
       y += *(const ca_f32x4 *)(s_o + (w * S::PAIRS + c) * S::O_PITCH + e0);
     }
     const int row = p / a.group, r = seq.row0 + row, h = kvh * a.group + p % a.group;
-    if (s_bad) {
-      const int last = min(last_seen(seq, row, a.causal), stop * S::TOKENS - 1);
-      for (int t = max(first * S::TOKENS, least + 1); t <= last; ++t) {
+    if (s_bad.last >= 0) {
+      const int last = min(last_seen(seq, row, a.causal), s_bad.last);
+      for (int t = s_bad.first; t <= last; ++t) {
         const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
         if (page < 0) continue;
 #pragma unroll
@@ -419,6 +443,16 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
     }
     finish<T, HD>(a, split, r, h, e0, y, m, l);
   }
+  return true;
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
+  __shared__ BadSlots s_bad;
+  if (threadIdx.x == 0) s_bad = BadSlots{1 << 30, -1, 0};
+  if (stream_tile<T, HD, false>(a, s_bad)) return;   // (the same for all of a workgroup)
+  __syncthreads();
+  stream_tile<T, HD, true>(a, s_bad);
 }
 
 // ------------------------------------------------------------------ many pairs
@@ -438,24 +472,25 @@ template <int HD, int WAVES> struct Tile {
   static constexpr size_t LDS = TILES > SUMS ? TILES : SUMS;
 };
 
-template <int HD, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
+// false, for some lanes: sums that are no numbers, as above (but they are written, for to keep them over the branch costs 68 registers)
+template <int HD, int WAVES, bool AGAIN>
+__device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) {
   using T = bf16_t;
   using S = Tile<HD, WAVES>;
   constexpr int STEPS = HD * (int)sizeof(T) / 32;   // 16-byte pieces of a query that a lane holds
   extern __shared__ uint4 ca_smem[];
-  __shared__ int s_bad;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int nkv = a.cache.n_kv_heads, kvh = blockIdx.x % nkv, split = blockIdx.x / nkv % a.splits;
+  const int thread = this_thread<AGAIN>(), block = this_block<AGAIN>();
+  const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), col = lane & 31, half = lane >> 5;
+  const int nkv = a.cache.n_kv_heads, kvh = block % nkv, split = block / nkv % a.splits;
   Sequence seq;
   int tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, blockIdx.x / nkv / a.splits, seq, tile, count)) return;
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, block / nkv / a.splits, seq, tile, count)) return true;
   tile = count - 1 - tile;   // the longest first
   const int pair0 = tile * S::PAIRS, pairs = min(S::PAIRS, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
   const int first = split * share, stop = min(all, first + share);   // tiles of tokens
-  if (threadIdx.x == 0) s_bad = 0;
+  const int sure = AGAIN ? -1 : least;   // values up to this slot go in as they are
 
   const int p = pair0 + min(wave * 32 + col, pairs - 1), row = p / a.group;
   const bool works = wave * 32 < pairs;
@@ -470,7 +505,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
   }
 
   char *lds = (char *)ca_smem;
-  const int st = threadIdx.x / S::LPT, sc16 = threadIdx.x % S::LPT;   // this thread's token in a pass, and 16 bytes of it
+  const int st = thread / S::LPT, sc16 = thread % S::LPT;   // this thread's token in a pass, and 16 bytes of it
   ca_u32x4 kr[S::LOADS], vr[S::LOADS];
   // a tile's four 16s are found by lanes 0..3; a wave's tokens of a pass lie in one of them
   auto ask_tile = [&](int t) { return ask(seq, a.cache, 4 * t + (lane & 3), t < stop ? end : 0); };
@@ -484,16 +519,14 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
       to[i] = *(const ca_u32x4 *)(at_lane(planes[which], f, i * (S::PER / 16) + sixteen) + in_sixteen);
     }
   };
-  auto clean = [&](int t, unsigned here) {   // values behind `least`, and of no page
-    if (t * S::TOKENS + S::TOKENS - 1 <= least && here == 15u) return;
-    bool bad = false;
+  auto clean = [&](int t, unsigned here) {   // values behind `sure`, and of no page
+    if (t * S::TOKENS + S::TOKENS - 1 <= sure && here == 15u) return;
 #pragma unroll
     for (int i = 0; i < S::LOADS; ++i) {
       const int in = i * S::PER + st, token = t * S::TOKENS + in;
       if (token >= end || !((here >> (in >> 4)) & 1)) vr[i] = ca_u32x4{0, 0, 0, 0};
-      else if (token > least) bad |= ca_only_numbers<T>(vr[i]);
+      else if (token > sure && ca_only_numbers<T>(vr[i])) note_bad(s_bad, token);
     }
-    if (bad) s_bad = 1;
   };
   auto store = [&](char *to, const ca_u32x4 (&from)[S::LOADS]) {
 #pragma unroll
@@ -648,10 +681,15 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
     }
     __syncthreads();
   }
+  bool numbers = true;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) numbers &= fabsf(o[d][r]) < INFINITY;
 
   sum = ca_sum_halves(sum);
-  if (s_bad) {   // (the last store lies before the last barrier)
-    for (int t = max(first * S::TOKENS, least + 1); t < min(end, stop * S::TOKENS); ++t) {
+  if (s_bad.last >= 0) {   // (the last store lies before the last barrier)
+    for (int t = s_bad.first; t <= s_bad.last; ++t) {
       const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
       if (page < 0 || t > limit) continue;
       const T *v = a.cache.plane<T>(page, 1, kvh) + t % a.cache.page_tokens * HD + 4 * half;
@@ -693,6 +731,19 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
         finish<T, HD>(a, split, out_row[i], out_head[i], 32 * d + 4 * (lane & 7), *(const ca_f32x4 *)(s_o + c * S::O_PITCH + 4 * (lane & 7)), ml.x, ml.y);
     }
   }
+  return numbers;
+}
+
+template <int HD, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
+  __shared__ BadSlots s_bad;
+  if (threadIdx.x == 0) s_bad = BadSlots{1 << 30, -1, 0};
+  if (!work_tile<HD, WAVES, false>(a, s_bad)) s_bad.again = 1;
+  wait_memory_ops();   // (what has been written is written over)
+  __syncthreads();
+  if (!__builtin_amdgcn_readfirstlane(s_bad.again)) return;
+  __syncthreads();
+  work_tile<HD, WAVES, true>(a, s_bad);
 }
 
 // ------------------------------------------------------------------ the parts together
@@ -748,7 +799,7 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
     if (s0 > group) fetch(s0);
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k) {
-      const bool none = s0 + k * GROUPS >= a.splits || ml[k].y == 0.f;   // (its sums were not written)
+      const bool none = s0 + k * GROUPS >= a.splits;
       const float g = none ? 0.f : ca_exp2(ml[k].x - base);
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] += none ? 0.f : g == 0.f && !(fabsf(v[k][e]) < INFINITY) ? v[k][e] : v[k][e] * g;   // (an infinity stays one)

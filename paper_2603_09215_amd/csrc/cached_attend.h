@@ -11,8 +11,9 @@
 //                    unfinished sums come through the workspace; this adds them up in order.
 //
 // In all: scores transposed, S^T [token][pair] = K Q^T, so a lane holds scores of one pair and finds their maximum and sum
-// by itself; and since a sum over tokens may go in any order, those registers are, rounded, the operand of O^T = V^T P^T as
-// they are.  Exponentials are of base 2, the scores' factor is scale log2 e.
+// by itself; and since a sum over tokens may go in any order, those registers are the operand of O^T = V^T P^T as
+// they are, with a bf16 cache as two parts of bf16 (one would be 2^-8 off, as much as the result's own rounding).  Exponentials are of base 2, the
+// scores' factor is scale log2 e.
 //
 // Slots that a row does not see: their scores are replaced, not added to.  Their values meet zeros, and zero times infinity is
 // NaN, so behind the first row's last slot values that are no numbers go in as zeros, and what the rows that do see
@@ -379,7 +380,10 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
         sum += sc[i][e];
       }
     if constexpr (BF) {
-      const ca_bf16x8 p = ca_operand(ca_u32x4{pack_bf16(sc[0][0], sc[0][1]), pack_bf16(sc[0][2], sc[0][3]), pack_bf16(sc[1][0], sc[1][1]), pack_bf16(sc[1][2], sc[1][3])});
+      uint32_t high[4], low[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pack_bf16_parts(sc[i / 2][i % 2 * 2], sc[i / 2][i % 2 * 2 + 1], high[i], low[i]);
+      const ca_bf16x8 p = ca_operand(ca_u32x4{high[0], high[1], high[2], high[3]}), rest = ca_operand(ca_u32x4{low[0], low[1], low[2], low[3]});
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
         union { ca_s16x4 h[2]; ca_bf16x8 v; } x;
@@ -390,6 +394,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
               (__attribute__((address_space(3))) ca_s16x4 *)(s_v + t * HD * 2 + ((c ^ ca_turn<T, HD>(t)) << 4) + 8 * (col & 1)));
         }
         o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, p, o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, rest, o[d], 0, 0, 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -459,14 +464,15 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
 
 // WAVES waves of 32 pairs each, bf16; tiles of 64 tokens' keys and values in LDS, two of them, so that the next one's loads run while one is
 // worked on.  Matrix instructions of 32 x 32 (A: a lane's token or head element is l mod 32, its k those of l / 32); a lane
-// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.  8191 rows of 28 heads of 128: 535 us and more, 900 TFLOP/s, where a
-// library's product reaches 1140.  (fp32's matrix instructions
+// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.  8191 rows of 28 heads of 128: 711 us, 1015 TFLOP/s with the second part's
+// products (one part took 545), where a library's product reaches 1140.  (fp32's matrix instructions
 // take so long that the stream keeps up: such a kernel took 339 us against 361 for 2000 rows of 28 heads, 106 against 101 for 16 heads of 64.)
 template <int HD, int WAVES> struct Tile {
   static constexpr int TOKENS = 64, PAIRS = 32 * WAVES;
   static constexpr int ROW = HD * (int)sizeof(bf16_t), LPT = ROW / 16;                   // bytes of a token, lanes that they take
   static constexpr int PER = 64 * WAVES / LPT, LOADS = TOKENS / PER;                // tokens of a pass of loads, passes
   static constexpr int BYTES = TOKENS * ROW;
+  static constexpr int AHEAD = HD == 128 ? 0 : 1;                                    // steps of 16 tokens' values read ahead
   static constexpr int O_PITCH = 36;                                                // floats of a pair, of 32 elements
   static constexpr size_t TILES = 4 * (size_t)BYTES, SUMS = sizeof(float) * PAIRS * (O_PITCH + 2);   // keys and values, two buffers; later results
   static constexpr size_t LDS = TILES > SUMS ? TILES : SUMS;
@@ -539,7 +545,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
   auto values_at = [&](int t) { return lds + (2 + ((t - first) & 1)) * S::BYTES; };
 
   ca_f32x16 o[HD / 32], sc[2];   // unfinished sums [head element][pair], scores [token][pair]
-  uint32_t pr[16];               // probabilities in bf16, two a register
+  uint32_t pr[2][16];            // probabilities: parts, two of bf16 a register
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
@@ -606,7 +612,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
       for (int b = 0; b < 2; ++b) {
         sc[b][r] = ca_exp2(fmaf(sc[b][r], a.factor, -base));
         s2[b] += sc[b][r];
-        if (r & 1) pr[8 * b + (r >> 1)] = pack_bf16(sc[b][r - 1], sc[b][r]);
+        if (r & 1) pack_bf16_parts(sc[b][r - 1], sc[b][r], pr[0][8 * b + (r >> 1)], pr[1][8 * b + (r >> 1)]);
       }
     sum += s2[0] + s2[1];
   };
@@ -622,19 +628,31 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
       }
       return x.v;
     };
-    ca_bf16x8 v[2][HD / 32];
+    // Operands are used for both parts of the probabilities.  They are read 16 tokens ahead; of heads of 128, for which registers do not reach, two blocks of
+    // the head as soon as the last tokens' are done with (tiles of eight waves, which have them for either: 711 us so, 716).  The barriers hold the order.
+    constexpr int AHEAD = S::AHEAD;
+    ca_bf16x8 v[1 + AHEAD][HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) v[0][d] = value(0, d);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (j < 3)
+      if (AHEAD && j < 3)
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d) v[(j + 1) & 1][d] = value(j + 1, d);
-      __builtin_amdgcn_sched_barrier(0);
-      const ca_bf16x8 p8 = ca_operand(ca_u32x4{pr[4 * j], pr[4 * j + 1], pr[4 * j + 2], pr[4 * j + 3]});
+        for (int d = 0; d < HD / 32; ++d) v[(j + 1) & AHEAD][d] = value(j + 1, d);
+      const ca_bf16x8 p[2] = {ca_operand(ca_u32x4{pr[0][4 * j], pr[0][4 * j + 1], pr[0][4 * j + 2], pr[0][4 * j + 3]}),
+                              ca_operand(ca_u32x4{pr[1][4 * j], pr[1][4 * j + 1], pr[1][4 * j + 2], pr[1][4 * j + 3]})};
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[j & 1][d], p8, o[d], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int d0 = 0; d0 < HD / 32; d0 += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = d0; d < d0 + 2; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[j & AHEAD][d], p[i], o[d], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!AHEAD && j < 3)
+#pragma unroll
+          for (int d = d0; d < d0 + 2; ++d) v[0][d] = value(j + 1, d);
+      }
     }
   };
 

@@ -35,6 +35,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {   // half to e
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, ca_bf16x2));
 }
 
+// two parts that add up to a and b but for 2^-16 of them: what each is rounded to, and what that leaves
+__device__ __forceinline__ void pack_bf16_parts(float a, float b, uint32_t &high, uint32_t &low) {
+  high = pack_bf16(a, b);
+  low = pack_bf16(a - __uint_as_float(high << 16), b - __uint_as_float(high & 0xffff0000u));
+}
+
 __device__ __forceinline__ int cut(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 __device__ __forceinline__ Sequence sequence(const BatchView &b, int s, int page_tokens) {

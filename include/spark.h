@@ -493,7 +493,7 @@ int spark_cache_workspace_bytes(const spark_cache *cache, const spark_cache_batc
  * with kv head h / (n_q_heads / n_kv_heads); q and out of the cache's type, 16-byte aligned, strides multiples of 8 elements.
  * lse (or NULL) fp32 [m][n_q_heads]: log sum exp(scale q . k_t).  A row that sees nothing gets zeros, and minus infinity
  * in lse, and so does one whose scores are all minus infinity.  An element of a value that is seen and no number makes that element of the result
- * infinite or NaN, as any probability above zero does.  scale is not 0 and at most 2^127.  Scores, maxima and sums are fp32; with a bf16 cache the probabilities go into their products with the
+ * infinite or NaN, as any probability above zero does; values up to 2^127 make no result infinite.  scale is not 0 and at most 2^127.  Scores, maxima and sums are fp32; with a bf16 cache the probabilities go into their products with the
  * values as two parts of bf16, 2^-16 of each off. */
 int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q,
                        int64_t q_stride, float scale, int32_t causal, void *out, int64_t out_stride, float *lse,

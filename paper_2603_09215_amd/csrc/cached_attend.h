@@ -18,7 +18,9 @@
 // Slots that a row does not see: their scores are replaced, not added to.  Their values meet zeros, and zero times infinity is
 // NaN, so behind the first row's last slot values that are no numbers go in as zeros, and what the rows that do see
 // them get from them is added at the end (a probability is positive: infinity stays, NaN too).  Slots that all rows see are not
-// looked at: if sums that are no numbers come of them, the tile is worked on AGAIN, and takes them all so.
+// looked at: if sums that are no numbers come of them, the tile is worked on AGAIN, and takes them all so.  Sums of large values may
+// have left fp32's range before they were divided by L: the second time all probabilities are 2^32 smaller (2^23 slots of up to 2^8 each have room), which
+// changes no bit of what was in range; parts say so by a negative sum.
 #pragma once
 #include "cached_format.h"
 #include "cached_plan.h"
@@ -169,24 +171,25 @@ __device__ __forceinline__ const char *at_lane(const char *plane, const Found &f
 }
 
 template <typename T, int HD>
-__device__ __forceinline__ void write_result(const AttendArgs &a, int r, int h, int e0, ca_f32x4 y, float m, float l) {
-  y *= l == 0.f ? 0.f : 1.0f / l;
+__device__ __forceinline__ void write_result(const AttendArgs &a, int r, int h, int e0, ca_f32x4 y, float m, float l, float scale) {   // y: of sums as many times smaller
+  y *= l == 0.f ? 0.f : scale / l;
   T *out = (T *)a.out + r * a.out_stride + (long long)h * HD + e0;
   if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
   else *(ca_f32x4 *)out = y;
   if (a.lse && e0 == 0) a.lse[(long long)r * a.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
 }
-// four elements of a row and head: the result, or with more parts than one what it is joined from (m: maximum, l: sum)
-template <typename T, int HD>
+// four elements of a row and head: the result, or with more parts than one what it is joined from (m: maximum, l: sum; SMALL: y is 2^32 smaller).
+// Every part of a row that is somebody's comes here, an empty one with zeros.
+template <typename T, int HD, bool SMALL>
 __device__ __forceinline__ void finish(const AttendArgs &a, int split, int r, int h, int e0, ca_f32x4 y, float m, float l) {
   const long long i = (long long)r * a.n_q_heads + h;
   if (a.splits > 1) {
     const long long at = (long long)split * a.batch.m * a.n_q_heads + i;
     *(ca_f32x4 *)(a.part + at * HD + e0) = y;
-    if (e0 == 0) a.part_ml[at] = make_float2(m, l);
+    if (e0 == 0) a.part_ml[at] = make_float2(m, SMALL ? -l : l);
     return;
   }
-  write_result<T, HD>(a, r, h, e0, y, m, l);
+  write_result<T, HD>(a, r, h, e0, y, m, l, SMALL ? 0x1p32f : 1.f);
 }
 
 // ------------------------------------------------------------------ few pairs
@@ -223,6 +226,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
   const int first = split * share, stop = min(all, first + share);   // pieces
   const int sure = AGAIN ? -1 : least;   // values up to this slot go in as they are
+  constexpr float SMALL = AGAIN ? 0x1p-32f : 1.f;
 
   // (waiting for a load waits for all before it: a piece's pages are asked for ahead of the last piece's keys and values)
   auto ask_piece = [&](int piece) { return ask(seq, a.cache, piece * S::BLOCKS + (lane & (S::BLOCKS - 1)), piece < stop ? end : 0); };
@@ -376,7 +380,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
     for (int i = 0; i < S::BLOCKS; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        sc[i][e] = ca_exp2(fmaf(sc[i][e], a.factor, -base));
+        sc[i][e] = SMALL * ca_exp2(fmaf(sc[i][e], a.factor, -base));
         sum += sc[i][e];
       }
     if constexpr (BF) {
@@ -408,7 +412,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
 
   // the waves' sums brought to one maximum and added in order
   sum += __shfl_xor(sum, 16, 64);
-  sum = ca_sum_halves(sum);
+  sum = ca_sum_halves(sum) * (1.f / SMALL);
   if (quad == 0) { s_max[wave][col] = top; s_sum[wave][col] = sum; }
   __syncthreads();   // (and every wave is done with its values)
   const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
@@ -418,7 +422,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
     const ca_f32x4 x = o[d] * f;
     *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) numbers &= fabsf(x[e]) < INFINITY;
+    for (int e = 0; e < 4; ++e) numbers &= fabsf(x[e]) < 0x1p125f;   // (four of them are added)
   }
   if (!AGAIN && !numbers) s_bad.again = 1;
   __syncthreads();
@@ -446,7 +450,7 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
         }
       }
     }
-    finish<T, HD>(a, split, r, h, e0, y, m, l);
+    finish<T, HD, AGAIN>(a, split, r, h, e0, y, m, l);
   }
   return true;
 }
@@ -497,6 +501,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
   const int all = (end + S::TOKENS - 1) / S::TOKENS, share = (all + a.splits - 1) / a.splits;
   const int first = split * share, stop = min(all, first + share);   // tiles of tokens
   const int sure = AGAIN ? -1 : least;   // values up to this slot go in as they are
+  constexpr float SMALL = AGAIN ? 0x1p-32f : 1.f;
 
   const int p = pair0 + min(wave * 32 + col, pairs - 1), row = p / a.group;
   const bool works = wave * 32 < pairs;
@@ -610,7 +615,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
     for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        sc[b][r] = ca_exp2(fmaf(sc[b][r], a.factor, -base));
+        sc[b][r] = SMALL * ca_exp2(fmaf(sc[b][r], a.factor, -base));
         s2[b] += sc[b][r];
         if (r & 1) pack_bf16_parts(sc[b][r - 1], sc[b][r], pr[0][8 * b + (r >> 1)], pr[1][8 * b + (r >> 1)]);
       }
@@ -705,7 +710,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
 #pragma unroll
     for (int r = 0; r < 16; ++r) numbers &= fabsf(o[d][r]) < INFINITY;
 
-  sum = ca_sum_halves(sum);
+  sum = ca_sum_halves(sum) * (1.f / SMALL);
   if (s_bad.last >= 0) {   // (the last store lies before the last barrier)
     for (int t = s_bad.first; t <= s_bad.last; ++t) {
       const int page = page_of(seq, t, a.cache.page_tokens, a.cache.n_pages);
@@ -746,7 +751,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
       const int c = 8 * i + (lane >> 3);
       const float2 ml = s_ml[c];
       if (out_row[i] >= 0)
-        finish<T, HD>(a, split, out_row[i], out_head[i], 32 * d + 4 * (lane & 7), *(const ca_f32x4 *)(s_o + c * S::O_PITCH + 4 * (lane & 7)), ml.x, ml.y);
+        finish<T, HD, AGAIN>(a, split, out_row[i], out_head[i], 32 * d + 4 * (lane & 7), *(const ca_f32x4 *)(s_o + c * S::O_PITCH + 4 * (lane & 7)), ml.x, ml.y);
     }
   }
   return numbers;
@@ -792,11 +797,13 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
     }
   };
   fetch(group);
-  bool ours = false;   // somebody's row
+  bool ours = false, small = false;   // somebody's row; some of its parts are 2^32 smaller
   for (int s = lane; s < a.batch.n; s += LANES) ours |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1];
   float l = 0.f, m = -INFINITY;
   for (int s = lane; s < a.splits; s += LANES) {
-    const float2 x = a.part_ml[s * step + i];
+    float2 x = a.part_ml[s * step + i];
+    small |= x.y < 0.f;
+    x.y = fabsf(x.y);
     const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
     l = (l == 0.f ? 0.f : l * ca_exp2(m - base)) + (x.y == 0.f ? 0.f : x.y * ca_exp2(x.x - base));
     m = top;
@@ -806,19 +813,22 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
   for (int o = LANES / 2; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor(m, o, LANES));
     ours |= __shfl_xor((int)ours, o, LANES) != 0;
+    small |= __shfl_xor((int)small, o, LANES) != 0;
   }
   if (!ours) return;
   const float base = m == -INFINITY ? 0.f : m;
   l = l == 0.f ? 0.f : l * ca_exp2(mine - base);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, LANES);
+  static_assert(MOST_SPLITS <= 256, "sums that fp32 holds, 2^8 smaller, have room");
+  const float scale = small ? 0x1p-32f : 0x1p-8f;
   ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = group; s0 < a.splits; s0 += JOIN_AHEAD * GROUPS) {
     if (s0 > group) fetch(s0);
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k) {
       const bool none = s0 + k * GROUPS >= a.splits;
-      const float g = none ? 0.f : ca_exp2(ml[k].x - base);
+      const float g = none ? 0.f : ca_exp2(ml[k].x - base) * (ml[k].y < 0.f ? 1.f : scale);
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] += none ? 0.f : g == 0.f && !(fabsf(v[k][e]) < INFINITY) ? v[k][e] : v[k][e] * g;   // (an infinity stays one)
     }
@@ -831,7 +841,7 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
 #pragma unroll
     for (int j = 1; j < GROUPS; ++j) y += s_y[j][lane];
   }
-  write_result<T, HD>(a, r, (int)(i % a.n_q_heads), e0, y, m, l);
+  write_result<T, HD>(a, r, (int)(i % a.n_q_heads), e0, y, m, l, 1.f / scale);
 }
 
 }  // namespace spark

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
       if (sum > 1e-30f && sum < 1e37f) {
         const float f = __builtin_amdgcn_rsqf(sum * (1.0f / HD) + (float)a.eps);   // (off by a last bit)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= f * gain[e];
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * f * gain[e];   // (the factor times the gain might leave fp32's range)
       } else {   // squares that leave fp32's range (the same lanes for all of a head)
         double wide = 0.0;
 #pragma unroll

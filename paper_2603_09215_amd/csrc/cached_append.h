@@ -181,11 +181,11 @@ __global__ void __launch_bounds__(256) cached_append_k(AppendArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
       sum = head_sum<LANES>(sum);
-      if (sum > 1e-30f && sum < 1e37f) {
+      if (sum > 1e-30f && sum < 1e37f && a.eps < 1e37) {
         const float f = __builtin_amdgcn_rsqf(sum * (1.0f / HD) + (float)a.eps);   // (off by a last bit)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * f * gain[e];   // (the factor times the gain might leave fp32's range)
-      } else {   // squares that leave fp32's range (the same lanes for all of a head)
+      } else {   // squares, or eps, that leave fp32's range (the same lanes for all of a head)
         double wide = 0.0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) wide += (double)x[e] * x[e];

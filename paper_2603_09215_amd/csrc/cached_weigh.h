@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
-  float total[TB];
+  float total[TB], lost[TB];   // of this wave's blocks so far, and what their additions have lost: rows may be many
   // what a block's pairs give tokens t0 + 32 j + col
   auto add_block = [&](int b, int t0, const ca_u32x4 (&k)[TB][STEPS], const ca_u32x4 (&q)[STEPS]) {
     const bool masked = some_out || t0 + 32 * TB - 1 > last_seen(seq, b * 32 / a.group, a.causal);
@@ -134,6 +134,9 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
         }
       }
     }
+    float sum[TB];
+#pragma unroll
+    for (int j = 0; j < TB; ++j) sum[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {   // pairs 8 i + 4 half + 0..3
       const float4 bias = s_bias[wave][2 * i + half];
@@ -154,8 +157,18 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
 #pragma unroll
       for (int j = 0; j < TB; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) total[j] += x[j][e];
+        for (int e = 0; e < 4; ++e) sum[j] += x[j][e];
     }
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const float more = sum[j] - lost[j], now = total[j] + more;
+      lost[j] = now < INFINITY ? now - total[j] - more : 0.f;   // (an infinity stays one)
+      total[j] = now;
+    }
+  };
+  auto begin = [&]() {
+#pragma unroll
+    for (int j = 0; j < TB; ++j) total[j] = lost[j] = 0.f;
   };
   auto last_of = [&](int b) { return last_seen(seq, min(b * 32 + 31, pairs - 1) / a.group, a.causal); };   // what block b sees
   auto write = [&](int piece, bool has_page, float sum) {
@@ -196,9 +209,9 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
         block[token * VECS + ((lane ^ token) & (VECS - 1))] = share[j];
       }
       __syncthreads();
+      begin();
 #pragma unroll
       for (int j = 0; j < TB; ++j) {
-        total[j] = 0.f;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) k[j][i] = turned((W::WAVES + j) * 32 + col, i);
       }
@@ -239,7 +252,7 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
         asked = ask_piece(piece + 2 * step);
         load_keys(found, ahead);
       }
-      total[0] = 0.f;
+      begin();
       for (int b = 0; b < blocks; ++b) {
         if (t0 > last_of(b)) continue;
         if (b != held) {

@@ -45,7 +45,7 @@ def _heads(t, what: str, head_dim: int, dtypes, shape=None):
         _refuse(f"{what} is {m} x {heads} x {hd}, {' x '.join(map(str, (*(shape or ('rows', 'heads')), head_dim)))} is wanted")
     if step != 1 or (of_head != hd and heads > 1) or (m > 1 and stride < heads * hd):
         _refuse(f"{what}: a row's heads must lie next to each other, and rows apart")
-    return t.data_ptr(), stride if m > 1 else max(stride, heads * hd)
+    return t.data_ptr(), stride if m > 1 else heads * hd   # (of a single row torch may say anything)
 
 
 def _call(what: str, cache, batch, tensors, written, call, *args):

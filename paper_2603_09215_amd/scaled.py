@@ -64,12 +64,12 @@ def _matrix(t, what: str, shape=None):
     return t.data_ptr(), code, stride, m, k
 
 
-def _no_gradient(*tensors):
+def _no_gradient(*tensors, what: str = "an operator on 8-bit rows"):
     """nothing may pass whose gradient or tangent would be lost without a word"""
     dual = forward_ad._current_level >= 0   # (outside a level of forward mode there are no tangents)
     for t in tensors:
         if t is not None and ((t.requires_grad and torch.is_grad_enabled()) or (dual and forward_ad.unpack_dual(t).tangent is not None)):
-            _refuse("the operators on 8-bit rows have no derivatives, and a gradient or tangent of a tensor is wanted")
+            _refuse(f"{what} has no derivatives, and a gradient or tangent of a tensor is wanted")
 
 
 def _launch(what: str, tensors, written, call, *args):
@@ -81,9 +81,9 @@ def _launch(what: str, tensors, written, call, *args):
             if t.get_device() != dev:
                 _refuse("the tensors are on different devices")
             if t.requires_grad:
-                _no_gradient(t)
+                _no_gradient(t, what=what)
     if forward_ad._current_level >= 0:
-        _no_gradient(*tensors)
+        _no_gradient(*tensors, what=what)
     if dev == _device():
         rc = call(*args, _stream(dev))
     else:

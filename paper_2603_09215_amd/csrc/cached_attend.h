@@ -307,11 +307,11 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
     for (int w = 1; w < S::WAVES; ++w) m = fmaxf(m, s_max[w][c]);
     return m;
   };
-  __syncthreads();   // (s_bad)
   if (piece < stop) {
     load_keys();
     load_values();
   }
+  __syncthreads();   // (s_bad)
   for (; piece < stop; piece += S::WAVES) {
     const unsigned here = (unsigned)__ballot(found.there) & ((1u << S::BLOCKS) - 1);   // which 16s of the piece have a page
     const int t0 = piece * S::TOKENS;
@@ -415,28 +415,40 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
   sum = ca_sum_halves(sum) * (1.f / SMALL);
   if (quad == 0) { s_max[wave][col] = top; s_sum[wave][col] = sum; }
   __syncthreads();   // (and every wave is done with its values)
-  const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
-  bool numbers = true;
+  {
+    const float m = most(col), f = ca_exp2(top - (m == -INFINITY ? 0.f : m));
 #pragma unroll
-  for (int d = 0; d < HD / 16; ++d) {
-    const ca_f32x4 x = o[d] * f;
-    *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) numbers &= fabsf(x[e]) < 0x1p125f;   // (four of them are added)
+    for (int d = 0; d < HD / 16; ++d) *(ca_f32x4 *)(s_o + (wave * S::PAIRS + col) * S::O_PITCH + 16 * d + 4 * quad) = o[d] * f;
   }
-  if (!AGAIN && !numbers) s_bad.again = 1;
   __syncthreads();
-  if (!AGAIN && __builtin_amdgcn_readfirstlane(s_bad.again)) return false;
-  for (int i = thread; i < pairs * (HD / 4); i += 64 * S::WAVES) {
-    const int c = i / (HD / 4), e0 = i % (HD / 4) * 4, p = pair0 + c;
-    const float m = most(c);
-    float l = 0.f;
-    ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  // a thread has four elements of ITEMS pairs
+  constexpr int ITEMS = S::PAIRS * (HD / 4) / (64 * S::WAVES);
+  float m[ITEMS], l[ITEMS];
+  ca_f32x4 y[ITEMS];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = k * 64 * S::WAVES + thread, c = i / (HD / 4);
+    m[k] = most(c);
+    l[k] = 0.f;
+    y[k] = ca_f32x4{0.f, 0.f, 0.f, 0.f};
+    bool numbers = true;
 #pragma unroll
     for (int w = 0; w < S::WAVES; ++w) {
-      l += s_sum[w][c] * ca_exp2(s_max[w][c] - (m == -INFINITY ? 0.f : m));
-      y += *(const ca_f32x4 *)(s_o + (w * S::PAIRS + c) * S::O_PITCH + e0);
+      l[k] += s_sum[w][c] * ca_exp2(s_max[w][c] - (m[k] == -INFINITY ? 0.f : m[k]));
+      y[k] += *(const ca_f32x4 *)(s_o + (w * S::PAIRS + c) * S::O_PITCH + i % (HD / 4) * 4);
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) numbers &= fabsf(y[k][e]) < INFINITY;
+    if (!AGAIN && !numbers) s_bad.again = 1;
+  }
+  if constexpr (!AGAIN) {
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(s_bad.again)) return false;
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = k * 64 * S::WAVES + thread, c = i / (HD / 4), e0 = i % (HD / 4) * 4, p = pair0 + c;
+    if (c >= pairs) break;
     const int row = p / a.group, r = seq.row0 + row, h = kvh * a.group + p % a.group;
     if (s_bad.last >= 0) {
       const int last = min(last_seen(seq, row, a.causal), s_bad.last);
@@ -446,11 +458,11 @@ __device__ __forceinline__ bool stream_tile(const AttendArgs &a, BadSlots &s_bad
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float v = Elem<T>::widen(a.cache.plane<T>(page, 1, kvh)[t % a.cache.page_tokens * HD + e0 + e]);
-          if (!(fabsf(v) < INFINITY)) y[e] += v;
+          if (!(fabsf(v) < INFINITY)) y[k][e] += v;
         }
       }
     }
-    finish<T, HD, AGAIN>(a, split, r, h, e0, y, m, l);
+    finish<T, HD, AGAIN>(a, split, r, h, e0, y[k], m[k], l[k]);
   }
   return true;
 }
@@ -482,9 +494,9 @@ template <int HD, int WAVES> struct Tile {
   static constexpr size_t LDS = TILES > SUMS ? TILES : SUMS;
 };
 
-// false, for some lanes: sums that are no numbers, as above (but they are written, for to keep them over the branch costs 68 registers)
+// As stream_tile, but that it says so in s_bad and goes on to the end without writing (to leave in the middle keeps the sums over the branch, in 68 registers).
 template <int HD, int WAVES, bool AGAIN>
-__device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) {
+__device__ __forceinline__ void work_tile(const AttendArgs &a, BadSlots &s_bad) {
   using T = bf16_t;
   using S = Tile<HD, WAVES>;
   constexpr int STEPS = HD * (int)sizeof(T) / 32;   // 16-byte pieces of a query that a lane holds
@@ -494,7 +506,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
   const int nkv = a.cache.n_kv_heads, kvh = block % nkv, split = block / nkv % a.splits;
   Sequence seq;
   int tile, count;
-  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, block / nkv / a.splits, seq, tile, count)) return true;
+  if (!find_tile(a.batch, a.cache.page_tokens, a.group, S::PAIRS, a.by_row, block / nkv / a.splits, seq, tile, count)) return;
   tile = count - 1 - tile;   // the longest first
   const int pair0 = tile * S::PAIRS, pairs = min(S::PAIRS, seq.rows * a.group - pair0);
   const int end = last_seen(seq, (pair0 + pairs - 1) / a.group, a.causal) + 1, least = last_seen(seq, pair0 / a.group, a.causal);
@@ -704,12 +716,16 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
     }
     __syncthreads();
   }
-  bool numbers = true;
+  if constexpr (!AGAIN) {
+    bool numbers = true;
 #pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
+    for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) numbers &= fabsf(o[d][r]) < INFINITY;
-
+      for (int r = 0; r < 16; ++r) numbers &= fabsf(o[d][r]) < INFINITY;
+    if (!numbers) s_bad.again = 1;
+    __syncthreads();
+  }
+  const bool writes = AGAIN || !s_bad.again;
   sum = ca_sum_halves(sum) * (1.f / SMALL);
   if (s_bad.last >= 0) {   // (the last store lies before the last barrier)
     for (int t = s_bad.first; t <= s_bad.last; ++t) {
@@ -734,7 +750,7 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int c = wave * 32 + 8 * i + (lane >> 3), pc = pair0 + c;
-    out_row[i] = c < pairs ? seq.row0 + pc / a.group : -1;
+    out_row[i] = writes && c < pairs ? seq.row0 + pc / a.group : -1;
     out_head[i] = kvh * a.group + pc % a.group;
   }
 #pragma unroll
@@ -754,15 +770,13 @@ __device__ __forceinline__ bool work_tile(const AttendArgs &a, BadSlots &s_bad) 
         finish<T, HD, AGAIN>(a, split, out_row[i], out_head[i], 32 * d + 4 * (lane & 7), *(const ca_f32x4 *)(s_o + c * S::O_PITCH + 4 * (lane & 7)), ml.x, ml.y);
     }
   }
-  return numbers;
 }
 
 template <int HD, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
   __shared__ BadSlots s_bad;
   if (threadIdx.x == 0) s_bad = BadSlots{1 << 30, -1, 0};
-  if (!work_tile<HD, WAVES, false>(a, s_bad)) s_bad.again = 1;
-  wait_memory_ops();   // (what has been written is written over)
+  work_tile<HD, WAVES, false>(a, s_bad);
   __syncthreads();
   if (!__builtin_amdgcn_readfirstlane(s_bad.again)) return;
   __syncthreads();
@@ -797,12 +811,13 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
     }
   };
   fetch(group);
-  bool ours = false, small = false;   // somebody's row; some of its parts are 2^32 smaller
-  for (int s = lane; s < a.batch.n; s += LANES) ours |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1];
+  constexpr int OURS = 1, SMALL = 2;   // somebody's row; some of its parts are 2^32 smaller
+  int is = 0;
+  for (int s = lane; s < a.batch.n; s += LANES) is |= a.batch.starts[s] <= r && r < a.batch.starts[s + 1] ? OURS : 0;
   float l = 0.f, m = -INFINITY;
   for (int s = lane; s < a.splits; s += LANES) {
     float2 x = a.part_ml[s * step + i];
-    small |= x.y < 0.f;
+    is |= x.y < 0.f ? SMALL : 0;
     x.y = fabsf(x.y);
     const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
     l = (l == 0.f ? 0.f : l * ca_exp2(m - base)) + (x.y == 0.f ? 0.f : x.y * ca_exp2(x.x - base));
@@ -812,16 +827,15 @@ __global__ void __launch_bounds__(256) cached_join_k(AttendArgs a) {
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor(m, o, LANES));
-    ours |= __shfl_xor((int)ours, o, LANES) != 0;
-    small |= __shfl_xor((int)small, o, LANES) != 0;
+    is |= __shfl_xor(is, o, LANES);
   }
-  if (!ours) return;
+  if (!(is & OURS)) return;
   const float base = m == -INFINITY ? 0.f : m;
   l = l == 0.f ? 0.f : l * ca_exp2(mine - base);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, LANES);
   static_assert(MOST_SPLITS <= 256, "sums that fp32 holds, 2^8 smaller, have room");
-  const float scale = small ? 0x1p-32f : 0x1p-8f;
+  const float scale = is & SMALL ? 0x1p-32f : 0x1p-8f;
   ca_f32x4 y = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = group; s0 < a.splits; s0 += JOIN_AHEAD * GROUPS) {
     if (s0 > group) fetch(s0);

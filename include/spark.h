@@ -503,7 +503,8 @@ int spark_cache_attend(const spark_cache *cache, const spark_cache_batch *batch,
  * over the rows of s that see t and the query heads of kv_head of exp(scale q . k_t - lse), for t below the
  * sequence's length; a row with lse of minus infinity gives nothing.  q, scale and causal as for spark_cache_attend, lse as it wrote it.
  * out, before fp32 [n][n_kv_heads][max_pages * page_tokens], before may be out itself, or NULL (zeros); decay is finite, and
- * with 0 before is not read. */
+ * with 0 before is not read.  The way it is done goes by the rows that a sequence has on average: a batch of a long
+ * chunk and many single rows is faster in two calls. */
 int spark_cache_weigh(const spark_cache *cache, const spark_cache_batch *batch, int32_t n_q_heads, const void *q,
                       int64_t q_stride, float scale, int32_t causal, const float *lse, const float *before, float decay,
                       float *out, void *hip_stream);

@@ -154,7 +154,7 @@ def cached_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Page
                   out: torch.Tensor | None = None) -> torch.Tensor:
     """q [m][q_heads][head_dim], k and v [m][kv_heads][head_dim] (fp32 or bf16, one type; views of one product's rows will do): heads of q and k
     normed where a gain (fp32 [head_dim]) is given, turned by position (positions int32 [m], or each row's slot), k and v written to their rows'
-    slots of the cache; returns q in the cache's type (`out`; may be q itself)."""
+    slots of the cache; returns q in the cache's type (`out`; may be q itself), whose rows that are no sequence's are not written."""
     hd = cache.head_dim
     q_at, q_stride = _heads(q, "q", hd, _DTYPE)
     m, heads, _ = q.shape
@@ -221,7 +221,7 @@ def cached_attend(q: torch.Tensor, cache: PagedCache, batch: CachedRows, layer: 
                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
     """softmax(scale q k^T) v over the slots that each row sees, [m][q_heads][head_dim] in the cache's type, q's too; scale: by default
     head_dim^-1/2; causal: a row sees the slots up to its own, else all of its sequence.  lse (fp32 [m][q_heads]) is given the
-    logarithm of each row's sum.  A row that sees nothing: zeros, and minus infinity."""
+    logarithm of each row's sum.  A row that sees nothing: zeros, and minus infinity; rows that are no sequence's are not written."""
     hd = cache.head_dim
     at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape
@@ -250,7 +250,8 @@ def cached_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: C
                  causal: bool = True, before: torch.Tensor | None = None, decay: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
     """The attention weight of each slot, fp32 [n][kv_heads][slots a sequence has at most]: decay * before (zeros without) + the probabilities
     that the batch's rows gave it, summed over rows and the heads of its group; q, scale and causal as cached_attend had them, lse
-    from it.  Slots behind a sequence's length are left alone (zeros in a new result).  out may be before."""
+    from it.  Slots behind a sequence's length are left alone (zeros in a new result).  out may be before.  (A batch of a long chunk and many single rows is
+    faster in two calls.)"""
     hd = cache.head_dim
     at, stride = _heads(q, "q", hd, cache._types)
     m, heads, _ = q.shape

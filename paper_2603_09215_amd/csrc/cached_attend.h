@@ -107,7 +107,7 @@ template <typename T, int HD> __device__ __forceinline__ int ca_turn(int row) {
 // numbered from a place that its first row gives: that row times a row's tiles, or its pairs before, in tiles, and one for every
 // sequence before, each of which may leave a tile unfilled.  (Which: attend_tiles_by_row.)  So some numbers are nobody's, and the sequence
 // is the last one whose place is not behind the tile: found in steps of 64, one up to 64 sequences, where a count over all
-// of them takes a step for each 64 (a step's attention of 512 dialogues of up to 250 slots: 49 us, counted 56; of 2048 174 and 279).
+// of them takes a step for each 64 (a step's attention of 2048 dialogues of up to 250 slots: 279 us with the count, 174 with this; 180 since probabilities have two parts).
 // Called by whole waves.
 __device__ __forceinline__ bool find_tile(const BatchView &b, int page_tokens, int group, int per_tile, bool by_row, int tile, Sequence &q, int &t, int &count) {
   const int lane = threadIdx.x & 63, each = (group + per_tile - 1) / per_tile;
@@ -197,7 +197,7 @@ __device__ __forceinline__ void finish(const AttendArgs &a, int split, int r, in
 // Tiles of 16 pairs; four waves, each with every fourth piece of TOKENS tokens of the workgroup's.  Matrix instructions of 16 x 16:
 //   A of the scores: a lane's token is l mod 16, its k values come straight from the cache, 16 bytes a load;
 //   A of the values: bf16 through LDS of the wave's own, read transposed; fp32 straight from the cache.
-// The next piece's loads are on their way while a piece is worked on.  32 steps over up to 8191 slots, 32 + 2 heads of 128: 42 us, 4.8 TB/s.
+// The next piece's loads are on their way while a piece is worked on.  32 steps over up to 8191 slots, 32 + 2 heads of 128: 45 us, 4.5 TB/s.
 template <typename T, int HD> struct Stream {
   static constexpr int PAIRS = 16, WAVES = 4, TOKENS = sizeof(T) == 2 ? 32 : 16, BLOCKS = TOKENS / 16;
   static constexpr int STEPS = HD * (int)sizeof(T) / 64;                        // 16-byte loads of a lane for 16 tokens' keys
@@ -480,8 +480,8 @@ __global__ void __launch_bounds__(256, 2) cached_stream_k(AttendArgs a) {
 
 // WAVES waves of 32 pairs each, bf16; tiles of 64 tokens' keys and values in LDS, two of them, so that the next one's loads run while one is
 // worked on.  Matrix instructions of 32 x 32 (A: a lane's token or head element is l mod 32, its k those of l / 32); a lane
-// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.  8191 rows of 28 heads of 128: 711 us, 1015 TFLOP/s with the second part's
-// products (one part took 545), where a library's product reaches 1140.  (fp32's matrix instructions
+// holds 32 of a tile's 64 scores of its pair, the other half of the wave the others.  8191 rows of 28 heads of 128: 694 us, 1040 TFLOP/s with the second part's
+// products (one part took 537), where a library's product reaches 1140.  (fp32's matrix instructions
 // take so long that the stream keeps up: such a kernel took 339 us against 361 for 2000 rows of 28 heads, 106 against 101 for 16 heads of 64.)
 template <int HD, int WAVES> struct Tile {
   static constexpr int TOKENS = 64, PAIRS = 32 * WAVES;
@@ -742,7 +742,7 @@ __device__ __forceinline__ void work_tile(const AttendArgs &a, BadSlots &s_bad) 
     }
   }
   // Through LDS, 32 elements at a time, so that eight lanes write 32 elements of a pair next to each other (straight from the registers, where a
-  // store's lanes are 16 bytes of 64 rows: 542 us for 8191 rows instead of 523).
+  // store's lanes are 16 bytes of 64 rows: 19 us more for 8191 rows).
   float *s_o = (float *)ca_smem + wave * 32 * S::O_PITCH;
   float2 *s_ml = (float2 *)((float *)ca_smem + S::PAIRS * S::O_PITCH) + wave * 32;
   if (half == 0) s_ml[col] = make_float2(top, sum);
@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) cached_tile_k(AttendArgs a) {
 
 // ------------------------------------------------------------------ the parts together
 
-constexpr int JOIN_AHEAD = 4;   // parts on their way (both launches, a group of lanes to a vector: one step of 28 heads in 13 parts, one 12.7 us, four 10.9, eight 10.5, sixteen 10.3;
+constexpr int JOIN_AHEAD = 4;   // parts on their way (both launches, a group of lanes to a vector, probabilities of one part: one step of 28 heads in 13 parts, one 12.7 us, four 10.9, eight 10.5, sixteen 10.3;
                                 // 511 rows in 4 parts 39.8, 40.1, 40.5, 44.3)
 
 // GROUPS of lanes to a vector, each with every GROUPS-th part, whose sums are added in their order.

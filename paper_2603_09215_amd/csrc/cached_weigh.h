@@ -4,12 +4,12 @@
 //
 // With few rows bound by the keys' way through memory, with many by the exponentials and the queries' way out of L2.  A wave takes 32 tokens, whose keys
 // stay in registers, and goes through the (row, head) pairs in blocks of 32: scores S [pair][token] = Q K^T, so that a lane has 16 scores of one
-// token and its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens (in bf16 two pieces of 32, for each block's
-// queries come from L2, 134 MB for 1024 pairs of 8191 slots and two heads with one piece, which took 20 us; each wave loads an eighth of the keys,
-// 14.1 us, where each loading them all took 16.2; and operands of queries read from LDS as they are used 12.3), deal out the blocks, the next one's queries on their way while one is worked on, and add up
-// their sums in order.  (Of 16.2: without the exponentials 13, without the queries 13.7, with a quarter of the blocks 9.  Sixteen waves 14.8 against 14.1.)  Few:
-// each wave has its own tokens, the next ones' keys are on their way while they are worked on, and a single block's queries stay.
-// Nothing is added by atomics.
+// token and its sum is one register.  Many pairs: the eight waves of a workgroup share their tokens, each loading an eighth of their keys, deal out the
+// blocks, the next one's queries on their way while one is worked on, and add up their sums in order.  1024 pairs of 8191 slots and two heads, bf16: 12.4 us.
+// On the way there: one piece of 32 tokens instead of two, so twice the queries out of L2 (134 MB), 20; two 16.2 (3.2 of it exponentials, 2.5 queries); keys
+// loaded once 14.1 (sixteen waves 14.8); operands of queries read from LDS as they are used 12.3.  Few: each wave has its own tokens, the next ones' keys are on
+// their way while they are worked on, and a single block's queries stay: 32 steps of up to 4095 slots, 4 heads, 25 us, 4.1 TB/s.
+// Nothing is added by atomics.  What a wave's blocks lose in their additions is carried along, so the error does not grow with the rows.
 #pragma once
 #include "cached_attend.h"
 
@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(MANY ? 512 : 256) cached_weigh_k(WeighArgs a) 
       for (int i = 0; i < STEPS; ++i) k[j][i] = *(const ca_u32x4 *)(at + 32 * i);
     }
   };
-  // Queries of block b and their lse.  As operands (few pairs), or whole rows in the lanes' order (many: 16.2 us for 1024 pairs
-  // of 8191 slots and two heads, where 32 bytes of each of 32 rows a load took 16.9) that go to LDS.
+  // Queries of block b and their lse.  As operands (few pairs), or whole rows in the lanes' order (many: 0.7 us
+  // less, of 16.9 at the time, than with 32 bytes of each of 32 rows a load) that go to LDS.
   constexpr int VECS = 2 * STEPS;   // of a query
   auto load_queries = [&](int b, ca_u32x4 (&q)[STEPS], float &lse) {
     const int first = b * 32 / a.group, past = b * 32 - first * a.group, most = pairs - 1 - b * 32;   // (pairs past the last: that one, left out)

@@ -20,7 +20,7 @@
 // them get from them is added at the end (a probability is positive: infinity stays, NaN too).  Slots that all rows see are not
 // looked at: if sums that are no numbers come of them, the tile is worked on AGAIN, and takes them all so.  Sums of large values may
 // have left fp32's range before they were divided by L: the second time all probabilities are 2^32 smaller (2^23 slots of up to 2^8 each have room), which
-// changes no bit of what was in range; parts say so by a negative sum.
+// changes no bit of what was in range (but for products below 2^-94, which come close to the smallest numbers); parts say so by a negative sum.
 #pragma once
 #include "cached_format.h"
 #include "cached_plan.h"
